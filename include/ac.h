@@ -73,6 +73,9 @@ typedef enum {
 #define AC_FLAG_POSITION_OOB 2 /* context_lens[b] >= max_position or its page index >= max_pages_per_seq; in the
                                   single-launch step also context_lens[b] + 1 > the tokens the split grid covers */
 #define AC_FLAG_WAIT_TIMEOUT 4 /* a bounded wait on a shared-memory barrier gave up */
+#define AC_FLAG_POOL_EXHAUSTED 8 /* ac_cache_reserve / ac_cache_fork: fewer free pages than the call needs */
+#define AC_FLAG_REF_COUNT 16 /* a page that a row holds has reference count 0 (released twice, or never taken) */
+#define AC_FLAG_ROW_OOB 32 /* a row index outside the block table */
 
 /* Once per device, outside any stream capture, with no other call of this library running on that
  * device: reads the device properties, resolves the driver's tensor-map encoder and sets the
@@ -117,6 +120,11 @@ int ac_decode_plan_for_lengths(const int32_t* token_counts_host, int B, int Hq, 
 /* Tokens per split the attention kernel uses for a given (max_context_len, num_splits): the smallest
  * multiple of 64 whose num_splits-fold covers max_context_len.  Host only, pure. */
 int ac_split_tokens(int max_context_len, int num_splits);
+
+/* Largest number of tokens a row is partitioned over under a sliding window with sinks: window + 63, plus
+ * sinks rounded up to a multiple of 16 when there are any; INT_MAX for window <= 0 (no bound but the
+ * context).  Host only, pure. */
+int ac_window_span(int window, int sinks);
 
 /* Workspace bytes for (B, Hq, d, num_splits): partial_o fp32 [B,Hq,num_splits,d] followed by
  * partial_lse fp32 [B,Hq,num_splits]; 0 when num_splits == 1.  Host only, pure. */
@@ -322,14 +330,22 @@ typedef struct ac_attn_options {
                         RMSNorm, partial rotary, interleaved pairing) applied to q_in and k_new inside the
                         step, with the arithmetic and the table shapes of ac_rope_kv_append_ex; NULL or
                         all-default options = the plain rotation */
-    int reserved[2];
+    int sinks;       /* >= 0: with a window, the row's first `sinks` tokens stay visible beside it, i.e. the row
+                        attends over tokens t < sinks and max(0, n_b - window) .. n_b - 1; no effect
+                        without a window (every token is visible then) */
+    int reserved[1];
 } ac_attn_options;
 
 /* ac_paged_decode_attn / ac_paged_decode_attn_fused_merge / ac_decode_step_fused with options
  * (options == NULL means defaults).  With a window, tokens before the window's start are neither
  * read (whole tiles) nor weighted (the first tile masks them), so their pages may already have been
  * recycled; the splits partition the at most window + 63 tokens from the window's start rounded
- * down to a multiple of 64, so pass min(max_context_len, window + 63) to ac_decode_plan. */
+ * down to a multiple of 64, so pass min(max_context_len, window + 63) to ac_decode_plan.
+ * With sinks > 0 the tokens between the sinks and the window are skipped in the same way (whole tiles
+ * of 16 are not read, the tiles at the two borders mask theirs); the splits then partition the at most
+ * window + sinks + 30 tokens of the two pieces laid end to end, so pass
+ * min(max_context_len, ac_window_span(window, sinks)) to ac_decode_plan.  The softmax scale, the positions
+ * of the rotary embedding and the append are those of the row without a window. */
 int ac_paged_decode_attn_ex(const void* q_rot, const void* k_cache, const void* v_cache,
                             int64_t stride_page, int64_t stride_token, int64_t stride_head,
                             const int32_t* block_table, int max_pages_per_seq,
@@ -437,6 +453,150 @@ int ac_paged_decode_attn_static_scratch(const void* q_rot, const void* k_cache, 
                                         float softmax_scale, int num_splits, void* out, int B, int Hq,
                                         int Hkv, int d, int page_size, int num_pages,
                                         int max_context_len, int32_t* status_flag, void* stream);
+
+/* ---- the cache held in 4 bits --------------------------------------------------------------------
+ *
+ * A quarter of the bf16 cache's bytes per token, plus parameters.  A group of `group` consecutive
+ * elements (x_0, x_1, ...) of one token and KV head is held as
+ *   minimum m = min x_i,  scale s = bf16(fp32((max x_i - m) / 15))  (both bf16; the quotient in fp64),
+ *   codes   c_i = clamp(rint((x_i - m) / s), 0, 15)                 (fp64, ties to even; 0 when s = 0),
+ * and stands for c_i * s + m.  x is bf16: the rotated, bf16-rounded key, or the value vector.  A group
+ * that contains an infinity or a NaN is held as m = NaN, s = 0, c = 0 and reads back as NaN.
+ *
+ * Codes are two to a byte, element 2i in the low nibble of byte i.  They sit in two pools with caller's
+ * strides, like the bf16 cache; the parameters of K and V sit together in one dense pool, in which the
+ * slots of one page and head are contiguous whatever the codes' layout. */
+typedef struct ac_q4_cache {
+    void* k_codes;           /* byte j of (page, slot, head) at page*stride_page + slot*stride_token + head*stride_head + j, */
+    void* v_codes;           /* j < d/2; 16-byte aligned bases, strides in BYTES, multiples of 16, token and head >= d/2 */
+    void* params;            /* bf16 [num_pages, Hkv, page_size, 2 (K, V), d/group, 2 (s, m)], 16-byte aligned */
+    int64_t stride_page, stride_token, stride_head;
+    int group;               /* 32, 64 or 128, at most d */
+    int reserved[3];
+} ac_q4_cache;
+
+/* ac_rope_kv_append_ex into a 4-bit cache: q is rotated into q_out bit for bit as there; k is normalised
+ * and rotated as there, rounded to bf16 and then quantised, v is quantised as it is.  Rows that are
+ * inactive or out of range behave as there.  Supported shapes, errors and status bits as there; the
+ * cache's group must be one of 32, 64, 128 and at most d (AC_ERR_UNSUPPORTED). */
+int ac_rope_kv_append_q4(const void* q_in, void* q_out, const void* k_new, const void* v_new,
+                         const ac_q4_cache* cache, const int32_t* block_table, int max_pages_per_seq,
+                         const int32_t* context_lens, const float* rope_cos, const float* rope_sin,
+                         int max_position, int B, int Hq, int Hkv, int d, int page_size, int num_pages,
+                         int32_t* status_flag, void* stream, const ac_rope_options* options);
+
+/* Quantises many tokens of each row at once (a prompt whose keys are already rotated).  k, v are dense
+ * bf16 [total_tokens, Hkv, d]; row b owns the tokens row_offsets[b] .. row_offsets[b+1] - 1 and its i-th
+ * one is written to position start_pos[b] + i, i.e. page block_table[b, position / page_size].  row_offsets
+ * is device int32 [B + 1], non-decreasing from 0; tokens at or past row_offsets[B] are ignored, rows with
+ * start_pos[b] < 0 are inactive and write nothing.  total_tokens may be 0.  A token whose position or page
+ * is out of range writes nothing and sets the status bits of ac_rope_kv_append.  Two tokens of one call in
+ * the same slot are a caller error. */
+int ac_kv_store_q4(const void* k, const void* v, const ac_q4_cache* cache, const int32_t* block_table,
+                   int max_pages_per_seq, const int32_t* start_pos, const int32_t* row_offsets,
+                   int total_tokens, int B, int Hkv, int d, int page_size, int num_pages,
+                   int32_t* status_flag, void* stream);
+
+/* The reverse: reads the same tokens back as bf16(fp32(c * s + m)) into dense k, v [total_tokens, Hkv, d].
+ * Tokens of inactive rows, at or past row_offsets[B], or out of range (status bits set) read as +0. */
+int ac_kv_load_q4(void* k, void* v, const ac_q4_cache* cache, const int32_t* block_table,
+                  int max_pages_per_seq, const int32_t* start_pos, const int32_t* row_offsets,
+                  int total_tokens, int B, int Hkv, int d, int page_size, int num_pages,
+                  int32_t* status_flag, void* stream);
+
+/* Split plan for ac_paged_decode_attn_q4: arguments and outputs as ac_decode_plan_for_lengths, except that
+ * token_counts_host may be NULL (every row then counts max_context_len tokens) and the workspace is the
+ * one of the fused merge (ac_fused_workspace_bytes).  Host only, pure; any plan gives the same results. */
+int ac_decode_plan_q4(const int32_t* token_counts_host, int B, int Hq, int Hkv, int d, int page_size,
+                      int max_context_len, int sm_count, int* num_splits_out, int* split_tokens_out,
+                      size_t* workspace_bytes_out);
+
+/* Paged decode attention over the 4-bit cache, merge included: ac_paged_decode_attn_ex with fused_merge
+ * set (grid, splits, workspace, inactive rows, window, sinks, row_order, max_context_len and status bits as
+ * there; options->rope must be NULL).  K and V enter as the exact values c * s + m; q is bf16, products
+ * and sums are fp32, and the softmax weights times a V group's scale are rounded to fp16 (2^-11 relative, or
+ * 2^-31 of the largest V scale seen, whichever is more) for the second product.  Queries of magnitude 2^116
+ * and more are outside the supported range.  Slots at or past n_b, unreferenced pages and unused
+ * block-table entries never influence the result; a page id outside [0, num_pages) reads as zeros. */
+int ac_paged_decode_attn_q4(const void* q_rot, const ac_q4_cache* cache, const int32_t* block_table,
+                            int max_pages_per_seq, const int32_t* context_lens, int new_tokens,
+                            float softmax_scale, int num_splits, void* workspace, size_t workspace_bytes,
+                            void* out, int B, int Hq, int Hkv, int d, int page_size, int num_pages,
+                            int max_context_len, int32_t* status_flag, void* stream,
+                            const ac_attn_options* options);
+
+/* ---- pages ----------------------------------------------------------------------------------------
+ *
+ * Bookkeeping of a page pool on the device, so that sequences can be grown, forked and dropped between
+ * steps without a copy to the host.  State, all int32 in device memory: block_table [rows,
+ * max_pages_per_seq], context_lens [rows] (tokens held; < 0: the row is unused) and ref_counts [num_pages]
+ * (rows that hold the page; 0: free).  A row holds its first ceil(context_lens / page_size) pages, after
+ * ac_cache_reserve also those of the reserved tokens until context_lens grows to count them.
+ *
+ * Free pages are handed out lowest index first, in the order of the call's list, so every call's
+ * result is determined by its inputs.  The pools themselves are opaque bytes: any number of them (K and V
+ * of every layer, codes, parameters) can share one block table. */
+typedef struct ac_page_pool {
+    void* base;              /* page p occupies bytes [p*page_bytes, (p+1)*page_bytes); 16-byte aligned */
+    int64_t page_bytes;      /* a multiple of 16 * segments */
+    int segments;            /* a page is this many equal pieces, each holding the page's slots in order: 1 for
+                                [page, slot, head, d], Hkv for [page, head, slot, ...] */
+    int reserved;
+} ac_page_pool;
+
+/* Most pools of one call. */
+#define AC_MAX_PAGE_POOLS 128
+
+/* Copies whole pages, pairs[i] = (source, destination), device int32 [n, 2], in every pool.  A pair with a
+ * page outside [0, num_pages) is skipped and sets AC_FLAG_PAGE_OOB; source == destination is a no-op.  A
+ * destination that is listed twice or is also a source is a caller error.  n may be 0. */
+int ac_cache_copy_pages(const ac_page_pool* pools, int n_pools, const int32_t* pairs, int n, int num_pages,
+                        int32_t* status_flag, void* stream);
+
+/* Bytes of workspace the next three calls need: host only, pure. */
+size_t ac_cache_workspace_bytes(int rows, int num_pages, int n);
+
+/* Gives every active row room for new_tokens more tokens: pages ceil(n/page_size) .. ceil((n + new_tokens) /
+ * page_size) - 1 of the row are taken from the free pages (reference count 1), rows in order.  Pages are
+ * taken again at each call: reserve, then let context_lens grow by new_tokens before reserving anew.
+ * When the free pages run out, the row that does not get all of its pages and every later row that needs
+ * any get none, and AC_FLAG_POOL_EXHAUSTED is set; a row whose pages would exceed max_pages_per_seq gets
+ * none and sets AC_FLAG_POSITION_OOB. */
+int ac_cache_reserve(int32_t* block_table, int max_pages_per_seq, const int32_t* context_lens,
+                     int32_t* ref_counts, int new_tokens, int rows, int page_size, int num_pages,
+                     void* workspace, size_t workspace_bytes, int32_t* status_flag, void* stream);
+
+/* Forks: pairs[i] = (parent row, child row), device int32 [n, 2].  The child holds the parent's full pages
+ * too (reference counts go up) and, where the parent's last page is partly filled, a page of its own
+ * with a copy of the filled slots in every pool; context_lens[child] = context_lens[parent].  What else the
+ * page and the child's table row held stays as it was.  The child row must be unused before (its
+ * old pages are not released); a child listed twice, or that is also a parent, is a caller error; one parent
+ * may have many children.  A fork whose page the pool cannot supply makes its child unused and sets
+ * AC_FLAG_POOL_EXHAUSTED; an unused parent gives an unused child.  n_pools may be 0 (bookkeeping only). */
+int ac_cache_fork(const ac_page_pool* pools, int n_pools, int32_t* block_table, int max_pages_per_seq,
+                  int32_t* context_lens, int32_t* ref_counts, const int32_t* pairs, int n, int rows,
+                  int page_size, int num_pages, void* workspace, size_t workspace_bytes,
+                  int32_t* status_flag, void* stream);
+
+/* Drops the rows listed in row_list (device int32 [n]): the reference counts of their pages go down and
+ * context_lens[row] becomes -1; the table entries stay.  A row that is unused, or listed again, is a
+ * no-op.  A count that is already 0 stays 0 and sets AC_FLAG_REF_COUNT. */
+int ac_cache_release(const int32_t* block_table, int max_pages_per_seq, int32_t* context_lens,
+                     int32_t* ref_counts, const int32_t* row_list, int n, int rows, int page_size,
+                     int num_pages, int32_t* status_flag, void* stream);
+
+/* Moves the live pages (reference count > 0) to the lowest ids: with L of them, the live pages at ids >= L
+ * move, in order, to the free ids < L, in every pool, and the block table entries of the active rows and the
+ * reference counts follow; *live_out (optional) = L.  Only free pages are written, so a step in flight
+ * that still reads the old table reads the same bytes until those pages are handed out again.  The new
+ * table and counts go to block_table_out and ref_counts_out, which may be the inputs themselves or other
+ * buffers of the same shape (both or neither aliased); context_lens does not change.  Table entries past a
+ * row's pages and rows that are not active are copied as they are: call it with nothing reserved. */
+int ac_cache_compact(const ac_page_pool* pools, int n_pools, const int32_t* block_table,
+                     int32_t* block_table_out, int max_pages_per_seq, const int32_t* context_lens,
+                     const int32_t* ref_counts, int32_t* ref_counts_out, int rows, int page_size,
+                     int num_pages, int32_t* live_out, void* workspace, size_t workspace_bytes,
+                     int32_t* status_flag, void* stream);
 
 #ifdef __cplusplus
 }

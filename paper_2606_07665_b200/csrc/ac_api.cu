@@ -1,4 +1,5 @@
 // The C ABI of libac: argument validation, the split plan, tensor-map construction and the launches.
+#include <limits.h>
 #include <math.h>
 #include <stdlib.h>
 
@@ -142,6 +143,7 @@ int ac_init(int device) {
         e = attn_set_attributes(st.smem_optin);
         if (e == cudaSuccess) e = qkv_set_attributes(st.smem_optin);
         if (e == cudaSuccess) e = proj_tc_set_attributes(st.smem_optin);
+        if (e == cudaSuccess) e = q4_attn_set_attributes(st.smem_optin);
         if (e != cudaSuccess) {
             status = fail_cuda(static_cast<int>(e));
             break;
@@ -177,6 +179,13 @@ int ac_sm_count(void) { return g_last_sm_count; }
 
 int ac_split_tokens(int max_context_len, int num_splits) {
     return split_tokens_for(max_context_len, num_splits);
+}
+
+int ac_window_span(int window, int sinks) {
+    if (window <= 0) return INT_MAX;
+    const long long span = static_cast<long long>(window) + 63 +
+                           (sinks > 0 ? (static_cast<long long>(sinks) + 15) / 16 * 16 : 0);
+    return span < INT_MAX ? static_cast<int>(span) : INT_MAX;
 }
 
 size_t ac_workspace_bytes(int B, int Hq, int d, int num_splits) {
@@ -589,13 +598,14 @@ static int attn_common(const void* q_rot, const void* k_cache, const void* v_cac
                        float softmax_scale, int num_splits, void* workspace, size_t workspace_bytes,
                        void* out, int B, int Hq, int Hkv, int d, int page_size, int num_pages,
                        int max_context_len, int32_t* status_flag, void* stream, bool fused_merge,
-                       const FusedRopeArgs* rope = nullptr, int window = 0,
+                       const FusedRopeArgs* rope = nullptr, int window = 0, int sinks = 0,
                        const int32_t* row_order = nullptr) {
     if (!q_rot || !k_cache || !v_cache || !block_table || !context_lens) return AC_ERR_NULL;
     Shape s{B, Hq, Hkv, d, page_size, num_pages};
     int st = check_shape(s);
     if (st != AC_OK) return st;
-    if (max_pages_per_seq <= 0 || max_context_len <= 0 || num_splits <= 0) return AC_ERR_SHAPE;
+    if (max_pages_per_seq <= 0 || max_context_len <= 0 || num_splits <= 0 || window < 0 || sinks < 0)
+        return AC_ERR_SHAPE;
     if (new_tokens != 0 && new_tokens != 1) return AC_ERR_UNSUPPORTED;
     if (num_splits > 65535) return AC_ERR_UNSUPPORTED;
     st = check_strides(s, stride_page, stride_token, stride_head);
@@ -628,15 +638,14 @@ static int attn_common(const void* q_rot, const void* k_cache, const void* v_cac
     if (st != AC_OK) return st;
     const float scale = softmax_scale > 0.0f ? softmax_scale : 1.0f / sqrtf(static_cast<float>(d));
     // With a sliding window a row attends over at most window + 63 tokens (its range starts at a
-    // multiple of 64 at or below the window's first token).
-    if (window < 0) return AC_ERR_SHAPE;
-    const int span = (window > 0 && window + 63 < max_context_len) ? window + 63 : max_context_len;
-    const int split_tokens = split_tokens_for(span, num_splits);
+    // multiple of 64 at or below the window's first token), and over the sinks' tiles.
+    const int limit = ac_window_span(window, sinks);
+    const int split_tokens = split_tokens_for(limit < max_context_len ? limit : max_context_len, num_splits);
     cudaError_t e = launch_paged_decode_attn(k_map, v_map, q_rot, block_table,
                                              max_pages_per_seq, context_lens, new_tokens, scale,
                                              num_splits, split_tokens, partial_o, partial_lse, arrivals,
                                              out, B, Hq, Hkv, d, page_size, status_flag, rope, window,
-                                             row_order, static_cast<cudaStream_t>(stream));
+                                             sinks, row_order, static_cast<cudaStream_t>(stream));
     return e == cudaSuccess ? AC_OK : fail_cuda(static_cast<int>(e));
 }
 
@@ -707,6 +716,7 @@ static int decode_step_fused_impl(const void* q_in, void* q_rot_out, const void*
                                   int page_size, int num_pages, int max_context_len, int32_t* status_flag,
                                   void* stream, const ac_attn_options* options, void* out_mirror) {
     const int window = options != nullptr ? options->window : 0;
+    const int sinks = options != nullptr ? options->sinks : 0;
     const int32_t* row_order = options != nullptr ? options->row_order : nullptr;
     if (!q_in || !k_new || !v_new || !rope_cos || !rope_sin) return AC_ERR_NULL;
     if (max_position <= 0) return AC_ERR_SHAPE;
@@ -736,7 +746,7 @@ static int decode_step_fused_impl(const void* q_in, void* q_rot_out, const void*
     return attn_common(q_in, k_cache, v_cache, stride_page, stride_token, stride_head, block_table,
                        max_pages_per_seq, context_lens, 1, softmax_scale, num_splits, workspace,
                        workspace_bytes, out, B, Hq, Hkv, d, page_size, num_pages, max_context_len,
-                       status_flag, stream, true, &rope, window, row_order);
+                       status_flag, stream, true, &rope, window, sinks, row_order);
 }
 
 int ac_decode_step_fused_ex(const void* q_in, void* q_rot_out, const void* k_new, const void* v_new,
@@ -763,11 +773,12 @@ int ac_paged_decode_attn_ex(const void* q_rot, const void* k_cache, const void* 
                             int32_t* status_flag, void* stream, const ac_attn_options* options) {
     const bool fused = options != nullptr && options->fused_merge != 0;
     const int window = options != nullptr ? options->window : 0;
+    const int sinks = options != nullptr ? options->sinks : 0;
     const int32_t* row_order = options != nullptr ? options->row_order : nullptr;
     return attn_common(q_rot, k_cache, v_cache, stride_page, stride_token, stride_head, block_table,
                        max_pages_per_seq, context_lens, new_tokens, softmax_scale, num_splits, workspace,
                        workspace_bytes, out, B, Hq, Hkv, d, page_size, num_pages, max_context_len,
-                       status_flag, stream, fused, nullptr, window, row_order);
+                       status_flag, stream, fused, nullptr, window, sinks, row_order);
 }
 
 int ac_splitkv_merge(const void* workspace, int num_splits, const int32_t* context_lens, void* out,
@@ -872,6 +883,294 @@ int ac_decode_step_host(const void* q_host, const void* k_new_host, const void* 
                                 status_flag, stream, nullptr, mirror);
     if (st != AC_OK || mirror != nullptr) return st;
     e = cudaMemcpyAsync(out_host, out, q_bytes, cudaMemcpyDeviceToHost, cs);
+    return e == cudaSuccess ? AC_OK : fail_cuda(static_cast<int>(e));
+}
+
+// ---- the 4-bit cache ------------------------------------------------------------------------------
+
+// Checks the cache descriptor against the shape and translates it.
+static int parse_q4_cache(const ac_q4_cache* cache, const Shape& s, Q4View* view) {
+    if (!cache || !cache->k_codes || !cache->v_codes || !cache->params) return AC_ERR_NULL;
+    if (cache->group != 32 && cache->group != 64 && cache->group != 128) return AC_ERR_UNSUPPORTED;
+    if (cache->group > s.d) return AC_ERR_UNSUPPORTED;
+    if (cache->stride_page <= 0 || cache->stride_token <= 0 || cache->stride_head <= 0) return AC_ERR_SHAPE;
+    if (cache->stride_page % 16 || cache->stride_token % 16 || cache->stride_head % 16) return AC_ERR_ALIGN;
+    if (cache->stride_token < s.d / 2 || cache->stride_head < s.d / 2) return AC_ERR_SHAPE;
+    if (!aligned16(cache->k_codes) || !aligned16(cache->v_codes) || !aligned16(cache->params)) return AC_ERR_ALIGN;
+    view->k_codes = static_cast<uint8_t*>(cache->k_codes);
+    view->v_codes = static_cast<uint8_t*>(cache->v_codes);
+    view->params = static_cast<uint32_t*>(cache->params);
+    view->stride_page = cache->stride_page;
+    view->stride_token = cache->stride_token;
+    view->stride_head = cache->stride_head;
+    view->group = cache->group;
+    return AC_OK;
+}
+
+int ac_rope_kv_append_q4(const void* q_in, void* q_out, const void* k_new, const void* v_new,
+                         const ac_q4_cache* cache, const int32_t* block_table, int max_pages_per_seq,
+                         const int32_t* context_lens, const float* rope_cos, const float* rope_sin,
+                         int max_position, int B, int Hq, int Hkv, int d, int page_size, int num_pages,
+                         int32_t* status_flag, void* stream, const ac_rope_options* options) {
+    if (!q_in || !q_out || !k_new || !v_new || !block_table || !context_lens || !rope_cos || !rope_sin)
+        return AC_ERR_NULL;
+    Shape s{B, Hq, Hkv, d, page_size, num_pages};
+    int st = check_shape(s);
+    if (st != AC_OK) return st;
+    if (max_pages_per_seq <= 0 || max_position <= 0) return AC_ERR_SHAPE;
+    Q4View view;
+    st = parse_q4_cache(cache, s, &view);
+    if (st != AC_OK) return st;
+    if (!aligned16(q_in) || !aligned16(q_out) || !aligned16(k_new) || !aligned16(v_new) ||
+        !aligned16(rope_cos) || !aligned16(rope_sin))
+        return AC_ERR_ALIGN;
+    RopeVariant variant;
+    const RopeVariant* vp = nullptr;
+    st = parse_rope_options(options, d, &variant, &vp);
+    if (st != AC_OK) return st;
+    int dev;
+    st = current_ready_device(&dev);
+    if (st != AC_OK) return st;
+    cudaError_t e = launch_rope_kv_append_q4(q_in, q_out, k_new, v_new, view, block_table, max_pages_per_seq,
+                                             context_lens, rope_cos, rope_sin, max_position, B, Hq, Hkv, d,
+                                             page_size, num_pages, status_flag, vp,
+                                             static_cast<cudaStream_t>(stream));
+    return e == cudaSuccess ? AC_OK : fail_cuda(static_cast<int>(e));
+}
+
+static int kv_bulk_q4(void* k, void* v, const ac_q4_cache* cache, const int32_t* block_table,
+                      int max_pages_per_seq, const int32_t* start_pos, const int32_t* row_offsets,
+                      int total_tokens, int B, int Hkv, int d, int page_size, int num_pages,
+                      int32_t* status_flag, void* stream, bool store) {
+    if (!k || !v || !block_table || !start_pos || !row_offsets) return AC_ERR_NULL;
+    Shape s{B, Hkv, Hkv, d, page_size, num_pages};
+    int st = check_shape(s);
+    if (st != AC_OK) return st;
+    if (max_pages_per_seq <= 0 || total_tokens < 0) return AC_ERR_SHAPE;
+    Q4View view;
+    st = parse_q4_cache(cache, s, &view);
+    if (st != AC_OK) return st;
+    if (!aligned16(k) || !aligned16(v)) return AC_ERR_ALIGN;
+    int dev;
+    st = current_ready_device(&dev);
+    if (st != AC_OK) return st;
+    if (total_tokens == 0) return AC_OK;
+    cudaError_t e = launch_kv_bulk_q4(k, v, view, block_table, max_pages_per_seq, start_pos, row_offsets,
+                                      total_tokens, B, Hkv, d, page_size, num_pages, status_flag, store,
+                                      static_cast<cudaStream_t>(stream));
+    return e == cudaSuccess ? AC_OK : fail_cuda(static_cast<int>(e));
+}
+
+int ac_kv_store_q4(const void* k, const void* v, const ac_q4_cache* cache, const int32_t* block_table,
+                   int max_pages_per_seq, const int32_t* start_pos, const int32_t* row_offsets,
+                   int total_tokens, int B, int Hkv, int d, int page_size, int num_pages,
+                   int32_t* status_flag, void* stream) {
+    return kv_bulk_q4(const_cast<void*>(k), const_cast<void*>(v), cache, block_table, max_pages_per_seq, start_pos,
+                      row_offsets, total_tokens, B, Hkv, d, page_size, num_pages, status_flag, stream, true);
+}
+
+int ac_kv_load_q4(void* k, void* v, const ac_q4_cache* cache, const int32_t* block_table,
+                  int max_pages_per_seq, const int32_t* start_pos, const int32_t* row_offsets,
+                  int total_tokens, int B, int Hkv, int d, int page_size, int num_pages,
+                  int32_t* status_flag, void* stream) {
+    return kv_bulk_q4(k, v, cache, block_table, max_pages_per_seq, start_pos, row_offsets, total_tokens, B, Hkv, d,
+                      page_size, num_pages, status_flag, stream, false);
+}
+
+int ac_decode_plan_q4(const int32_t* token_counts_host, int B, int Hq, int Hkv, int d, int page_size,
+                      int max_context_len, int sm_count, int* num_splits_out, int* split_tokens_out,
+                      size_t* workspace_bytes_out) {
+    if (!num_splits_out || !split_tokens_out || !workspace_bytes_out) return AC_ERR_NULL;
+    Shape s{B, Hq, Hkv, d, page_size, 1};
+    int st = check_shape(s);
+    if (st != AC_OK) return st;
+    if (max_context_len <= 0) return AC_ERR_SHAPE;
+    if (sm_count <= 0) sm_count = g_last_sm_count > 0 ? g_last_sm_count : 148;
+    long long tokens = static_cast<long long>(B) * max_context_len;
+    if (token_counts_host != nullptr) {
+        tokens = 0;
+        for (int b = 0; b < B; ++b)
+            if (token_counts_host[b] > 0)
+                tokens += token_counts_host[b] < max_context_len ? token_counts_host[b] : max_context_len;
+    }
+    // Two CTAs are resident per SM; aim at two waves of equal chunks of at least 256 tokens.
+    long long chunk = tokens * Hkv / (4ll * sm_count);
+    if (chunk < 256) chunk = 256;
+    long long S = (max_context_len + chunk - 1) / chunk;
+    if (S > 65535) S = 65535;
+    const int len = split_tokens_for(max_context_len, static_cast<int>(S));
+    S = (static_cast<long long>(max_context_len) + len - 1) / len;
+    *num_splits_out = static_cast<int>(S);
+    *split_tokens_out = split_tokens_for(max_context_len, static_cast<int>(S));
+    *workspace_bytes_out = ac_fused_workspace_bytes(B, Hq, Hkv, d, static_cast<int>(S));
+    return AC_OK;
+}
+
+int ac_paged_decode_attn_q4(const void* q_rot, const ac_q4_cache* cache, const int32_t* block_table,
+                            int max_pages_per_seq, const int32_t* context_lens, int new_tokens,
+                            float softmax_scale, int num_splits, void* workspace, size_t workspace_bytes,
+                            void* out, int B, int Hq, int Hkv, int d, int page_size, int num_pages,
+                            int max_context_len, int32_t* status_flag, void* stream,
+                            const ac_attn_options* options) {
+    (void)status_flag;                                     // no wait of this kernel can run out
+    const int window = options != nullptr ? options->window : 0;
+    const int sinks = options != nullptr ? options->sinks : 0;
+    const int32_t* row_order = options != nullptr ? options->row_order : nullptr;
+    if (!q_rot || !block_table || !context_lens || !out) return AC_ERR_NULL;
+    Shape s{B, Hq, Hkv, d, page_size, num_pages};
+    int st = check_shape(s);
+    if (st != AC_OK) return st;
+    if (max_pages_per_seq <= 0 || max_context_len <= 0 || num_splits <= 0 || window < 0 || sinks < 0)
+        return AC_ERR_SHAPE;
+    if ((new_tokens != 0 && new_tokens != 1) || num_splits > 65535) return AC_ERR_UNSUPPORTED;
+    if (options != nullptr && options->rope != nullptr) return AC_ERR_UNSUPPORTED;
+    Q4View view;
+    st = parse_q4_cache(cache, s, &view);
+    if (st != AC_OK) return st;
+    if (!aligned16(q_rot) || !aligned16(out)) return AC_ERR_ALIGN;
+    float* partial_o = nullptr;
+    float* partial_lse = nullptr;
+    int32_t* arrivals = nullptr;
+    if (num_splits > 1) {
+        if (!workspace || workspace_bytes < ac_fused_workspace_bytes(B, Hq, Hkv, d, num_splits)) return AC_ERR_WORKSPACE;
+        if (!aligned16(workspace)) return AC_ERR_ALIGN;
+        partial_o = static_cast<float*>(workspace);
+        partial_lse = partial_o + static_cast<size_t>(B) * Hq * num_splits * d;
+        arrivals = reinterpret_cast<int32_t*>(partial_lse + static_cast<size_t>(B) * Hq * num_splits);
+    }
+    int dev;
+    st = current_ready_device(&dev);
+    if (st != AC_OK) return st;
+    const float scale = softmax_scale > 0.0f ? softmax_scale : 1.0f / sqrtf(static_cast<float>(d));
+    const int limit = ac_window_span(window, sinks);
+    const int split_tokens = split_tokens_for(limit < max_context_len ? limit : max_context_len, num_splits);
+    cudaError_t e = launch_paged_decode_attn_q4(q_rot, view, block_table, max_pages_per_seq, context_lens, new_tokens,
+                                                scale, num_splits, split_tokens, partial_o, partial_lse, arrivals, out,
+                                                B, Hq, Hkv, d, page_size, num_pages, window, sinks, row_order,
+                                                static_cast<cudaStream_t>(stream));
+    return e == cudaSuccess ? AC_OK : fail_cuda(static_cast<int>(e));
+}
+
+// ---- pages ----------------------------------------------------------------------------------------
+
+static int check_pools(const ac_page_pool* pools, int n_pools, int page_size) {
+    if (n_pools < 0) return AC_ERR_SHAPE;
+    if (n_pools > AC_MAX_PAGE_POOLS) return AC_ERR_UNSUPPORTED;
+    if (n_pools > 0 && pools == nullptr) return AC_ERR_NULL;
+    for (int i = 0; i < n_pools; ++i) {
+        if (pools[i].base == nullptr) return AC_ERR_NULL;
+        if (pools[i].page_bytes <= 0 || pools[i].segments <= 0) return AC_ERR_SHAPE;
+        if (!aligned16(pools[i].base) || pools[i].page_bytes % (16ll * pools[i].segments) != 0) return AC_ERR_ALIGN;
+        if (page_size > 0 && pools[i].page_bytes / pools[i].segments % page_size != 0) return AC_ERR_SHAPE;
+    }
+    return AC_OK;
+}
+
+static int check_pages(int max_pages_per_seq, int rows, int page_size, int num_pages) {
+    if (max_pages_per_seq <= 0 || rows <= 0 || page_size <= 0 || num_pages <= 0) return AC_ERR_SHAPE;
+    if (num_pages > 1 << 30) return AC_ERR_UNSUPPORTED;
+    return AC_OK;
+}
+
+int ac_cache_copy_pages(const ac_page_pool* pools, int n_pools, const int32_t* pairs, int n, int num_pages,
+                        int32_t* status_flag, void* stream) {
+    if (!pairs) return AC_ERR_NULL;
+    if (n < 0 || num_pages <= 0 || n_pools <= 0) return AC_ERR_SHAPE;
+    int st = check_pools(pools, n_pools, 0);
+    if (st != AC_OK) return st;
+    if (reinterpret_cast<uintptr_t>(pairs) & 7u) return AC_ERR_ALIGN;
+    int dev;
+    st = current_ready_device(&dev);
+    if (st != AC_OK) return st;
+    if (n == 0) return AC_OK;
+    cudaError_t e = launch_copy_pages(pools, n_pools, pairs, n, num_pages, status_flag, g_devices[dev].sm_count,
+                                      static_cast<cudaStream_t>(stream));
+    return e == cudaSuccess ? AC_OK : fail_cuda(static_cast<int>(e));
+}
+
+size_t ac_cache_workspace_bytes(int rows, int num_pages, int n) {
+    if (rows <= 0 || num_pages <= 0 || n < 0) return 0;
+    // reserve: offsets [rows], pages [num_pages]; fork: jobs [n] of 8 bytes, used [n], pages [min(n, num_pages)];
+    // compact: head, moves [num_pages / 2 + 1] of 8 bytes, place [num_pages]
+    const size_t p = static_cast<size_t>(num_pages), r = static_cast<size_t>(rows), k = static_cast<size_t>(n);
+    return (32 + 8 * p + 8 * r + 16 * k + 15) / 16 * 16;
+}
+
+int ac_cache_reserve(int32_t* block_table, int max_pages_per_seq, const int32_t* context_lens,
+                     int32_t* ref_counts, int new_tokens, int rows, int page_size, int num_pages,
+                     void* workspace, size_t workspace_bytes, int32_t* status_flag, void* stream) {
+    if (!block_table || !context_lens || !ref_counts) return AC_ERR_NULL;
+    int st = check_pages(max_pages_per_seq, rows, page_size, num_pages);
+    if (st != AC_OK) return st;
+    if (new_tokens < 0) return AC_ERR_SHAPE;
+    if (!workspace || workspace_bytes < ac_cache_workspace_bytes(rows, num_pages, 0)) return AC_ERR_WORKSPACE;
+    if (!aligned16(ref_counts) || !aligned16(workspace)) return AC_ERR_ALIGN;
+    int dev;
+    st = current_ready_device(&dev);
+    if (st != AC_OK) return st;
+    if (new_tokens == 0) return AC_OK;
+    cudaError_t e = launch_reserve(block_table, max_pages_per_seq, context_lens, ref_counts, new_tokens, rows, page_size,
+                                   num_pages, workspace, status_flag, static_cast<cudaStream_t>(stream));
+    return e == cudaSuccess ? AC_OK : fail_cuda(static_cast<int>(e));
+}
+
+int ac_cache_fork(const ac_page_pool* pools, int n_pools, int32_t* block_table, int max_pages_per_seq,
+                  int32_t* context_lens, int32_t* ref_counts, const int32_t* pairs, int n, int rows,
+                  int page_size, int num_pages, void* workspace, size_t workspace_bytes,
+                  int32_t* status_flag, void* stream) {
+    if (!block_table || !context_lens || !ref_counts || !pairs) return AC_ERR_NULL;
+    int st = check_pages(max_pages_per_seq, rows, page_size, num_pages);
+    if (st != AC_OK) return st;
+    if (n < 0) return AC_ERR_SHAPE;
+    st = check_pools(pools, n_pools, page_size);
+    if (st != AC_OK) return st;
+    if (!workspace || workspace_bytes < ac_cache_workspace_bytes(rows, num_pages, n)) return AC_ERR_WORKSPACE;
+    if (!aligned16(ref_counts) || !aligned16(workspace) || (reinterpret_cast<uintptr_t>(pairs) & 7u)) return AC_ERR_ALIGN;
+    int dev;
+    st = current_ready_device(&dev);
+    if (st != AC_OK) return st;
+    if (n == 0) return AC_OK;
+    cudaError_t e = launch_fork(pools, n_pools, block_table, max_pages_per_seq, context_lens, ref_counts, pairs, n, rows,
+                                page_size, num_pages, workspace, status_flag, g_devices[dev].sm_count,
+                                static_cast<cudaStream_t>(stream));
+    return e == cudaSuccess ? AC_OK : fail_cuda(static_cast<int>(e));
+}
+
+int ac_cache_release(const int32_t* block_table, int max_pages_per_seq, int32_t* context_lens,
+                     int32_t* ref_counts, const int32_t* row_list, int n, int rows, int page_size,
+                     int num_pages, int32_t* status_flag, void* stream) {
+    if (!block_table || !context_lens || !ref_counts || !row_list) return AC_ERR_NULL;
+    int st = check_pages(max_pages_per_seq, rows, page_size, num_pages);
+    if (st != AC_OK) return st;
+    if (n < 0) return AC_ERR_SHAPE;
+    int dev;
+    st = current_ready_device(&dev);
+    if (st != AC_OK) return st;
+    if (n == 0) return AC_OK;
+    cudaError_t e = launch_release(block_table, max_pages_per_seq, context_lens, ref_counts, row_list, n, rows, page_size,
+                                   num_pages, status_flag, static_cast<cudaStream_t>(stream));
+    return e == cudaSuccess ? AC_OK : fail_cuda(static_cast<int>(e));
+}
+
+int ac_cache_compact(const ac_page_pool* pools, int n_pools, const int32_t* block_table,
+                     int32_t* block_table_out, int max_pages_per_seq, const int32_t* context_lens,
+                     const int32_t* ref_counts, int32_t* ref_counts_out, int rows, int page_size,
+                     int num_pages, int32_t* live_out, void* workspace, size_t workspace_bytes,
+                     int32_t* status_flag, void* stream) {
+    if (!block_table || !block_table_out || !context_lens || !ref_counts || !ref_counts_out) return AC_ERR_NULL;
+    int st = check_pages(max_pages_per_seq, rows, page_size, num_pages);
+    if (st != AC_OK) return st;
+    if ((block_table == block_table_out) != (ref_counts == ref_counts_out)) return AC_ERR_UNSUPPORTED;
+    st = check_pools(pools, n_pools, 0);
+    if (st != AC_OK) return st;
+    if (!workspace || workspace_bytes < ac_cache_workspace_bytes(rows, num_pages, 0)) return AC_ERR_WORKSPACE;
+    if (!aligned16(ref_counts) || !aligned16(workspace)) return AC_ERR_ALIGN;
+    int dev;
+    st = current_ready_device(&dev);
+    if (st != AC_OK) return st;
+    cudaError_t e = launch_compact(pools, n_pools, block_table, block_table_out, max_pages_per_seq, context_lens,
+                                   ref_counts, ref_counts_out, rows, page_size, num_pages, live_out, workspace,
+                                   status_flag, g_devices[dev].sm_count, static_cast<cudaStream_t>(stream));
     return e == cudaSuccess ? AC_OK : fail_cuda(static_cast<int>(e));
 }
 

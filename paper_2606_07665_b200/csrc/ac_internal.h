@@ -61,6 +61,15 @@ struct FusedRopeArgs {
     const RopeVariant* variant;   // optional: prelude variants applied to q and k_new (nullptr: plain rotation)
 };
 
+// The 4-bit cache as the kernels see it (validated by the ABI layer).
+struct Q4View {
+    uint8_t* k_codes;
+    uint8_t* v_codes;
+    uint32_t* params;                                 // one word per group: s in the low half, m in the high half
+    int64_t stride_page, stride_token, stride_head;   // bytes
+    int group;
+};
+
 // Per-kernel launchers; each validates nothing (the ABI layer did) and returns a cudaError_t.
 cudaError_t attn_set_attributes(int smem_optin);
 cudaError_t launch_rope_kv_append(const void* q_in, void* q_out, const void* k_new, const void* v_new,
@@ -78,8 +87,8 @@ cudaError_t launch_paged_decode_attn(const CUtensorMap& k_map, const CUtensorMap
                                      int num_splits, int split_tokens, float* partial_o,
                                      float* partial_lse, int32_t* arrivals, void* out, int B, int Hq,
                                      int Hkv, int d, int page_size, int32_t* status_flag,
-                                     const FusedRopeArgs* rope, int window, const int32_t* row_order,
-                                     cudaStream_t stream);
+                                     const FusedRopeArgs* rope, int window, int sinks,
+                                     const int32_t* row_order, cudaStream_t stream);
 cudaError_t qkv_set_attributes(int smem_optin);
 int qkv_batch_tile(int B);
 cudaError_t launch_qkv_rope_kv_append(const CUtensorMap& w_map, const CUtensorMap& x_map, void* q_out,
@@ -109,6 +118,37 @@ cudaError_t launch_qkv_rope_kv_append_tc(const CUtensorMap& w_map, const CUtenso
 cudaError_t launch_oproj_residual_tc(const CUtensorMap& w_map, const CUtensorMap& x_map,
                                      const void* residual_in, void* residual_out, int B, int K, int N,
                                      cudaStream_t stream);
+cudaError_t launch_rope_kv_append_q4(const void* q_in, void* q_out, const void* k_new, const void* v_new,
+                                     const Q4View& cache, const int32_t* block_table, int max_pages_per_seq,
+                                     const int32_t* context_lens, const float* rope_cos, const float* rope_sin,
+                                     int max_position, int B, int Hq, int Hkv, int d, int page_size, int num_pages,
+                                     int32_t* status_flag, const RopeVariant* variant, cudaStream_t stream);
+cudaError_t launch_kv_bulk_q4(void* k, void* v, const Q4View& cache, const int32_t* block_table,
+                              int max_pages_per_seq, const int32_t* start_pos, const int32_t* row_offsets,
+                              int total_tokens, int B, int Hkv, int d, int page_size, int num_pages,
+                              int32_t* status_flag, bool store, cudaStream_t stream);
+cudaError_t q4_attn_set_attributes(int smem_optin);
+cudaError_t launch_paged_decode_attn_q4(const void* q_rot, const Q4View& cache, const int32_t* block_table,
+                                        int max_pages_per_seq, const int32_t* context_lens, int new_tokens,
+                                        float scale, int num_splits, int split_tokens, float* partial_o,
+                                        float* partial_lse, int32_t* arrivals, void* out, int B, int Hq, int Hkv,
+                                        int d, int page_size, int num_pages, int window, int sinks,
+                                        const int32_t* row_order, cudaStream_t stream);
+cudaError_t launch_copy_pages(const ac_page_pool* pools, int n_pools, const int32_t* pairs, int n, int num_pages,
+                              int32_t* status_flag, int sms, cudaStream_t stream);
+cudaError_t launch_reserve(int32_t* block_table, int max_pages_per_seq, const int32_t* context_lens, int32_t* refs,
+                           int new_tokens, int rows, int page_size, int num_pages, void* workspace,
+                           int32_t* status_flag, cudaStream_t stream);
+cudaError_t launch_fork(const ac_page_pool* pools, int n_pools, int32_t* block_table, int max_pages_per_seq,
+                        int32_t* context_lens, int32_t* refs, const int32_t* pairs, int n, int rows, int page_size,
+                        int num_pages, void* workspace, int32_t* status_flag, int sms, cudaStream_t stream);
+cudaError_t launch_release(const int32_t* block_table, int max_pages_per_seq, int32_t* context_lens, int32_t* refs,
+                           const int32_t* row_list, int n, int rows, int page_size, int num_pages,
+                           int32_t* status_flag, cudaStream_t stream);
+cudaError_t launch_compact(const ac_page_pool* pools, int n_pools, const int32_t* block_table, int32_t* table_out,
+                           int max_pages_per_seq, const int32_t* context_lens, const int32_t* refs, int32_t* refs_out,
+                           int rows, int page_size, int num_pages, int32_t* live_out, void* workspace,
+                           int32_t* status_flag, int sms, cudaStream_t stream);
 cudaError_t launch_stage_inputs(const void* const src[5], void* const dst[5], const size_t bytes[5],
                                 void* zero_dst, size_t zero_bytes, cudaStream_t stream);
 cudaError_t launch_splitkv_merge(const float* partial_o, const float* partial_lse, int num_splits,

@@ -1,0 +1,504 @@
+// Page bookkeeping and page copies: reserve, fork, release, compact, copy.
+//
+// The bookkeeping kernels hand out free pages lowest index first.  A single CTA walks the reference counts in
+// order, 16 pages per thread and step, and turns the free (or live) ones into ranks by a scan over the CTA; it
+// stops as soon as it has what the call needs.  Bound: latency (a few dependent passes over num_pages * 4 bytes
+// that sit in L2).  The copies are bound by HBM: a warp moves pieces of up to 4 KB, 16 bytes a lane, eight loads in
+// flight before the first store.
+#include "ac_device.cuh"
+#include "ac_internal.h"
+
+namespace ac {
+namespace {
+
+constexpr int kPlanThreads = 1024;
+constexpr int kPagesPerThread = 16;
+constexpr int kStep = kPlanThreads * kPagesPerThread;
+constexpr int kCopyThreads = 256;
+constexpr int kPiece = 4096;                  // bytes a warp moves at a time
+
+// Exclusive prefix sum over the CTA; *total is the sum.  Every thread calls it.
+template <class T>
+__device__ __forceinline__ T block_scan(T v, T* total) {
+    __shared__ T s_warp[kPlanThreads / 32];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    T x = v;
+#pragma unroll
+    for (int off = 1; off < 32; off <<= 1) {
+        const T y = __shfl_up_sync(0xffffffffu, x, off);
+        if (lane >= off) x += y;
+    }
+    if (lane == 31) s_warp[warp] = x;
+    __syncthreads();
+    T w = s_warp[lane];                        // kPlanThreads / 32 == 32 warps
+#pragma unroll
+    for (int off = 1; off < 32; off <<= 1) {
+        const T y = __shfl_up_sync(0xffffffffu, w, off);
+        if (lane >= off) w += y;
+    }
+    *total = __shfl_sync(0xffffffffu, w, 31);
+    const T before = warp > 0 ? __shfl_sync(0xffffffffu, w, warp - 1) : 0;
+    __syncthreads();                           // s_warp may be written again
+    return before + x - v;
+}
+
+// Bit i of the result: page base + i exists and is free.
+__device__ __forceinline__ uint32_t free_bits(const int32_t* refs, int base, int num_pages) {
+    uint32_t bits = 0;
+    if (base + kPagesPerThread <= num_pages) {
+        const int4* src = reinterpret_cast<const int4*>(refs + base);
+        int4 v[kPagesPerThread / 4];
+#pragma unroll
+        for (int i = 0; i < kPagesPerThread / 4; ++i) v[i] = src[i];
+#pragma unroll
+        for (int i = 0; i < kPagesPerThread / 4; ++i)
+            bits |= ((v[i].x == 0 ? 1u : 0u) | (v[i].y == 0 ? 2u : 0u) | (v[i].z == 0 ? 4u : 0u) |
+                     (v[i].w == 0 ? 8u : 0u)) << (4 * i);
+    } else {
+        for (int i = 0; i < kPagesPerThread; ++i)
+            if (base + i < num_pages && refs[base + i] == 0) bits |= 1u << i;
+    }
+    return bits;
+}
+
+// Writes the `need` lowest free pages to list, in order; returns how many there are (at most need).
+__device__ int find_free(const int32_t* refs, int num_pages, int need, int32_t* list) {
+    int found = 0;
+    for (int at = 0; at < num_pages && found < need; at += kStep) {
+        const int base = at + threadIdx.x * kPagesPerThread;
+        uint32_t bits = base < num_pages ? free_bits(refs, base, num_pages) : 0u;
+        int total;
+        int rank = found + block_scan(__popc(bits), &total);
+        while (bits != 0 && rank < need) {
+            list[rank++] = base + __ffs(bits) - 1;
+            bits &= bits - 1;
+        }
+        found += total;
+    }
+    __syncthreads();                           // the list is visible to the whole CTA
+    return found < need ? found : need;
+}
+
+__device__ __forceinline__ void raise(int32_t* status_flag, int bit) {
+    if (status_flag != nullptr) atomicOr(status_flag, bit);
+}
+
+// Pages that n tokens take.
+__device__ __forceinline__ int pages_for(long long n, int page_size) {
+    return static_cast<int>((n + page_size - 1) / page_size);
+}
+
+// ---- reserve ---------------------------------------------------------------------------------------------
+
+__global__ void __launch_bounds__(kPlanThreads) reserve_kernel(int32_t* block_table, int max_pages_per_seq,
+                                                               const int32_t* context_lens, int32_t* refs,
+                                                               int new_tokens, int rows, int page_size, int num_pages,
+                                                               int32_t* offsets, int32_t* list, int32_t* status_flag) {
+    auto pages_of = [&](int r, int& first) {   // pages row r needs, and its first new table index
+        const int n = context_lens[r];
+        first = 0;
+        if (n < 0) return 0;
+        first = pages_for(n, page_size);
+        const int last = pages_for(static_cast<long long>(n) + new_tokens, page_size);
+        return last > max_pages_per_seq ? -1 : last - first;
+    };
+    long long need = 0;
+    for (int at = 0; at < rows; at += kPlanThreads) {
+        const int r = at + threadIdx.x;
+        int first;
+        long long mine = r < rows ? pages_of(r, first) : 0, total;
+        if (mine < 0) {
+            raise(status_flag, AC_FLAG_POSITION_OOB);
+            mine = 0;
+        }
+        const long long o = need + block_scan(mine, &total);
+        if (r < rows) {
+            offsets[r] = o > num_pages ? num_pages + 1 : static_cast<int>(o);
+        }
+        need += total;
+    }
+    const int want = need > num_pages ? num_pages : static_cast<int>(need);
+    const int found = find_free(refs, num_pages, want, list);
+    if (need > found && threadIdx.x == 0) raise(status_flag, AC_FLAG_POOL_EXHAUSTED);
+    const int lane = threadIdx.x & 31;
+    for (int r = threadIdx.x >> 5; r < rows; r += kPlanThreads / 32) {
+        int first;
+        const int mine = pages_of(r, first);
+        const long long off = offsets[r];
+        if (mine <= 0 || off + mine > found) continue;
+        for (int i = lane; i < mine; i += 32) {
+            const int page = list[off + i];
+            block_table[static_cast<size_t>(r) * max_pages_per_seq + first + i] = page;
+            refs[page] = 1;
+        }
+    }
+}
+
+// ---- page copies -----------------------------------------------------------------------------------------
+
+struct PoolArgs {
+    ac_page_pool pool[AC_MAX_PAGE_POOLS];
+};
+
+// A warp copies bytes [lo, hi) of a piece (hi - lo <= kPiece, lo a multiple of 16, addresses 16-byte aligned).
+__device__ __forceinline__ void copy_piece(char* dst, const char* src, int64_t lo, int64_t hi, int lane) {
+    constexpr int N = kPiece / 512;
+    const int bytes = static_cast<int>(hi - lo);
+    const uint4* s = reinterpret_cast<const uint4*>(src + lo);
+    uint4* d = reinterpret_cast<uint4*>(dst + lo);
+    const int whole = bytes / 16;
+    uint4 v[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+        if (i * 32 + lane < whole) v[i] = __ldcs(s + i * 32 + lane);
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+        if (i * 32 + lane < whole) __stcs(d + i * 32 + lane, v[i]);
+    const int tail = whole * 16 + lane;
+    if (tail < bytes) dst[lo + tail] = src[lo + tail];
+}
+
+// Jobs (source, destination) with, where used != nullptr, the number of slots that count.  blockIdx.y is the pool;
+// the warps of its CTAs take (job, segment, piece) units in turn.
+__device__ __forceinline__ void run_copies(const ac_page_pool& pool, const int2* jobs, const int32_t* used, int n,
+                                           int page_size, int num_pages, int32_t* status_flag) {
+    const int lane = threadIdx.x & 31;
+    const int segments = used != nullptr ? pool.segments : 1;
+    const int64_t seg_bytes = pool.page_bytes / segments;
+    const int pieces = static_cast<int>((seg_bytes + kPiece - 1) / kPiece);
+    const long long per_job = static_cast<long long>(segments) * pieces;
+    const long long units = per_job * n;
+    const long long step = static_cast<long long>(gridDim.x) * (kCopyThreads / 32);
+    for (long long u = static_cast<long long>(blockIdx.x) * (kCopyThreads / 32) + (threadIdx.x >> 5); u < units;
+         u += step) {
+        const int job = static_cast<int>(u / per_job);
+        const int rest = static_cast<int>(u - job * per_job);
+        const int seg = rest / pieces, piece = rest - seg * pieces;
+        const int2 j = jobs[job];
+        if (j.x < 0 || j.y < 0 || j.x >= num_pages || j.y >= num_pages) {
+            if (used == nullptr && lane == 0) raise(status_flag, AC_FLAG_PAGE_OOB);
+            continue;
+        }
+        if (j.x == j.y) continue;
+        const int64_t end = used != nullptr ? seg_bytes / page_size * used[job] : seg_bytes;
+        const int64_t lo = static_cast<int64_t>(piece) * kPiece;
+        const int64_t hi = min(end, lo + kPiece);
+        if (lo >= hi) continue;
+        char* base = static_cast<char*>(pool.base) + seg * seg_bytes;
+        copy_piece(base + j.y * pool.page_bytes, base + j.x * pool.page_bytes, lo, hi, lane);
+    }
+}
+
+__global__ void __launch_bounds__(kCopyThreads) copy_pages_kernel(const __grid_constant__ PoolArgs pools,
+                                                                  const int2* pairs, int n, int num_pages,
+                                                                  int32_t* status_flag) {
+    run_copies(pools.pool[blockIdx.y], pairs, nullptr, n, 1, num_pages, status_flag);
+}
+
+// ---- fork ------------------------------------------------------------------------------------------------
+
+// Gives every fork that needs a page its page; jobs[i] = (parent's last page, child's page) or (-1, page or -1)
+// where nothing is copied, used[i] = filled slots, and -1 there for a fork that does not take place.
+__global__ void __launch_bounds__(kPlanThreads) fork_plan_kernel(const int32_t* block_table, int max_pages_per_seq,
+                                                                 const int32_t* context_lens, const int32_t* refs,
+                                                                 const int2* pairs, int n, int rows, int page_size,
+                                                                 int num_pages, int2* jobs, int32_t* used,
+                                                                 int32_t* list, int32_t* status_flag) {
+    int need = 0;
+    for (int at = 0; at < n; at += kPlanThreads) {
+        const int i = at + threadIdx.x;
+        int part = 0, src = -1, state = -1;
+        if (i < n) {
+            const int2 pc = pairs[i];
+            if (pc.x < 0 || pc.x >= rows || pc.y < 0 || pc.y >= rows) {
+                raise(status_flag, AC_FLAG_ROW_OOB);
+            } else {
+                const int len = context_lens[pc.x];
+                if (len >= 0 && pages_for(len, page_size) > max_pages_per_seq) {
+                    raise(status_flag, AC_FLAG_POSITION_OOB);
+                } else if (len >= 0) {
+                    part = len % page_size;
+                    state = part;
+                    if (part > 0) src = block_table[static_cast<size_t>(pc.x) * max_pages_per_seq + len / page_size];
+                }
+            }
+        }
+        int total;
+        const int rank = need + block_scan(part > 0 ? 1 : 0, &total);
+        if (i < n) {
+            used[i] = state;
+            jobs[i] = make_int2(src, part > 0 ? rank : -1);      // the rank, until the pages are known
+        }
+        need += total;
+    }
+    const int found = find_free(refs, num_pages, min(need, num_pages), list);
+    if (need > found && threadIdx.x == 0) raise(status_flag, AC_FLAG_POOL_EXHAUSTED);
+    for (int i = threadIdx.x; i < n; i += kPlanThreads) {
+        const int2 j = jobs[i];
+        if (used[i] <= 0) continue;
+        if (j.y >= found) {
+            used[i] = -1;
+            jobs[i] = make_int2(-1, -1);
+        } else {
+            jobs[i].y = list[j.y];
+        }
+    }
+}
+
+// grid.y = 0: the tables, one CTA per fork in turn; grid.y >= 1: the copies in pool grid.y - 1.
+__global__ void __launch_bounds__(kCopyThreads) fork_apply_kernel(const __grid_constant__ PoolArgs pools,
+                                                                  int32_t* block_table, int max_pages_per_seq,
+                                                                  int32_t* context_lens, int32_t* refs,
+                                                                  const int2* pairs, const int2* jobs,
+                                                                  const int32_t* used, int n, int rows, int page_size,
+                                                                  int num_pages, int32_t* status_flag) {
+    if (blockIdx.y > 0) {
+        run_copies(pools.pool[blockIdx.y - 1], jobs, used, n, page_size, num_pages, nullptr);
+        return;
+    }
+    for (int i = blockIdx.x; i < n; i += gridDim.x) {
+        const int2 pc = pairs[i];
+        if (pc.x < 0 || pc.x >= rows || pc.y < 0 || pc.y >= rows) continue;
+        const int part = used[i];
+        if (part < 0) {
+            if (threadIdx.x == 0) context_lens[pc.y] = -1;
+            continue;
+        }
+        const int len = context_lens[pc.x];
+        const int full = len / page_size;
+        const int32_t* from = block_table + static_cast<size_t>(pc.x) * max_pages_per_seq;
+        int32_t* to = block_table + static_cast<size_t>(pc.y) * max_pages_per_seq;
+        for (int k = threadIdx.x; k < full; k += kCopyThreads) {
+            const int page = from[k];
+            to[k] = page;
+            if (page < 0 || page >= num_pages) raise(status_flag, AC_FLAG_PAGE_OOB);
+            else atomicAdd(refs + page, 1);
+        }
+        if (threadIdx.x == 0) {
+            if (part > 0) {
+                const int2 j = jobs[i];
+                to[full] = j.y;
+                refs[j.y] = 1;
+                if (j.x < 0 || j.x >= num_pages) raise(status_flag, AC_FLAG_PAGE_OOB);
+            }
+            context_lens[pc.y] = len;
+        }
+    }
+}
+
+// ---- release ---------------------------------------------------------------------------------------------
+
+__global__ void __launch_bounds__(kCopyThreads) release_kernel(const int32_t* block_table, int max_pages_per_seq,
+                                                               int32_t* context_lens, int32_t* refs,
+                                                               const int32_t* row_list, int rows, int page_size,
+                                                               int num_pages, int32_t* status_flag) {
+    __shared__ int s_len;
+    const int row = row_list[blockIdx.x];
+    if (row < 0 || row >= rows) {
+        if (threadIdx.x == 0) raise(status_flag, AC_FLAG_ROW_OOB);
+        return;
+    }
+    if (threadIdx.x == 0) s_len = atomicExch(context_lens + row, -1);    // a row listed twice is dropped once
+    __syncthreads();
+    const int len = s_len;
+    if (len <= 0) return;
+    int pages = pages_for(len, page_size);
+    if (pages > max_pages_per_seq) {
+        if (threadIdx.x == 0) raise(status_flag, AC_FLAG_POSITION_OOB);
+        pages = max_pages_per_seq;
+    }
+    for (int k = threadIdx.x; k < pages; k += kCopyThreads) {
+        const int page = block_table[static_cast<size_t>(row) * max_pages_per_seq + k];
+        if (page < 0 || page >= num_pages) {
+            raise(status_flag, AC_FLAG_PAGE_OOB);
+        } else if (atomicSub(refs + page, 1) <= 0) {
+            atomicAdd(refs + page, 1);
+            raise(status_flag, AC_FLAG_REF_COUNT);
+        }
+    }
+}
+
+// ---- compact ---------------------------------------------------------------------------------------------
+
+// head[0] = moves, head[1] = live pages; moves[k] = (from, to); place[p] for p >= live: the page's new id, or -1.
+__global__ void __launch_bounds__(kPlanThreads) compact_plan_kernel(const int32_t* refs, int num_pages, int32_t* head,
+                                                                    int2* moves, int32_t* place, int32_t* live_out) {
+    int live = 0;
+    for (int at = 0; at < num_pages; at += kStep) {
+        const int base = at + threadIdx.x * kPagesPerThread;
+        int mine = 0, total;
+        if (base < num_pages)
+            mine = min(kPagesPerThread, num_pages - base) - __popc(free_bits(refs, base, num_pages));
+        block_scan(mine, &total);
+        live += total;
+    }
+    // holes below `live` and live pages from there on, each in order: equally many
+    int holes = 0, movers = 0;
+    for (int at = 0; at < num_pages; at += kStep) {
+        const int base = at + threadIdx.x * kPagesPerThread;
+        uint32_t hole = 0, mover = 0;
+        if (base < num_pages) {
+            const uint32_t exist = num_pages - base >= kPagesPerThread ? 0xffffu : (1u << (num_pages - base)) - 1u;
+            const uint32_t below = base >= live ? 0u : live - base >= kPagesPerThread ? 0xffffu : (1u << (live - base)) - 1u;
+            const uint32_t open = free_bits(refs, base, num_pages);
+            hole = open & below;
+            mover = ~open & exist & ~below;
+            for (int i = 0; i < kPagesPerThread; ++i)
+                if (((exist & ~below) >> i) & 1u) place[base + i] = -1;
+        }
+        int hole_total, mover_total;
+        int hr = holes + block_scan(__popc(hole), &hole_total);
+        int mr = movers + block_scan(__popc(mover), &mover_total);
+        while (hole != 0) {
+            moves[hr++].y = base + __ffs(hole) - 1;
+            hole &= hole - 1;
+        }
+        while (mover != 0) {
+            moves[mr++].x = base + __ffs(mover) - 1;
+            mover &= mover - 1;
+        }
+        holes += hole_total;
+        movers += mover_total;
+    }
+    __syncthreads();
+    for (int k = threadIdx.x; k < movers; k += kPlanThreads) {
+        const int2 m = moves[k];
+        place[m.x] = m.y;
+    }
+    if (threadIdx.x == 0) {
+        head[0] = movers;
+        head[1] = live;
+        if (live_out != nullptr) *live_out = live;
+    }
+}
+
+// grid.y = 0: block table and reference counts; grid.y >= 1: the moves in pool grid.y - 1.
+__global__ void __launch_bounds__(kCopyThreads) compact_apply_kernel(const __grid_constant__ PoolArgs pools,
+                                                                     const int32_t* block_table, int32_t* table_out,
+                                                                     int max_pages_per_seq, const int32_t* context_lens,
+                                                                     const int32_t* refs, int32_t* refs_out, int rows,
+                                                                     int page_size, int num_pages, const int32_t* head,
+                                                                     const int2* moves, const int32_t* place,
+                                                                     int32_t* status_flag) {
+    const int n = head[0], live = head[1];
+    if (blockIdx.y > 0) {
+        run_copies(pools.pool[blockIdx.y - 1], moves, nullptr, n, 1, num_pages, nullptr);
+        return;
+    }
+    const int first = blockIdx.x * kCopyThreads + threadIdx.x, step = gridDim.x * kCopyThreads;
+    // Counts: each move carries its own two entries; the rest is copied where the output is another buffer.
+    for (int k = first; k < n; k += step) {
+        const int2 m = moves[k];
+        refs_out[m.y] = refs[m.x];
+        refs_out[m.x] = 0;
+    }
+    if (refs_out != refs)
+        for (int q = first; q < num_pages; q += step)
+            if ((refs[q] != 0) == (q < live)) refs_out[q] = refs[q];
+    for (int r = blockIdx.x; r < rows; r += gridDim.x) {
+        const int len = context_lens[r];
+        const int held = len < 0 ? 0 : min(pages_for(len, page_size), max_pages_per_seq);
+        const size_t row = static_cast<size_t>(r) * max_pages_per_seq;
+        for (int k = threadIdx.x; k < max_pages_per_seq; k += kCopyThreads) {
+            int page = block_table[row + k];
+            if (k < held) {
+                if (page < 0 || page >= num_pages) {
+                    raise(status_flag, AC_FLAG_PAGE_OOB);
+                } else if (page >= live) {
+                    const int to = place[page];
+                    if (to >= 0) page = to; else raise(status_flag, AC_FLAG_REF_COUNT);
+                }
+            }
+            table_out[row + k] = page;
+        }
+    }
+}
+
+PoolArgs pool_args(const ac_page_pool* pools, int n_pools) {
+    PoolArgs a;
+    for (int i = 0; i < AC_MAX_PAGE_POOLS; ++i) a.pool[i] = i < n_pools ? pools[i] : ac_page_pool{nullptr, 0, 1, 0};
+    return a;
+}
+
+// CTAs per pool: enough warps for every piece of `jobs` pages (jobs < 0: not known), at most four waves of 8 CTAs
+// per SM over all pools.
+unsigned copy_grid(const ac_page_pool* pools, int n_pools, long long jobs, int sms) {
+    long long most = 1;
+    for (int i = 0; i < n_pools; ++i) {
+        const long long seg = pools[i].page_bytes / pools[i].segments;
+        const long long units = jobs * pools[i].segments * ((seg + kPiece - 1) / kPiece);
+        const long long ctas = (units + kCopyThreads / 32 - 1) / (kCopyThreads / 32);
+        most = ctas > most ? ctas : most;
+    }
+    const long long cap = (8ll * sms + n_pools - 1) / (n_pools > 0 ? n_pools : 1);
+    return static_cast<unsigned>(most < cap ? most : cap);
+}
+
+}  // namespace
+
+cudaError_t launch_copy_pages(const ac_page_pool* pools, int n_pools, const int32_t* pairs, int n, int num_pages,
+                              int32_t* status_flag, int sms, cudaStream_t stream) {
+    const dim3 grid(copy_grid(pools, n_pools, n, sms), n_pools);
+    copy_pages_kernel<<<grid, kCopyThreads, 0, stream>>>(pool_args(pools, n_pools), reinterpret_cast<const int2*>(pairs),
+                                                         n, num_pages, status_flag);
+    return cudaGetLastError();
+}
+
+cudaError_t launch_reserve(int32_t* block_table, int max_pages_per_seq, const int32_t* context_lens, int32_t* refs,
+                           int new_tokens, int rows, int page_size, int num_pages, void* workspace,
+                           int32_t* status_flag, cudaStream_t stream) {
+    int32_t* offsets = static_cast<int32_t*>(workspace);
+    reserve_kernel<<<1, kPlanThreads, 0, stream>>>(block_table, max_pages_per_seq, context_lens, refs, new_tokens, rows,
+                                                   page_size, num_pages, offsets, offsets + rows, status_flag);
+    return cudaGetLastError();
+}
+
+cudaError_t launch_fork(const ac_page_pool* pools, int n_pools, int32_t* block_table, int max_pages_per_seq,
+                        int32_t* context_lens, int32_t* refs, const int32_t* pairs, int n, int rows, int page_size,
+                        int num_pages, void* workspace, int32_t* status_flag, int sms, cudaStream_t stream) {
+    int2* jobs = static_cast<int2*>(workspace);
+    int32_t* used = reinterpret_cast<int32_t*>(jobs + n);
+    int32_t* list = used + n;
+    const int2* pc = reinterpret_cast<const int2*>(pairs);
+    fork_plan_kernel<<<1, kPlanThreads, 0, stream>>>(block_table, max_pages_per_seq, context_lens, refs, pc, n, rows,
+                                                     page_size, num_pages, jobs, used, list, status_flag);
+    cudaError_t e = cudaGetLastError();
+    if (e != cudaSuccess) return e;
+    unsigned x = copy_grid(pools, n_pools, n, sms);
+    const unsigned forks = n < 8 * sms ? n : 8 * sms;
+    if (x < forks) x = forks;
+    fork_apply_kernel<<<dim3(x, n_pools + 1), kCopyThreads, 0, stream>>>(
+        pool_args(pools, n_pools), block_table, max_pages_per_seq, context_lens, refs, pc, jobs, used, n, rows, page_size,
+        num_pages, status_flag);
+    return cudaGetLastError();
+}
+
+cudaError_t launch_release(const int32_t* block_table, int max_pages_per_seq, int32_t* context_lens, int32_t* refs,
+                           const int32_t* row_list, int n, int rows, int page_size, int num_pages,
+                           int32_t* status_flag, cudaStream_t stream) {
+    release_kernel<<<n, kCopyThreads, 0, stream>>>(block_table, max_pages_per_seq, context_lens, refs, row_list, rows,
+                                                   page_size, num_pages, status_flag);
+    return cudaGetLastError();
+}
+
+cudaError_t launch_compact(const ac_page_pool* pools, int n_pools, const int32_t* block_table, int32_t* table_out,
+                           int max_pages_per_seq, const int32_t* context_lens, const int32_t* refs, int32_t* refs_out,
+                           int rows, int page_size, int num_pages, int32_t* live_out, void* workspace,
+                           int32_t* status_flag, int sms, cudaStream_t stream) {
+    int32_t* head = static_cast<int32_t*>(workspace);
+    int2* moves = reinterpret_cast<int2*>(head + 4);
+    int32_t* place = reinterpret_cast<int32_t*>(moves + num_pages / 2 + 1);
+    compact_plan_kernel<<<1, kPlanThreads, 0, stream>>>(refs, num_pages, head, moves, place, live_out);
+    cudaError_t e = cudaGetLastError();
+    if (e != cudaSuccess) return e;
+    // how many pages move is known on the device only: at most half of them
+    unsigned x = copy_grid(pools, n_pools, num_pages / 2 + 1, sms);
+    const unsigned table = static_cast<unsigned>(rows < 2 * sms ? rows : 2 * sms);
+    if (x < table) x = table;
+    compact_apply_kernel<<<dim3(x, n_pools + 1), kCopyThreads, 0, stream>>>(
+        pool_args(pools, n_pools), block_table, table_out, max_pages_per_seq, context_lens, refs, refs_out, rows,
+        page_size, num_pages, head, moves, place, status_flag);
+    return cudaGetLastError();
+}
+
+}  // namespace ac

@@ -40,6 +40,7 @@
 #include "ac_device.cuh"
 #include "ac_internal.h"
 #include "rope_variant.cuh"
+#include "split_merge.cuh"
 
 namespace ac {
 namespace {
@@ -99,7 +100,8 @@ struct AttnParams {
     int fused_merge;              // 1: the last CTA of a (request, KV head) merges the splits itself
     const int32_t* row_order;     // optional [B] permutation: grid row y serves request row_order[y]
     int longest_first;            // 1: grid row y serves the request with the y-th longest context
-    int window;                   // > 0: attend over the last `window` tokens of each row only
+    int window;                   // > 0: attend over the last `window` tokens of each row only ...
+    int sinks;                    // ... and over its first `sinks` tokens
     int cluster_merge;            // 1: the splits of a (request, KV head) are one thread-block cluster and
                                   //    split 0 merges them out of the others' shared memory
     // -- only for the fused step with prelude variants (ROPE = 2)
@@ -113,82 +115,6 @@ struct AttnParams {
 // Rotation flavours of the kernel: none (q arrives rotated), the plain rotate-half of the fused step,
 // and the fused step with the prelude variants (per-head RMSNorm, partial rotary, interleaved pairing).
 constexpr int ROPE_NONE = 0, ROPE_PLAIN = 1, ROPE_VARIANT = 2;
-
-// The merge of the ticket path: the CTA that arrived last combines the splits' partial results of its
-// (request, KV head) out of the workspace.  An item is four consecutive output elements of one query
-// row; a thread owns ITEMS of them (item = thread + k * THREADS) and walks the splits in groups of GS
-// for all its items at once: the ITEMS * GS 16-byte partial loads and their log-sum-exps are issued
-// before any is used, so a group costs one L2 round trip whatever the number of items, and groups are
-// combined with the same running-maximum rescaling as the main loop.  ITEMS * GS <= 16 keeps the
-// loads in registers.
-template <int D, int THREADS, int ITEMS, int GS>
-__device__ __forceinline__ void merge_splits_from_workspace(const AttnParams& p, size_t hq0, int items, int S,
-                                                            int n_active) {
-    constexpr int D4 = D / 4;
-    static_assert(ITEMS * GS <= 16, "loads of a group stay in registers");
-    const float* lse_g[ITEMS];
-    const float4* po[ITEMS];
-    bool live[ITEMS];
-    float M[ITEMS], den[ITEMS];
-    float4 acc[ITEMS];
-    size_t out_at[ITEMS];
-#pragma unroll
-    for (int k = 0; k < ITEMS; ++k) {
-        const int e = threadIdx.x + k * THREADS;
-        live[k] = e < items;
-        const int row = live[k] ? e / D4 : 0;
-        const int c4 = live[k] ? e - row * D4 : 0;
-        lse_g[k] = p.partial_lse + (hq0 + row) * S;
-        po[k] = reinterpret_cast<const float4*>(p.partial_o + (hq0 + row) * S * D) + c4;
-        out_at[k] = (hq0 + row) * D + c4 * 4;
-        M[k] = -INFINITY;
-        den[k] = 0.0f;
-        acc[k] = make_float4(0.f, 0.f, 0.f, 0.f);
-    }
-    for (int s0 = 0; s0 < n_active; s0 += GS) {
-        float4 v[ITEMS][GS];
-        float l[ITEMS][GS];
-#pragma unroll
-        for (int k = 0; k < ITEMS; ++k)
-#pragma unroll
-            for (int u = 0; u < GS; ++u) {
-                const bool on = live[k] && s0 + u < n_active;
-                l[k][u] = on ? __ldcg(lse_g[k] + s0 + u) : -INFINITY;
-                v[k][u] = on ? __ldcg(po[k] + static_cast<size_t>(s0 + u) * D4) : make_float4(0.f, 0.f, 0.f, 0.f);
-            }
-#pragma unroll
-        for (int k = 0; k < ITEMS; ++k) {
-            float gm = M[k];
-#pragma unroll
-            for (int u = 0; u < GS; ++u) gm = fmaxf(gm, l[k][u]);
-            const float rescale = __expf(M[k] - gm);           // 0 on the first group (M = -inf)
-            acc[k].x *= rescale;
-            acc[k].y *= rescale;
-            acc[k].z *= rescale;
-            acc[k].w *= rescale;
-            den[k] *= rescale;
-            M[k] = gm;
-#pragma unroll
-            for (int u = 0; u < GS; ++u) {
-                const float wgt = __expf(l[k][u] - gm);        // 0 for the padding entries
-                acc[k].x = fmaf(wgt, v[k][u].x, acc[k].x);
-                acc[k].y = fmaf(wgt, v[k][u].y, acc[k].y);
-                acc[k].z = fmaf(wgt, v[k][u].z, acc[k].z);
-                acc[k].w = fmaf(wgt, v[k][u].w, acc[k].w);
-                den[k] += wgt;
-            }
-        }
-    }
-#pragma unroll
-    for (int k = 0; k < ITEMS; ++k) {
-        if (!live[k]) continue;
-        const float inv = 1.0f / den[k];
-        const uint2 bits = make_uint2(pack_bf16x2(acc[k].x * inv, acc[k].y * inv),
-                                      pack_bf16x2(acc[k].z * inv, acc[k].w * inv));
-        *reinterpret_cast<uint2*>(p.out + out_at[k]) = bits;
-        if (p.out_mirror != nullptr) *reinterpret_cast<uint2*>(p.out_mirror + out_at[k]) = bits;
-    }
-}
 
 template <int D, bool WIDE, int ROPE, int NW>
 __global__ void __launch_bounds__(NW * 32, NW == kFatWarps ? 1 : 2) paged_decode_attn_kernel(
@@ -248,9 +174,16 @@ __global__ void __launch_bounds__(NW * 32, NW == kFatWarps ? 1 : 2) paged_decode
     // written is independent of that kernel, so with a programmatic dependent launch it overlaps the
     // preceding kernel's execution.  The preceding kernel is either the RoPE + append kernel of this
     // step (writes slot ctx) or the fused step of the previous token (wrote slot ctx - 1).
-    int tok_begin = split * p.split_tokens;          // both move up when a sliding window applies
+    // The splits partition the row's attended tokens laid end to end ("range" positions): without a window
+    // that is the row itself; with one, range position r is token r + window_base; with sinks in front, the
+    // first tiles (j < j_window of a warp's tiles) are the row's own and only those behind them move up.
+    int tok_begin = split * p.split_tokens;          // range position; moves up when a sliding window applies
     int tile_begin = tok_begin / TILE;
-    auto tile_token0 = [&](int j) { return (tile_begin + warp + j * WARPS) * TILE; };
+    int window_base = 0;                             // multiple of TILE
+    int j_window = 0;
+    auto tile_token0 = [&](int j) {
+        return (tile_begin + warp + j * WARPS) * TILE + (j >= j_window ? window_base : 0);
+    };
     const int32_t* bt_row = p.block_table + static_cast<size_t>(b) * p.max_pages_per_seq;
     auto load_page_id = [&](int j) {
         const int idx = tile_token0(j) / p.page_size;
@@ -265,19 +198,30 @@ __global__ void __launch_bounds__(NW * 32, NW == kFatWarps ? 1 : 2) paged_decode
     int n_tokens = ctx < 0 ? 0 : ctx + p.new_tokens;
     const long long table_tokens = static_cast<long long>(p.max_pages_per_seq) * p.page_size;
     if (n_tokens > table_tokens) n_tokens = static_cast<int>(table_tokens);
-    // Sliding window: the row attends over tokens [tok_lo, n_tokens).  The splits partition the range
-    // that starts at tok_lo rounded down to a multiple of 64; tiles wholly below tok_lo are skipped
-    // and the first tile masks its leading tokens.
-    int tok_lo = 0, window_base = 0;
+    // Sliding window: the row attends over tokens [tok_lo, n_tokens).  The range starts at tok_lo rounded
+    // down to a multiple of 64; tiles wholly below tok_lo are skipped and the first tile masks its
+    // leading tokens.  With sinks the row also attends over [0, sinks): the range is the sinks' tiles
+    // followed by the tiles from the one that holds tok_lo, so no tile of it is masked wholly; where the
+    // two pieces meet or overlap nothing moves and the mask alone does the work.
+    int tok_lo = 0;
     if (p.window > 0) {
         tok_lo = max(0, n_tokens - p.window);
-        window_base = tok_lo / 64 * 64;
-        tok_begin = max(window_base + split * p.split_tokens, tok_lo / TILE * TILE);
-        tile_begin = tok_begin / TILE;
+        if (p.sinks == 0) {
+            window_base = tok_lo / 64 * 64;
+            tok_begin = max(split * p.split_tokens, tok_lo / TILE * TILE - window_base);
+            tile_begin = tok_begin / TILE;
+        } else if (p.sinks >= tok_lo) {
+            tok_lo = 0;                                  // sinks and window cover the whole row
+        } else {
+            const int sink_tiles = (p.sinks + TILE - 1) / TILE;
+            window_base = max(0, tok_lo / TILE - sink_tiles) * TILE;
+            j_window = max(0, sink_tiles - tile_begin - warp + WARPS - 1) / WARPS;
+        }
 #pragma unroll
         for (int s = 0; s < STAGES; ++s) page_first[s] = load_page_id(s);     // the range moved
     }
-    const int tok_end = min(window_base + (split + 1) * p.split_tokens, n_tokens);
+    const int range_tokens = n_tokens - window_base;
+    const int tok_end = min((split + 1) * p.split_tokens, range_tokens);
 
     // Programmatic launch completion is signalled only AFTER this CTA has synchronised on the
     // preceding kernel (dependency_sync below).  The next kernel of the stream (launched with the
@@ -339,8 +283,9 @@ __global__ void __launch_bounds__(NW * 32, NW == kFatWarps ? 1 : 2) paged_decode
     const uint64_t policy = l2_policy_evict_first();
     // Tiles from the one holding slot ctx - 1 onwards must not be fetched before the preceding kernel
     // has completed; new_token_tile is where this step's own token lives.
-    const int new_token_tile = p.new_tokens > 0 ? ctx / TILE : -1;
-    const int first_dependent_tile = (ctx > 0 ? ctx - 1 : 0) / TILE;
+    // (Both as tiles of the range; slot ctx - 1 may lie below a window's range, which only waits earlier.)
+    const int new_token_tile = p.new_tokens > 0 ? (ctx - window_base) / TILE : -1;
+    const int first_dependent_tile = ((ctx > 0 ? ctx - 1 : 0) - window_base) / TILE;
 
     auto issue_at = [&](int j, int slot, int page) {      // lane 0 only; slot = first token's slot inside its page
         const int stage = j % STAGES;
@@ -600,8 +545,9 @@ __global__ void __launch_bounds__(NW * 32, NW == kFatWarps ? 1 : 2) paged_decode
         }
         bool wrote_stage = false;                              // ordinary stores went into this stage
         const int tok0 = tile_token0(j);
-        const int n_valid = tok_end - tok0;                    // >= 1; < 16 only on the last tile
-        const int lo_valid = tok_lo - tok0;                    // > 0 only on the first tile of a window
+        const int n_valid = tok_end - (tile_begin + warp + j * WARPS) * TILE;   // >= 1; < 16 only on the last tile
+        const int lo_valid = tok_lo - tok0;                    // > 0 only on a window's first tile and on sinks
+        const int sink_valid = p.sinks - tok0;                 // < 16 on every tile but the sinks' full ones
 
         if (ROPE && j == append_j && append_ok) {
             // The tile just loaded still has the stale slot of the new token: overwrite that row with
@@ -650,22 +596,22 @@ __global__ void __launch_bounds__(NW * 32, NW == kFatWarps ? 1 : 2) paged_decode
             }
         }
 
-        if (n_valid < TILE || lo_valid > 0) {
-            // Slots past the request's length hold arbitrary bits, and tokens before a sliding
-            // window's start are not attended: mask their scores and clear their V rows (0 * NaN
+        if (n_valid < TILE || (lo_valid > 0 && sink_valid < TILE)) {
+            // Slots past the request's length hold arbitrary bits, and tokens between the sinks and a
+            // sliding window's start are not attended: mask their scores and clear their V rows (0 * NaN
             // would poison the product).
 #pragma unroll
             for (int nt = 0; nt < 2; ++nt)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const int col = nt * 8 + 2 * t + (e & 1);
-                    if (col >= n_valid || col < lo_valid) s[nt][e] = -INFINITY;
+                    if (col >= n_valid || (col < lo_valid && col >= sink_valid)) s[nt][e] = -INFINITY;
                 }
             const int chunks_per_row = L::HALVES * 8;
             for (int idx = lane; idx < TILE * chunks_per_row; idx += 32) {
                 const int row = idx / chunks_per_row;
                 const int rem = idx % chunks_per_row;
-                if (row >= n_valid || row < lo_valid) {
+                if (row >= n_valid || (row < lo_valid && row >= sink_valid)) {
                     uint4* dstz = reinterpret_cast<uint4*>(smem_gen + (vbase - smem_base) +
                                                            (rem >> 3) * L::HALF_BYTES + row * 128 + (rem & 7) * 16);
                     *dstz = make_uint4(0u, 0u, 0u, 0u);
@@ -730,6 +676,10 @@ __global__ void __launch_bounds__(NW * 32, NW == kFatWarps ? 1 : 2) paged_decode
             if (next_slot >= p.page_size) {
                 next_slot -= p.page_size;
                 ++next_idx;
+            }
+            if (issued + 1 == j_window) {                      // from the sinks' tiles to the window's
+                next_idx = tile_token0(j_window) / p.page_size;
+                next_slot = tile_token0(j_window) - next_idx * p.page_size;
             }
             page_next = issued + 1 < n_my ? (next_idx < p.max_pages_per_seq ? bt_row[next_idx] : -1) : 0;
             if (lane == 0) issue_at(issued, slot, page);
@@ -832,7 +782,7 @@ __global__ void __launch_bounds__(NW * 32, NW == kFatWarps ? 1 : 2) paged_decode
         // their shared memory.  No global round trip, no ticket; CTAs whose split has no tokens pass
         // through the same two barriers and nothing else.
         // splits with tokens, <= 16 (a row longer than the split grid covers still has S of them)
-        const int n_active = min(S, (n_tokens - window_base + p.split_tokens - 1) / p.split_tokens);
+        const int n_active = min(S, (range_tokens + p.split_tokens - 1) / p.split_tokens);
         cluster_sync_all();                              // every staged result is written and visible
         if (split == 0) {
             constexpr int D4 = D / 4;
@@ -883,7 +833,7 @@ __global__ void __launch_bounds__(NW * 32, NW == kFatWarps ? 1 : 2) paged_decode
     // Nobody waits for anybody: CTAs that are not last simply exit.
     __shared__ int s_is_last;
     // splits with tokens (a row longer than the split grid covers still has S of them)
-    const int n_active = min(S, (n_tokens - window_base + p.split_tokens - 1) / p.split_tokens);
+    const int n_active = min(S, (range_tokens + p.split_tokens - 1) / p.split_tokens);
     // One acquire-release atomic by one thread, bracketed by CTA barriers: the release orders the
     // partials that every thread of this CTA stored before the first barrier ahead of the ticket, the
     // acquire orders the ticket ahead of the partial loads that follow the second barrier.
@@ -1008,11 +958,12 @@ cudaError_t launch_paged_decode_attn(const CUtensorMap& k_map, const CUtensorMap
                                      int num_splits, int split_tokens, float* partial_o,
                                      float* partial_lse, int32_t* arrivals, void* out, int B, int Hq,
                                      int Hkv, int d, int page_size, int32_t* status_flag,
-                                     const FusedRopeArgs* rope, int window, const int32_t* row_order,
-                                     cudaStream_t stream) {
+                                     const FusedRopeArgs* rope, int window, int sinks,
+                                     const int32_t* row_order, cudaStream_t stream) {
     AttnParams p;
     p.row_order = row_order;
     p.window = window > 0 ? window : 0;
+    p.sinks = window > 0 ? sinks : 0;
     p.q_rot_out = nullptr;
     p.k_new = p.v_new = nullptr;
     p.k_cache = p.v_cache = nullptr;
