@@ -8,8 +8,11 @@
 //
 // Codes as matrix operands.  A nibble isolated at the low end of a 16-bit half is the fp16 subnormal c * 2^-24,
 // and at bit 4 it is 16 c * 2^-24: with one AND two of a word's eight codes are a finished operand register,
-// exact and without bias (five instructions for eight codes).  The 2^24 and the 1/16 of the odd codes are powers
-// of two and are taken back in q (odd elements of the fragment are divided by 16) and in the result.
+// exact and without bias.  The 2^24 and the 1/16 of the odd codes are powers of two and are taken back in q (odd
+// elements of the fragment are divided by 16) and in the result.  For V a whole byte (c0 + 16 c1) * 2^-24 and its
+// high nibble 16 c1 * 2^-24 are the operands instead, and the even element of the result is the difference of the two
+// fp32 sums, formed once at the end: a byte is one permutation away, which saves the shift.  ldmatrix brings both in
+// place: plain for K, transposed (as 16-bit halves, four codes of one token) for V.
 //
 // Tiles.  The codes are the 16-row A operand of mma.m16n8k16 and the query heads its 8 columns (two column
 // blocks for groups of 9-16 heads), S^T = K Q^T and O^T = V^T P^T: a KV tile costs half the instructions that it
@@ -68,7 +71,7 @@ struct Q4Smem {
     static constexpr int P_BYTES = TILE * PB;
     static constexpr int STAGE_BYTES = 2 * K_BYTES + P_BYTES;  // K codes, V codes, parameters
     static constexpr int RING_BYTES = STAGES * STAGE_BYTES;
-    static constexpr int TOTAL = NW * RING_BYTES + 128;        // + alignment slack
+    static constexpr int TOTAL = NW * RING_BYTES;
 };
 
 struct Q4AttnParams {
@@ -94,14 +97,10 @@ __global__ void __launch_bounds__(NW * 32, CTAS) paged_decode_attn_q4_kernel(con
     constexpr int WARPS = NW, THREADS = NW * 32;
     constexpr int RB = L::RB, PB = L::PB;
     constexpr int CPR = RB / 16;                   // 16-byte chunks per row
-    constexpr int GE = D / G;                      // elements per group
-    constexpr int KW = GE / 32;                    // K words (8 codes) per lane, row and group
-    constexpr int VE = GE / 8;                     // V elements per lane, token and group: 16, 8 or 4
-    constexpr int MT = GE / 16;                    // 16-row tiles of O^T per group
+    constexpr int NC = D / 32;                     // 16-byte chunks (32 elements) per row
+    constexpr int CPG = NC / G;                    // chunks per group
 
-    extern __shared__ uint8_t smem_raw[];
-    const uint32_t smem_base = (smem_addr(smem_raw) + 127u) & ~127u;
-    uint8_t* smem_gen = smem_raw + (smem_base - smem_addr(smem_raw));
+    extern __shared__ __align__(128) uint8_t smem[];
 
     const int h = blockIdx.x, split = blockIdx.z;
     const int b = p.row_order != nullptr ? p.row_order[blockIdx.y] : static_cast<int>(blockIdx.y);
@@ -143,70 +142,83 @@ __global__ void __launch_bounds__(NW * 32, CTAS) paged_decode_attn_q4_kernel(con
     }
 
     const int32_t* bt_row = p.block_table + static_cast<size_t>(b) * p.max_pages_per_seq;
-    const uint32_t ring = smem_base + warp * L::RING_BYTES;
     const int n_tiles = (tok_end - tok_begin + TILE - 1) / TILE;
     const int n_my = n_tiles > warp ? (n_tiles - warp + WARPS - 1) / WARPS : 0;
     const uint64_t policy = l2_policy_evict_first();
     auto range0 = [&](int j) { return tok_begin + (warp + j * WARPS) * TILE; };
-    auto token_of = [&](int r) { return r + (r >= sink_span ? window_base : 0); };
-    // page-table index and granule inside the page of the granule that starts at token tk
-    auto page_index = [&](int tk, int& sub) {
-        const uint32_t gr = static_cast<uint32_t>(tk) / GRAN;
+    // Range positions that are not attended: between the sinks and the window's first token.
+    const int hole_lo = tok_lo > 0 ? p.sinks : 0, hole_hi = tok_lo > 0 ? tok_lo - window_base : 0;
+
+    // Where the tiles lie.  The warp looks up the pages of 16 tiles at a time, one granule per lane (lane =
+    // tile * 2 + half), and turns them into offsets once; a tile then takes its two by shuffle.  The page ids of the
+    // next 16 tiles are loaded ahead.
+    auto locate = [&](int j0, int& sub) {          // this lane's granule of the tiles from j0: table index or -1
+        const int j = j0 + (lane >> 1);
+        const int r = range0(j) + (lane & 1) * GRAN;
+        const uint32_t gr = static_cast<uint32_t>(r + (r >= sink_span ? window_base : 0)) / GRAN;
         const uint32_t idx = p.gpp == 1 ? gr : __umulhi(gr, p.gpp_magic);
         sub = static_cast<int>(gr - idx * p.gpp);
-        return static_cast<int>(idx);
+        return j < n_my && r < tok_end && idx < static_cast<uint32_t>(p.max_pages_per_seq) ? static_cast<int>(idx) : -1;
     };
-    auto load_page = [&](int j, int half) {        // -1: nothing to read there
-        const int r = range0(j) + half * GRAN;
-        if (j >= n_my || r >= tok_end) return -1;
+    auto load_pages = [&](int j0) {
         int sub;
-        const int idx = page_index(token_of(r), sub);
-        return idx < p.max_pages_per_seq ? bt_row[idx] : -1;
+        const int idx = locate(j0, sub);
+        return idx >= 0 ? bt_row[idx] : -1;
     };
+    int64_t gr_off = 0;                            // byte offset of this lane's granule in the code pools
+    int gr_param = 0;                              // its index among the parameter granules
+    uint32_t gr_ok = 0;                            // bit per lane: the granule has a page (otherwise it reads as zeros)
+    auto settle_pages = [&](int j0, int page) {
+        int sub;
+        locate(j0, sub);
+        const bool on = page >= 0 && page < p.num_pages;
+        gr_ok = __ballot_sync(0xffffffffu, on);
+        gr_off = on ? static_cast<int64_t>(page) * p.cache.stride_page + sub * GRAN * p.cache.stride_token : 0;
+        gr_param = on ? static_cast<int>((static_cast<int64_t>(page) * p.Hkv + h) * p.gpp) + sub : 0;
+    };
+
     // This lane's share of a granule: row lane / CPR (and 8 further at D = 128), chunk lane % CPR.
+    constexpr int RPI = 32 / CPR;                  // rows per pass of the warp: 8 or 16
     const int64_t lane_off = static_cast<int64_t>(lane / CPR) * p.cache.stride_token + (lane % CPR) * 16 +
                              static_cast<int64_t>(h) * p.cache.stride_head;
-    auto issue = [&](int j, int page0, int page1) {
-        const uint32_t dst = ring + (j % STAGES) * L::STAGE_BYTES;
-        constexpr int RPI = 32 / CPR;              // rows per lane pass: 8 or 16
-        const uint8_t* prm[2];
-        int ok[2];
+    const uint8_t* const k_lane = p.cache.k_codes + lane_off;
+    const uint8_t* const v_lane = p.cache.v_codes + lane_off;
+    const int64_t next_rows = static_cast<int64_t>(RPI) * p.cache.stride_token;
+    const uint32_t ring = smem_addr(smem) + warp * L::RING_BYTES;
+    const uint32_t code_dst = ring + q4_tile_offset<RB>(lane / CPR, lane % CPR);
+    constexpr int PC = GRAN * PB / 16;             // parameter chunks per granule: 8, 16 or 32
+    auto issue = [&](int j, uint32_t stage) {      // stage = byte offset of the stage in the ring
+        const int src = 2 * (j & 15);
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
-            const int page = half ? page1 : page0;
-            const bool on = page >= 0 && page < p.num_pages;
-            int sub;
-            page_index(token_of(range0(j) + half * GRAN), sub);
-            ok[half] = on ? 16 : 0;
-            const int64_t pg = on ? page : 0;
-            const int slot = on ? sub * GRAN : 0;
-            const int64_t off = pg * p.cache.stride_page + slot * p.cache.stride_token + lane_off;
+            const int64_t off = __shfl_sync(0xffffffffu, gr_off, src + half);
+            const int bytes = (gr_ok >> (src + half)) & 1u ? 16 : 0;
 #pragma unroll
             for (int i = 0; i < GRAN / RPI; ++i) {
-                const int row = half * GRAN + i * RPI + lane / CPR;
-                const uint32_t at = q4_tile_offset<RB>(row, lane % CPR);
-                const int64_t o = off + static_cast<int64_t>(i * RPI) * p.cache.stride_token;
-                cp_async_16(dst + at, p.cache.k_codes + o, ok[half], policy);
-                cp_async_16(dst + L::K_BYTES + at, p.cache.v_codes + o, ok[half], policy);
+                const uint32_t dst = code_dst + stage + (half * GRAN + i * RPI) * RB;   // whole lines: same swizzle
+                const int64_t o = off + (i ? next_rows : 0);
+                cp_async_16(dst, k_lane + o, bytes, policy);
+                cp_async_16(dst + L::K_BYTES, v_lane + o, bytes, policy);
             }
-            prm[half] = reinterpret_cast<const uint8_t*>(p.cache.params) +
-                        ((pg * p.Hkv + h) * p.page_size + slot) * PB;
         }
-        constexpr int PC = GRAN * PB / 16;         // parameter chunks per granule: 8, 16 or 32
 #pragma unroll
         for (int i = 0; i < (2 * PC + 31) / 32; ++i) {
             const int c = i * 32 + lane;
-            if (2 * PC >= 32 || c < 2 * PC) {
-                const int half = c / PC;
-                cp_async_16(dst + 2 * L::K_BYTES + c * 16, (half ? prm[1] : prm[0]) + (c - half * PC) * 16,
-                            half ? ok[1] : ok[0], policy);
-            }
+            const int half = (c / PC) & 1;
+            const int granule = __shfl_sync(0xffffffffu, gr_param, src + half);
+            if (2 * PC >= 32 || c < 2 * PC)
+                cp_async_16(ring + stage + 2 * L::K_BYTES + c * 16,
+                            reinterpret_cast<const uint8_t*>(p.cache.params) +
+                                static_cast<int64_t>(granule) * (GRAN * PB) + (c - half * PC) * 16,
+                            (gr_ok >> (src + half)) & 1u ? 16 : 0, policy);
         }
     };
 
     // ---- prologue: fill the ring; tiles that hold slot ctx - 1 or later wait for the preceding kernel ---------
     const int dependent_from = (ctx > 0 ? ctx - 1 : 0) - window_base;     // range position, maybe negative
     bool dependency_met = false;
+    settle_pages(0, load_pages(0));
+    int pages_ahead = load_pages(16);
 #pragma unroll
     for (int s = 0; s < STAGES; ++s) {
         if (s < n_my) {
@@ -214,36 +226,33 @@ __global__ void __launch_bounds__(NW * 32, CTAS) paged_decode_attn_q4_kernel(con
                 dependency_sync();
                 dependency_met = true;
             }
-            issue(s, load_page(s, 0), load_page(s, 1));
+            issue(s, s * L::STAGE_BYTES);
         }
         cp_async_commit();
     }
-    int next0 = load_page(STAGES, 0), next1 = load_page(STAGES, 1);
     if (!dependency_met) dependency_sync();                                // q was written by the preceding kernel
 
     // ---- query fragments (B operand): lane (g, t) holds head g (+ 8), elements in the order of K's codes --------
-    uint32_t qb[NT][G][KW][4];
+    uint32_t qb[NT][NC][4];
     float qs[NT][G][2], cs[NT][2];                 // sums of q over a group and score factor, heads 2t and 2t + 1
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
         const int head = g + 8 * nt;
         const bool live = head < HG;
         const uint16_t* src = p.q + (static_cast<size_t>(b) * p.Hq + h * HG + (live ? head : 0)) * D;
-        float x[G][KW][8];
+        float x[NC][8];
         float mx = 0.0f;
 #pragma unroll
-        for (int gq = 0; gq < G; ++gq)
+        for (int c = 0; c < NC; ++c) {
+            const uint4 raw = *reinterpret_cast<const uint4*>(src + c * 32 + t * 8);
+            const uint32_t u[4] = {raw.x, raw.y, raw.z, raw.w};
 #pragma unroll
-            for (int w = 0; w < KW; ++w) {
-                const uint4 raw = *reinterpret_cast<const uint4*>(src + gq * GE + t * (GE / 4) + w * 8);
-                const uint32_t u[4] = {raw.x, raw.y, raw.z, raw.w};
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const float f = __uint_as_float((e & 1) ? (u[e >> 1] & 0xFFFF0000u) : (u[e >> 1] << 16));
-                    x[gq][w][e] = live ? f : 0.0f;
-                    mx = fmaxf(mx, fabsf(x[gq][w][e]));
-                }
+            for (int e = 0; e < 8; ++e) {
+                const float f = __uint_as_float((e & 1) ? (u[e >> 1] & 0xFFFF0000u) : (u[e >> 1] << 16));
+                x[c][e] = live ? f : 0.0f;
+                mx = fmaxf(mx, fabsf(x[c][e]));
             }
+        }
         mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
         mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
         // power of two that brings the row's largest element into [2^13, 2^14) (fp16 keeps 11 bits down to 2^-14)
@@ -256,17 +265,18 @@ __global__ void __launch_bounds__(NW * 32, CTAS) paged_decode_attn_q4_kernel(con
         for (int gq = 0; gq < G; ++gq) {
             sum[gq] = 0.0f;
 #pragma unroll
-            for (int w = 0; w < KW; ++w) {
+            for (int w = 0; w < CPG; ++w) {
+                const int c = gq * CPG + w;
                 float y[8];
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    y[e] = x[gq][w][e] * up;
+                    y[e] = x[c][e] * up;
                     sum[gq] += y[e];
                 }
-                qb[nt][gq][w][0] = pack_f16x2(y[0], y[4]);
-                qb[nt][gq][w][1] = pack_f16x2(y[1] * 0.0625f, y[5] * 0.0625f);
-                qb[nt][gq][w][2] = pack_f16x2(y[2], y[6]);
-                qb[nt][gq][w][3] = pack_f16x2(y[3] * 0.0625f, y[7] * 0.0625f);
+                qb[nt][c][0] = pack_f16x2(y[0], y[4]);
+                qb[nt][c][1] = pack_f16x2(y[1] * 0.0625f, y[5] * 0.0625f);
+                qb[nt][c][2] = pack_f16x2(y[2], y[6]);
+                qb[nt][c][3] = pack_f16x2(y[3] * 0.0625f, y[7] * 0.0625f);
             }
             sum[gq] += __shfl_xor_sync(0xffffffffu, sum[gq], 1);
             sum[gq] += __shfl_xor_sync(0xffffffffu, sum[gq], 2);
@@ -278,7 +288,8 @@ __global__ void __launch_bounds__(NW * 32, CTAS) paged_decode_attn_q4_kernel(con
         cs[nt][1] = __shfl_sync(0xffffffffu, factor, 8 * t + 4);
     }
 
-    float o[G][MT][NT][4];                         // O^T: rows = elements, columns = heads 2t, 2t + 1
+    float o[NC][2][NT][4];                         // O^T: columns = heads 2t, 2t + 1; tile (c, i): bytes 2g + i of chunk c, whole
+                                                   // in rows 0-7 and their high nibbles in rows 8-15
     float mo[NT][G][2], m_run[NT][2], l_run[NT][2];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
@@ -287,47 +298,34 @@ __global__ void __launch_bounds__(NW * 32, CTAS) paged_decode_attn_q4_kernel(con
             m_run[nt][hh] = kLowest;
             l_run[nt][hh] = 0.0f;
 #pragma unroll
-            for (int gq = 0; gq < G; ++gq) {
-                mo[nt][gq][hh] = 0.0f;
+            for (int gq = 0; gq < G; ++gq) mo[nt][gq][hh] = 0.0f;
 #pragma unroll
-                for (int mt = 0; mt < MT; ++mt) o[gq][mt][nt][hh] = o[gq][mt][nt][2 + hh] = 0.0f;
-            }
+            for (int c = 0; c < NC; ++c)
+#pragma unroll
+                for (int i = 0; i < 2; ++i) o[c][i][nt][hh] = o[c][i][nt][2 + hh] = 0.0f;
         }
     // power of two on V's scales: the largest one seen * vf is in [64, 128); before any, so high that one moves it
     float vf = 1.329227995784916e36f;              // 2^120
     float v_top = 0.0f;
 
-    // lane parts of the shared-memory addresses
-    constexpr int KB = 4 * KW;                     // K bytes per lane, row and group
-    uint32_t k_off[G], v_off[G];
-#pragma unroll
-    for (int gq = 0; gq < G; ++gq) {
-        const int kb = gq * (GE / 2) + t * KB;
-        k_off[gq] = q4_tile_offset<RB>(g, kb / 16) + kb % 16;
-        const int vb = VE == 4 ? gq * (GE / 2) + (g >> 1) * 4 : gq * (GE / 2) + g * (VE / 2);
-        v_off[gq] = q4_tile_offset<RB>(2 * t, vb / 16) + vb % 16;
-    }
-    constexpr uint32_t NEXT_ROW = RB;              // row 2t + 1 sits in the same line: its unit differs in one bit
-    constexpr uint32_t ROWS8 = 8 * RB;
+    // ldmatrix addresses, the same for K (word t of a row's chunk lands in lane (row, t)) and, transposed, for V (the
+    // 16-bit halves of tokens 2t and 2t + 1 side by side): matrices 0 and 1 are rows 0-7 and 8-15 of one chunk, 2 and
+    // 3 of the next.
+    const uint32_t mat_off = q4_tile_offset<RB>(((lane >> 3) & 1) * 8 + (lane & 7), lane >> 4);
 
+    uint32_t stage = 0;
     for (int j = 0; j < n_my; ++j) {
         cp_async_wait<STAGES - 1>();
         __syncwarp();
-        const uint32_t stage = (j % STAGES) * L::STAGE_BYTES;
-        const uint8_t* kt = smem_gen + (ring - smem_base) + stage;
-        const uint8_t* vt = kt + L::K_BYTES;
-        const uint8_t* pt = vt + L::K_BYTES;
+        const uint32_t kt = ring + stage;
+        const uint8_t* pt = smem + warp * L::RING_BYTES + stage + 2 * L::K_BYTES;
 
         // Which of the tile's tokens count: those before the end, and not between the sinks and the window.
         const int r0 = range0(j);
         uint32_t valid = 0xffffffffu;
-        {
-            const int a = token_of(r0), c = token_of(r0 + GRAN);
-            const bool hole = (a < tok_lo && a + GRAN > p.sinks) || (c < tok_lo && c + GRAN > p.sinks);
-            if (r0 + TILE > tok_end || hole) {
-                const int tk = token_of(r0 + (lane & ~15)) + (lane & 15);
-                valid = __ballot_sync(0xffffffffu, r0 + lane < tok_end && !(tk >= p.sinks && tk < tok_lo));
-            }
+        if (r0 + TILE > tok_end || (r0 < hole_hi && r0 + TILE > hole_lo)) {
+            const int r = r0 + lane;
+            valid = __ballot_sync(0xffffffffu, r < tok_end && !(r >= hole_lo && r < hole_hi));
         }
 
         // ---- scores ------------------------------------------------------------------------------------------
@@ -342,23 +340,25 @@ __global__ void __launch_bounds__(NW * 32, CTAS) paged_decode_attn_q4_kernel(con
             load_words(pr[sb][1], pt + (sb * 16 + 8 + g) * PB);
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) sc[sb][nt][0] = sc[sb][nt][1] = sc[sb][nt][2] = sc[sb][nt][3] = 0.0f;
+            uint32_t kw[NC][2];                    // word t of rows g and g + 8, per chunk
+#pragma unroll
+            for (int c = 0; c < NC; c += 2)        // the next two chunks: one bit of the swizzled unit
+                ldmatrix_x4(kw[c][0], kw[c][1], kw[c + 1][0], kw[c + 1][1], kt + sb * 16 * RB + (mat_off ^ (c * 16)));
 #pragma unroll
             for (int gq = 0; gq < G; ++gq) {
                 float acc[NT][4];
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) acc[nt][0] = acc[nt][1] = acc[nt][2] = acc[nt][3] = 0.0f;
-                uint32_t w0[KW], w1[KW];
-                load_words(w0, kt + sb * 16 * RB + k_off[gq]);
-                load_words(w1, kt + sb * 16 * RB + ROWS8 + k_off[gq]);
 #pragma unroll
-                for (int w = 0; w < KW; ++w) {
-                    const uint32_t x0 = w0[w], x1 = w1[w], y0 = x0 >> 8, y1 = x1 >> 8;
+                for (int w = 0; w < CPG; ++w) {
+                    const int c = gq * CPG + w;
+                    const uint32_t x0 = kw[c][0], x1 = kw[c][1], y0 = x0 >> 8, y1 = x1 >> 8;
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt) {
                         mma_f16_16816(acc[nt], x0 & 0x000F000Fu, x1 & 0x000F000Fu, x0 & 0x00F000F0u, x1 & 0x00F000F0u,
-                                      qb[nt][gq][w][0], qb[nt][gq][w][1]);
+                                      qb[nt][c][0], qb[nt][c][1]);
                         mma_f16_16816(acc[nt], y0 & 0x000F000Fu, y1 & 0x000F000Fu, y0 & 0x00F000F0u, y1 & 0x00F000F0u,
-                                      qb[nt][gq][w][2], qb[nt][gq][w][3]);
+                                      qb[nt][c][2], qb[nt][c][3]);
                     }
                 }
 #pragma unroll
@@ -385,19 +385,23 @@ __global__ void __launch_bounds__(NW * 32, CTAS) paged_decode_attn_q4_kernel(con
         }
 
         // ---- V parameters, and whether the references still serve -------------------------------------------------
+        if (valid != 0xffffffffu) {                // whatever those slots hold: 0 * NaN must not enter the sums
+#pragma unroll
+            for (int sb = 0; sb < 2; ++sb)
+#pragma unroll
+                for (int r = 0; r < 2; ++r)
+                    if (!((valid >> (sb * 16 + r * 8 + g)) & 1u)) {
+#pragma unroll
+                        for (int gq = 0; gq < G; ++gq) pr[sb][r][G + gq] = 0u;
+                    }
+        }
         float v_max = 0.0f;
 #pragma unroll
         for (int sb = 0; sb < 2; ++sb)
 #pragma unroll
-            for (int r = 0; r < 2; ++r) {
-                const int row = sb * 16 + r * 8 + g;
-                const bool on = (valid >> row) & 1u;
+            for (int r = 0; r < 2; ++r)
 #pragma unroll
-                for (int gq = 0; gq < G; ++gq) {
-                    if (!on) pr[sb][r][G + gq] = 0u;   // whatever the slot holds: 0 * NaN must not enter the sums
-                    v_max = fmaxf(v_max, __uint_as_float(pr[sb][r][G + gq] << 16));
-                }
-            }
+                for (int gq = 0; gq < G; ++gq) v_max = fmaxf(v_max, __uint_as_float(pr[sb][r][G + gq] << 16));
         bool move = v_max * vf >= 128.0f;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
@@ -435,20 +439,25 @@ __global__ void __launch_bounds__(NW * 32, CTAS) paged_decode_attn_q4_kernel(con
                     l_run[nt][hh] *= alpha;
                     const float both = alpha * vr;
 #pragma unroll
-                    for (int gq = 0; gq < G; ++gq) {
-                        mo[nt][gq][hh] *= alpha;
+                    for (int gq = 0; gq < G; ++gq) mo[nt][gq][hh] *= alpha;
 #pragma unroll
-                        for (int mt = 0; mt < MT; ++mt) {
-                            o[gq][mt][nt][hh] *= both;
-                            o[gq][mt][nt][2 + hh] *= both;
+                    for (int c = 0; c < NC; ++c)
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) {
+                            o[c][i][nt][hh] *= both;
+                            o[c][i][nt][2 + hh] *= both;
                         }
-                    }
                 }
         }
 
         // ---- weights and O^T += V^T P^T ----------------------------------------------------------------------------
 #pragma unroll
         for (int sb = 0; sb < 2; ++sb) {
+            uint32_t vw[NC][2];
+#pragma unroll
+            for (int c = 0; c < NC; c += 2)
+                ldmatrix_x4_trans(vw[c][0], vw[c][1], vw[c + 1][0], vw[c + 1][1],
+                                  kt + L::K_BYTES + sb * 16 * RB + (mat_off ^ (c * 16)));
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -469,31 +478,17 @@ __global__ void __launch_bounds__(NW * 32, CTAS) paged_decode_attn_q4_kernel(con
                         mo[nt][gq][0] = fmaf(sc[sb][nt][2 * r], vm, mo[nt][gq][0]);
                         mo[nt][gq][1] = fmaf(sc[sb][nt][2 * r + 1], vm, mo[nt][gq][1]);
                     }
-                const uint8_t* base = vt + sb * 16 * RB;
-                const uint32_t first = v_off[gq], second = v_off[gq] ^ NEXT_ROW;
-                constexpr int VW = VE >= 8 ? VE / 8 : 1;
-                uint32_t ta[VW], tb[VW], tc[VW], td[VW];
-                load_words(ta, base + first);
-                load_words(tb, base + second);
-                load_words(tc, base + ROWS8 + first);
-                load_words(td, base + ROWS8 + second);
 #pragma unroll
-                for (int w = 0; w < VW; ++w) {
-                    // pairs of tokens side by side: 16-bit halves (four codes) of tokens 2t, 2t + 1 and 2t + 8, 2t + 9
+                for (int w = 0; w < CPG; ++w) {
+                    const int c = gq * CPG + w;
+                    // halves (four codes) of tokens 2t, 2t + 1 in x and of 2t + 8, 2t + 9 in y; then their upper bytes
+                    const uint32_t x = vw[c][0], y = vw[c][1];
+                    const uint32_t x1 = __byte_perm(x, 0u, 0x4341), y1 = __byte_perm(y, 0u, 0x4341);
 #pragma unroll
-                    for (int half = 0; half < (VE >= 8 ? 2 : 1); ++half) {
-                        const uint32_t sel = VE == 4 ? ((g & 1) ? 0x7632u : 0x5410u) : (half ? 0x7632u : 0x5410u);
-                        const uint32_t x = __byte_perm(ta[w], tb[w], sel), y = __byte_perm(tc[w], td[w], sel);
-                        const int mt = VE >= 8 ? w * 4 + half * 2 : 0;
-#pragma unroll
-                        for (int nt = 0; nt < NT; ++nt)
-                            mma_f16_16816(o[gq][mt][nt], x & 0x000F000Fu, x & 0x00F000F0u, y & 0x000F000Fu,
-                                          y & 0x00F000F0u, pb[nt][0], pb[nt][1]);
-                        const uint32_t x8 = x >> 8, y8 = y >> 8;
-#pragma unroll
-                        for (int nt = 0; nt < NT; ++nt)
-                            mma_f16_16816(o[gq][mt + 1][nt], x8 & 0x000F000Fu, x8 & 0x00F000F0u, y8 & 0x000F000Fu,
-                                          y8 & 0x00F000F0u, pb[nt][0], pb[nt][1]);
+                    for (int nt = 0; nt < NT; ++nt) {
+                        mma_f16_16816(o[c][0][nt], x & 0x00FF00FFu, x & 0x00F000F0u, y & 0x00FF00FFu, y & 0x00F000F0u,
+                                      pb[nt][0], pb[nt][1]);
+                        mma_f16_16816(o[c][1][nt], x1, x1 & 0x00F000F0u, y1, y1 & 0x00F000F0u, pb[nt][0], pb[nt][1]);
                     }
                 }
             }
@@ -502,11 +497,15 @@ __global__ void __launch_bounds__(NW * 32, CTAS) paged_decode_attn_q4_kernel(con
         // ---- refill this stage ------------------------------------------------------------------------------------
         __syncwarp();
         if (j + STAGES < n_my) {
-            issue(j + STAGES, next0, next1);
-            next0 = load_page(j + STAGES + 1, 0);
-            next1 = load_page(j + STAGES + 1, 1);
+            const int next = j + STAGES;
+            if ((next & 15) == 0) {
+                settle_pages(next, pages_ahead);
+                pages_ahead = load_pages(next + 16);
+            }
+            issue(next, stage);
         }
         cp_async_commit();
+        stage = stage + L::STAGE_BYTES == L::RING_BYTES ? 0u : stage + L::STAGE_BYTES;
     }
     cp_async_wait<0>();
     __syncwarp();
@@ -515,7 +514,7 @@ __global__ void __launch_bounds__(NW * 32, CTAS) paged_decode_attn_q4_kernel(con
     constexpr int WROWS = 8 * NT;
     constexpr int WSTRIDE = D + 8;
     static_assert((WROWS * WSTRIDE + 2 * WROWS) * 4 <= L::RING_BYTES, "merge scratch must fit in a ring");
-    float* wo = reinterpret_cast<float*>(smem_gen + warp * L::RING_BYTES);
+    float* wo = reinterpret_cast<float*>(smem + warp * L::RING_BYTES);
     float* wm = wo + WROWS * WSTRIDE;
     float* wl = wm + WROWS;
     const float back = 16777216.0f, unscale = 1.0f / vf;       // two factors: their product may leave fp32's range
@@ -537,10 +536,16 @@ __global__ void __launch_bounds__(NW * 32, CTAS) paged_decode_attn_q4_kernel(con
 #pragma unroll
                 for (int off = 4; off < 32; off <<= 1) m += __shfl_xor_sync(0xffffffffu, m, off);
 #pragma unroll
-                for (int mt = 0; mt < MT; ++mt) {
-                    const float even = o[gq][mt][nt][hh] * back * unscale + m;
-                    const float odd = o[gq][mt][nt][2 + hh] * (back * 0.0625f) * unscale + m;
-                    *reinterpret_cast<float2*>(wo + row * WSTRIDE + gq * GE + g * VE + 2 * mt) = make_float2(even, odd);
+                for (int w = 0; w < CPG; ++w) {
+                    const int c = gq * CPG + w;
+                    float val[4];
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const float hi = o[c][i][nt][2 + hh];
+                        val[2 * i] = (o[c][i][nt][hh] - hi) * back * unscale + m;
+                        val[2 * i + 1] = hi * (back * 0.0625f) * unscale + m;
+                    }
+                    *reinterpret_cast<float4*>(wo + row * WSTRIDE + c * 32 + g * 4) = make_float4(val[0], val[1], val[2], val[3]);
                 }
             }
         }
@@ -554,14 +559,14 @@ __global__ void __launch_bounds__(NW * 32, CTAS) paged_decode_attn_q4_kernel(con
         float M = kLowest;
 #pragma unroll
         for (int w = 0; w < WARPS; ++w) {
-            mw[w] = reinterpret_cast<const float*>(smem_gen + w * L::RING_BYTES)[WROWS * WSTRIDE + row];
+            mw[w] = reinterpret_cast<const float*>(smem + w * L::RING_BYTES)[WROWS * WSTRIDE + row];
             M = fmaxf(M, mw[w]);
         }
         float4 num = make_float4(0.f, 0.f, 0.f, 0.f);
         float den = 0.0f;
 #pragma unroll
         for (int w = 0; w < WARPS; ++w) {
-            const float* base = reinterpret_cast<const float*>(smem_gen + w * L::RING_BYTES);
+            const float* base = reinterpret_cast<const float*>(smem + w * L::RING_BYTES);
             const float wgt = exp2f(mw[w] - M);
             const float4 o4 = *reinterpret_cast<const float4*>(base + row * WSTRIDE + col);
             num.x = fmaf(wgt, o4.x, num.x);

@@ -60,10 +60,9 @@ __device__ __forceinline__ uint32_t q4_quantise(const uint16_t (&x)[EPL], uint32
 }
 
 // Byte offset of 16-byte chunk `chunk` of row `row` in a tile of packed rows of RB bytes (64 or 32).  The rows
-// of a 128-byte line are XORed by a line-dependent unit so that every access pattern of the attention kernel
-// touches the 32 banks evenly: eight consecutive rows at one chunk (4-byte reads of a 32-element group), four
-// consecutive rows at two chunks (8-byte reads of a 64-element group), and rows 0, 2, 4, 6 at one or two chunks
-// (the V reads).
+// of a 128-byte line are XORed by a line-dependent unit so that one chunk of eight consecutive rows (what an ldmatrix
+// phase reads) falls into eight different 16-byte units.  Rows 8 further are 8 * RB bytes further (same unit), and
+// chunk ^ 2 of the same row is the offset ^ 32.
 template <int RB>
 __device__ __forceinline__ uint32_t q4_tile_offset(int row, int chunk) {
     if (RB == 64) {
