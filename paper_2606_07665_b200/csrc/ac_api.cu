@@ -957,7 +957,7 @@ static int kv_bulk_q4(void* k, void* v, const ac_q4_cache* cache, const int32_t*
     if (total_tokens == 0) return AC_OK;
     cudaError_t e = launch_kv_bulk_q4(k, v, view, block_table, max_pages_per_seq, start_pos, row_offsets,
                                       total_tokens, B, Hkv, d, page_size, num_pages, status_flag, store,
-                                      static_cast<cudaStream_t>(stream));
+                                      g_devices[dev].sm_count, static_cast<cudaStream_t>(stream));
     return e == cudaSuccess ? AC_OK : fail_cuda(static_cast<int>(e));
 }
 

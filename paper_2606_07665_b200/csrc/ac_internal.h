@@ -126,7 +126,7 @@ cudaError_t launch_rope_kv_append_q4(const void* q_in, void* q_out, const void* 
 cudaError_t launch_kv_bulk_q4(void* k, void* v, const Q4View& cache, const int32_t* block_table,
                               int max_pages_per_seq, const int32_t* start_pos, const int32_t* row_offsets,
                               int total_tokens, int B, int Hkv, int d, int page_size, int num_pages,
-                              int32_t* status_flag, bool store, cudaStream_t stream);
+                              int32_t* status_flag, bool store, int sms, cudaStream_t stream);
 cudaError_t q4_attn_set_attributes(int smem_optin);
 cudaError_t launch_paged_decode_attn_q4(const void* q_rot, const Q4View& cache, const int32_t* block_table,
                                         int max_pages_per_seq, const int32_t* context_lens, int new_tokens,

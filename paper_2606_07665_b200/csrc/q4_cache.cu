@@ -64,17 +64,16 @@ __global__ void __launch_bounds__(128) rope_kv_append_q4_kernel(
         for (int e = 0; e < EPL; ++e) dst[lane * EPL + e] = x[e];
         return;
     }
-    uint32_t c[EPL];
     constexpr int LANES = 32 / G;
-    const uint32_t sm = q4_quantise<EPL, LANES>(x, c, 0xffffffffu);
+    uint32_t words[EPL / 2], packed;
+#pragma unroll
+    for (int w = 0; w < EPL / 2; ++w) words[w] = x[2 * w] | (static_cast<uint32_t>(x[2 * w + 1]) << 16);
+    const uint32_t sm = q4_quantise<EPL / 2, LANES>(words, packed, 0xffffffffu);
     const int slot = p - page_idx * page_size;
     uint8_t* dst = (is_v ? cache.v_codes : cache.k_codes) + static_cast<int64_t>(page) * cache.stride_page +
                    slot * cache.stride_token + h * cache.stride_head + lane * (EPL / 2);
-    if (EPL == 4) {
-        *reinterpret_cast<uint16_t*>(dst) = static_cast<uint16_t>(c[0] | (c[1] << 4) | (c[EPL - 2] << 8) | (c[EPL - 1] << 12));
-    } else {
-        *dst = static_cast<uint8_t>(c[0] | (c[1] << 4));
-    }
+    if (EPL == 4) *reinterpret_cast<uint16_t*>(dst) = static_cast<uint16_t>(packed);
+    else *dst = static_cast<uint8_t>(packed);
     if (lane % LANES == 0) {
         uint32_t* prm = cache.params + ((static_cast<int64_t>(page) * Hkv + h) * page_size + slot) * (2 * G);
         prm[(is_v ? G : 0) + lane / LANES] = sm;
@@ -83,11 +82,15 @@ __global__ void __launch_bounds__(128) rope_kv_append_q4_kernel(
 
 // ---- bulk store and load ---------------------------------------------------------------------------------
 //
-// A CTA takes kTokens consecutive tokens of the dense side.  One thread per token finds its row (binary search in
-// row_offsets), position, page and slot; then the CTA walks (token, side, head) vectors, D/8 lanes of 16 dense
-// bytes (4 packed ones) each.  Bound: HBM, 2 dense and 0.56 packed bytes per element at group 64.
-constexpr int kTokens = 16;
-constexpr int kStoreThreads = 256;
+// Persistent CTAs take blocks of kTokens consecutive tokens in turn.  One warp does nothing but find the next block's
+// slots (row by binary search in row_offsets, position, page; a chain of dependent loads) while the others work on this
+// block's (token, head) vectors, K then V: D/8 lanes of 16 dense bytes (4 packed ones) per vector, kInHand vectors
+// per lane at a time so that their loads overlap.
+// Bound: HBM, 2 dense and 0.56 packed bytes per element at group 64.
+constexpr int kTokens = 32;
+constexpr int kStoreThreads = 256;                         // workers; one more warp looks up
+constexpr int kStoreCtas = 3;                              // per SM
+constexpr int kInHand = 4;
 
 struct TokenSlot {
     int page;             // -1: no slot
@@ -123,84 +126,122 @@ __device__ __forceinline__ TokenSlot find_slot(long long token, const int32_t* b
 }
 
 template <int D, int G, bool STORE>
-__global__ void __launch_bounds__(kStoreThreads) kv_bulk_q4_kernel(
+__global__ void __launch_bounds__(kStoreThreads + 32, kStoreCtas) kv_bulk_q4_kernel(
     uint16_t* k, uint16_t* v, const Q4View cache, const int32_t* __restrict__ block_table, int max_pages_per_seq,
     const int32_t* __restrict__ start_pos, const int32_t* __restrict__ row_offsets, int total_tokens, int B, int Hkv,
     int page_size, int num_pages, int32_t* status_flag) {
     constexpr int LPV = D / 8;                             // lanes per vector
-    constexpr int VECS = kStoreThreads / LPV;              // vectors in hand at a time
+    constexpr int VECS = kStoreThreads / LPV;              // vectors per pass of the CTA
     constexpr int LANES = LPV / G;                         // lanes per group
-    __shared__ TokenSlot s_slot[kTokens];
-    const long long t0 = static_cast<long long>(blockIdx.x) * kTokens;
-    if (threadIdx.x < kTokens) {
+    __shared__ TokenSlot s_slot[2][kTokens];
+    const int blocks = static_cast<int>((static_cast<long long>(total_tokens) + kTokens - 1) / kTokens);
+    const bool lookup = threadIdx.x >= kStoreThreads;
+    auto look_up = [&](int block, int buffer) {
+        const int lane = threadIdx.x & 31;
+        const long long token = static_cast<long long>(block) * kTokens + lane;
         TokenSlot r{-1, 0};
-        if (t0 + threadIdx.x < total_tokens)
-            r = find_slot(t0 + threadIdx.x, block_table, max_pages_per_seq, start_pos, row_offsets, B, page_size,
-                          num_pages, status_flag);
-        s_slot[threadIdx.x] = r;
-    }
+        if (token < total_tokens)
+            r = find_slot(token, block_table, max_pages_per_seq, start_pos, row_offsets, B, page_size, num_pages, status_flag);
+        s_slot[buffer][lane] = r;
+    };
+    if (lookup && static_cast<int>(blockIdx.x) < blocks) look_up(blockIdx.x, 0);
     __syncthreads();
-    const int tokens = total_tokens - t0 < kTokens ? static_cast<int>(total_tokens - t0) : kTokens;
+
     const int sub = threadIdx.x % LPV;
-    const int vecs = tokens * 2 * Hkv;                     // (side, token, head), head fastest
     const uint32_t lanes = LPV == 16 ? 0xffffu << (threadIdx.x & 16) : 0xffu << (threadIdx.x & 24);
-    for (int i = threadIdx.x / LPV; i < vecs; i += VECS) {
-        const int side = i / (tokens * Hkv);
-        const int rest = i - side * tokens * Hkv;
-        const int t = rest / Hkv;
-        const int h = rest - t * Hkv;
-        const TokenSlot at = s_slot[t];
-        uint16_t* dense = (side ? v : k) + ((t0 + t) * Hkv + h) * D + sub * 8;
-        uint8_t* codes = (side ? cache.v_codes : cache.k_codes) + static_cast<int64_t>(at.page) * cache.stride_page +
-                         at.slot * cache.stride_token + h * cache.stride_head + sub * 4;
-        uint32_t* prm = cache.params + ((static_cast<int64_t>(at.page) * Hkv + h) * page_size + at.slot) * (2 * G) +
-                        side * G + sub / LANES;
-        if (STORE) {
-            if (at.page < 0) continue;                     // uniform over the vector's lanes
-            const uint4 raw = *reinterpret_cast<const uint4*>(dense);
-            const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
-            uint16_t x[8];
-            uint32_t c[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] = static_cast<uint16_t>(w[e >> 1] >> ((e & 1) * 16));
-            const uint32_t sm = q4_quantise<8, LANES>(x, c, lanes);
-            uint32_t packed = 0;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) packed |= c[e] << (4 * e);
-            *reinterpret_cast<uint32_t*>(codes) = packed;
-            if (sub % LANES == 0) *prm = sm;
-        } else {
-            uint4 o = make_uint4(0u, 0u, 0u, 0u);
-            if (at.page >= 0) {
-                const uint32_t packed = *reinterpret_cast<const uint32_t*>(codes);
-                const uint32_t sm = *prm;
-                const float s = __uint_as_float(sm << 16), m = __uint_as_float(sm & 0xFFFF0000u);
-                float y[8];
-#pragma unroll
-                for (int e = 0; e < 8; ++e) y[e] = fmaf(static_cast<float>((packed >> (4 * e)) & 15u), s, m);
-                o = make_uint4(pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3]), pack_bf16x2(y[4], y[5]),
-                               pack_bf16x2(y[6], y[7]));
-            }
-            *reinterpret_cast<uint4*>(dense) = o;
+    // (token, head) of a lane's vectors is stepped instead of divided
+    const int first_t = (threadIdx.x / LPV) / Hkv, first_h = threadIdx.x / LPV - first_t * Hkv;
+    const int step_t = VECS / Hkv, step_h = VECS - step_t * Hkv;
+    int buffer = 0;
+    for (int block = blockIdx.x; block < blocks; block += gridDim.x, buffer ^= 1) {
+        if (lookup) {
+            if (block + static_cast<int>(gridDim.x) < blocks) look_up(block + gridDim.x, buffer ^ 1);
+            __syncthreads();
+            continue;
         }
+        const long long t0 = static_cast<long long>(block) * kTokens;
+        const int tokens = total_tokens - t0 < kTokens ? static_cast<int>(total_tokens - t0) : kTokens;
+        const int vecs = tokens * Hkv;                     // (token, head), head fastest: dense order
+        for (int side = 0; side < 2; ++side) {
+            uint16_t* const dense = (side ? v : k) + t0 * Hkv * D + sub * 8;
+            uint8_t* const codes = (side ? cache.v_codes : cache.k_codes) + sub * 4;
+            uint32_t* const params = cache.params + side * G + sub / LANES;
+            int t = first_t, h = first_h;
+            for (int i = threadIdx.x / LPV; i < vecs; i += kInHand * VECS) {
+                bool live[kInHand];
+                uint8_t* code_at[kInHand];
+                uint32_t* param_at[kInHand];
+                uint4 raw[kInHand];
+                uint32_t word[kInHand], sm[kInHand];
+#pragma unroll
+                for (int u = 0; u < kInHand; ++u) {
+                    const bool on = i + u * VECS < vecs;
+                    const TokenSlot at = s_slot[buffer][on ? t : 0];
+                    live[u] = on && at.page >= 0;
+                    const int64_t pg = live[u] ? at.page : 0;
+                    const int slot = live[u] ? at.slot : 0;
+                    const int hh = live[u] ? h : 0;
+                    code_at[u] = codes + pg * cache.stride_page + slot * cache.stride_token + hh * cache.stride_head;
+                    param_at[u] = params + ((pg * Hkv + hh) * page_size + slot) * (2 * G);
+                    if (STORE) {
+                        if (live[u]) raw[u] = __ldcs(reinterpret_cast<const uint4*>(dense + static_cast<int64_t>(i + u * VECS) * D));
+                    } else if (live[u]) {
+                        word[u] = *reinterpret_cast<const uint32_t*>(code_at[u]);
+                        sm[u] = *param_at[u];
+                    }
+                    t += step_t;
+                    h += step_h;
+                    if (h >= Hkv) {
+                        h -= Hkv;
+                        ++t;
+                    }
+                }
+#pragma unroll
+                for (int u = 0; u < kInHand; ++u) {
+                    if (STORE) {
+                        if (!live[u]) continue;            // uniform over the vector's lanes
+                        const uint32_t x[4] = {raw[u].x, raw[u].y, raw[u].z, raw[u].w};
+                        uint32_t packed;
+                        const uint32_t p = q4_quantise<4, LANES>(x, packed, lanes);
+                        *reinterpret_cast<uint32_t*>(code_at[u]) = packed;
+                        if (sub % LANES == 0) *param_at[u] = p;
+                    } else if (i + u * VECS < vecs) {
+                        uint4 o = make_uint4(0u, 0u, 0u, 0u);
+                        if (live[u]) {
+                            const float s = __uint_as_float(sm[u] << 16), m = __uint_as_float(sm[u] & 0xFFFF0000u);
+                            float y[8];
+#pragma unroll
+                            for (int e = 0; e < 8; ++e)    // 2^23 + c, whose low bits are the code, minus 2^23
+                                y[e] = fmaf(__uint_as_float(((word[u] >> (4 * e)) & 15u) | 0x4B000000u) - 8388608.0f, s, m);
+                            o = make_uint4(pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3]), pack_bf16x2(y[4], y[5]),
+                                           pack_bf16x2(y[6], y[7]));
+                        }
+                        __stcs(reinterpret_cast<uint4*>(dense + static_cast<int64_t>(i + u * VECS) * D), o);
+                    }
+                }
+            }
+        }
+        __syncthreads();                                   // this block's slots are free, the next one's are there
     }
 }
 
 template <int D, int G>
 cudaError_t launch_bulk(void* k, void* v, const Q4View& cache, const int32_t* block_table, int max_pages_per_seq,
                         const int32_t* start_pos, const int32_t* row_offsets, int total_tokens, int B, int Hkv,
-                        int page_size, int num_pages, int32_t* status_flag, bool store, cudaStream_t stream) {
+                        int page_size, int num_pages, int32_t* status_flag, bool store, int sms,
+                        cudaStream_t stream) {
     // Ordinary launches: what follows them in the stream may read the cache before its own synchronisation, which
     // is safe only behind kernels that do not signal early.
-    const unsigned grid = static_cast<unsigned>((static_cast<long long>(total_tokens) + kTokens - 1) / kTokens);
+    const long long blocks = (static_cast<long long>(total_tokens) + kTokens - 1) / kTokens;
+    const unsigned grid = static_cast<unsigned>(blocks < kStoreCtas * sms ? blocks : kStoreCtas * sms);
     uint16_t* kk = static_cast<uint16_t*>(k);
     uint16_t* vv = static_cast<uint16_t*>(v);
     if (store)
-        kv_bulk_q4_kernel<D, G, true><<<grid, kStoreThreads, 0, stream>>>(
+        kv_bulk_q4_kernel<D, G, true><<<grid, kStoreThreads + 32, 0, stream>>>(
             kk, vv, cache, block_table, max_pages_per_seq, start_pos, row_offsets, total_tokens, B, Hkv, page_size,
             num_pages, status_flag);
     else
-        kv_bulk_q4_kernel<D, G, false><<<grid, kStoreThreads, 0, stream>>>(
+        kv_bulk_q4_kernel<D, G, false><<<grid, kStoreThreads + 32, 0, stream>>>(
             kk, vv, cache, block_table, max_pages_per_seq, start_pos, row_offsets, total_tokens, B, Hkv, page_size,
             num_pages, status_flag);
     return cudaGetLastError();
@@ -241,10 +282,10 @@ cudaError_t launch_rope_kv_append_q4(const void* q_in, void* q_out, const void* 
 cudaError_t launch_kv_bulk_q4(void* k, void* v, const Q4View& cache, const int32_t* block_table,
                               int max_pages_per_seq, const int32_t* start_pos, const int32_t* row_offsets,
                               int total_tokens, int B, int Hkv, int d, int page_size, int num_pages,
-                              int32_t* status_flag, bool store, cudaStream_t stream) {
+                              int32_t* status_flag, bool store, int sms, cudaStream_t stream) {
 #define AC_Q4_BULK(D_, G_)                                                                                          \
     launch_bulk<D_, G_>(k, v, cache, block_table, max_pages_per_seq, start_pos, row_offsets, total_tokens, B, Hkv,  \
-                        page_size, num_pages, status_flag, store, stream)
+                        page_size, num_pages, status_flag, store, sms, stream)
     const int groups = d / cache.group;
     if (d == 128) return groups == 1 ? AC_Q4_BULK(128, 1) : groups == 2 ? AC_Q4_BULK(128, 2) : AC_Q4_BULK(128, 4);
     return groups == 1 ? AC_Q4_BULK(64, 1) : AC_Q4_BULK(64, 2);

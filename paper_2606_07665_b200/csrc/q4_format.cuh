@@ -6,53 +6,87 @@
 
 namespace acdev {
 
-// Quantises EPL consecutive elements per lane (bf16 bits).  A group is the elements of LANES consecutive,
-// aligned lanes, all of which must call this together with `mask` the lanes that execute it.  On return c[e]
-// are the codes, and every lane of the group has the group's (s, m) packed as two bf16 (s in the low half).
-//
-// Arithmetic, as the format defines it: minimum and maximum are exact; the quotient (max - min) / 15 is an
-// fp64 division, rounded to fp32 and then to bf16; the code is rint((x - m) / s) in fp64.  The fp64 division
-// is only made where it can matter: t = fl32(x - m) and q = fl32(t / s) are within 2^-22 of the real quotient
-// relative (two roundings of 2^-24 each, and the fp64 chain adds 2^-52), q <= 15.1, so |q - quotient| < 4e-6,
-// and the fp32 rint decides unless q lies within 1e-4 of a half.
-template <int EPL, int LANES>
-__device__ __forceinline__ uint32_t q4_quantise(const uint16_t (&x)[EPL], uint32_t (&c)[EPL], uint32_t mask) {
-    float f[EPL];
-    float lo = INFINITY, hi = -INFINITY;
-    uint32_t exponents = 0;                               // all ones in the exponent: infinity or NaN
-#pragma unroll
-    for (int e = 0; e < EPL; ++e) {
-        f[e] = bf16_bits_to_float(x[e]);
-        lo = fminf(lo, f[e]);
-        hi = fmaxf(hi, f[e]);
-        exponents = max(exponents, static_cast<uint32_t>(x[e] & 0x7F80u));
-    }
-#pragma unroll
-    for (int off = 1; off < LANES; off <<= 1) {
-        lo = fminf(lo, __shfl_xor_sync(mask, lo, off));
-        hi = fmaxf(hi, __shfl_xor_sync(mask, hi, off));
-        exponents = max(exponents, __shfl_xor_sync(mask, exponents, off));
-    }
-    if (exponents == 0x7F80u) {
-#pragma unroll
-        for (int e = 0; e < EPL; ++e) c[e] = 0u;
-        return 0x7FC00000u;                               // s = 0, m = NaN
-    }
+// Two bf16 at a time; a NaN in either operand comes through.
+__device__ __forceinline__ uint32_t bf16x2_max_nan(uint32_t a, uint32_t b) {
+    uint32_t r;
+    asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+__device__ __forceinline__ uint32_t bf16x2_min_nan(uint32_t a, uint32_t b) {
+    uint32_t r;
+    asm("min.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+
+// The definition in fp64, for what the fast path below cannot decide; out of line, it is rare.
+__device__ __noinline__ inline uint32_t q4_scale_f64(float lo, float hi) {
     const double range = __dsub_rn(static_cast<double>(hi), static_cast<double>(lo));
     const float s32 = __double2float_rn(__ddiv_rn(range, 15.0));
-    const uint32_t s16 = pack_bf16x2(s32, 0.0f) & 0x7FFFu;   // a group of both zeros may give -0: the scale is +0
-    const float s = __uint_as_float(s16 << 16);
+    return pack_bf16x2(s32, 0.0f) & 0x7FFFu;               // a group of both zeros may give -0: the scale is +0
+}
+__device__ __noinline__ inline float q4_code_f64(float x, float lo, float s) {
+    if (!(s > 0.0f)) return 0.0f;
+    const double q = __ddiv_rn(__dsub_rn(static_cast<double>(x), static_cast<double>(lo)), static_cast<double>(s));
+    return fminf(static_cast<float>(rint(q)), 15.0f);
+}
+
+// Quantises W words of two bf16 per lane.  A group is the elements of LANES consecutive, aligned lanes, all of
+// which must call this together with `mask` the lanes that execute it.  On return `packed` holds the lane's codes,
+// the first in the low nibble, and every lane of the group gets its (s, m) as two bf16, s in the low half.
+//
+// Arithmetic.  Minimum and maximum are exact (kept as the pair (max, -min), one shuffle and one instruction a step;
+// NaN comes through, an infinity shows in them).  The format's fp64 quotients are evaluated in fp32 wherever
+// that provably rounds alike:
+//   scale  s32 = fl(fl(max - min) / 15) is within 2^-22 relative (four of its own ulps) of the quotient, so the bf16
+//          next to it is the right one unless the 16 bits cut off lie within 8 of the tie; tiny and overflowing
+//          ranges are left to fp64;
+//   codes  with t = fl(x - m) and r the approximate reciprocal of s, t * r is within 2^-21 relative of the
+//          quotient, so below 16 within 8e-6: the integer nearest to it is the right code unless it is within
+//          2^-10 of a half (checked on the exact residual fma(t, r, -code)), or s is subnormal.
+template <int W, int LANES>
+__device__ __forceinline__ uint32_t q4_quantise(const uint32_t (&x)[W], uint32_t& packed, uint32_t mask) {
+    uint32_t top = x[0], bottom = x[0];
 #pragma unroll
-    for (int e = 0; e < EPL; ++e) {
-        float r = 0.0f;
-        if (s > 0.0f) {
-            const float q = __fdiv_rn(__fsub_rn(f[e], lo), s);
-            r = rintf(q);
-            if (!(fabsf(fabsf(q - r) - 0.5f) >= 1e-4f))   // near a half, or x - m beyond fp32
-                r = static_cast<float>(rint(__ddiv_rn(__dsub_rn(static_cast<double>(f[e]), static_cast<double>(lo)),
-                                                      static_cast<double>(s))));
-        }
-        c[e] = static_cast<uint32_t>(fminf(r, 15.0f));
+    for (int w = 1; w < W; ++w) {
+        top = bf16x2_max_nan(top, x[w]);
+        bottom = bf16x2_min_nan(bottom, x[w]);
+    }
+    bottom ^= 0x80008000u;
+    // (max, -min) of the lane: both halves against each other
+    uint32_t both = bf16x2_max_nan(__byte_perm(top, bottom, 0x5410), __byte_perm(top, bottom, 0x7632));
+#pragma unroll
+    for (int off = 1; off < LANES; off <<= 1) both = bf16x2_max_nan(both, __shfl_xor_sync(mask, both, off));
+    const float hi = __uint_as_float(both << 16);
+    const float lo = -__uint_as_float(both & 0xFFFF0000u);
+    packed = 0u;
+    if (!(fabsf(hi) < INFINITY && fabsf(lo) < INFINITY)) return 0x7FC00000u;   // s = 0, m = NaN
+    const float s32 = __fmul_rn(__fsub_rn(hi, lo), 0x1.111112p-4f);            // 1/15 and one rounding
+    const uint32_t u = __float_as_uint(s32);
+    uint32_t s16 = (u + 0x7FFFu + ((u >> 16) & 1u)) >> 16;
+    if (((u & 0xFFFFu) - 0x7FF8u) <= 16u || !(s32 >= 0x1p-100f && s32 <= 0x1p126f)) s16 = q4_scale_f64(lo, hi);
+    const float s = __uint_as_float(s16 << 16);
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(s));
+    constexpr float kMagic = 12582912.0f;                  // 1.5 * 2^23: adding it rounds to an integer
+    float c[2 * W], worst = 0.0f;
+#pragma unroll
+    for (int e = 0; e < 2 * W; ++e) {
+        const float f = __uint_as_float((e & 1) ? (x[e >> 1] & 0xFFFF0000u) : (x[e >> 1] << 16));
+        const float t = __fsub_rn(f, lo);
+        c[e] = __fsub_rn(__fmaf_rn(t, r, kMagic), kMagic);
+        worst = fmaxf(worst, fabsf(__fmaf_rn(t, r, -c[e])));
+    }
+    if (!(worst < 0.5f - 0x1p-10f && s >= 0x1p-100f && s32 < INFINITY)) {   // near a half, or s tiny, or t beyond fp32
+#pragma unroll
+        for (int e = 0; e < 2 * W; ++e)
+            c[e] = q4_code_f64(__uint_as_float((e & 1) ? (x[e >> 1] & 0xFFFF0000u) : (x[e >> 1] << 16)), lo, s);
+    }
+    // codes side by side, four at a time as an fp32 integer below 2^16
+#pragma unroll
+    for (int e = 0; e < 2 * W; e += 4) {
+        float v = fmaf(c[e + 1], 16.0f, c[e]);
+        if (2 * W >= e + 4) v = fmaf(fmaf(c[(e + 3) % (2 * W)], 16.0f, c[(e + 2) % (2 * W)]), 256.0f, v);
+        packed |= (__float_as_uint(v + 8388608.0f) & 0xFFFFu) << (4 * e);
     }
     // -0 and +0 compare equal, so the minimum of a group that holds both is either; it is kept as +0
     const uint32_t m16 = lo == 0.0f ? 0u : __float_as_uint(lo) >> 16;

@@ -260,15 +260,16 @@ _BF16 = (torch.bfloat16, torch.int16)          # bf16 values, or their bits
 
 
 def _want(t, name, shape, dtypes, device):
-    """t is a contiguous tensor of this shape, type and device; raises ValueError otherwise."""
+    """t is a contiguous tensor of this shape (a torch.Size), type and device; raises ValueError otherwise."""
+    if t.shape == shape and t.dtype in dtypes and t.is_contiguous() and t.device == device:
+        return
     if t.dtype not in dtypes:
         raise ValueError(f"{name}: type {t.dtype}, expected {' or '.join(map(str, dtypes))}")
     if tuple(t.shape) != tuple(shape):
         raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {tuple(shape)}")
     if t.device != device:
         raise ValueError(f"{name}: on {t.device}, expected {device}")
-    if not t.is_contiguous():
-        raise ValueError(f"{name}: not contiguous")
+    raise ValueError(f"{name}: not contiguous")
 
 
 class _OnDevice:
@@ -284,20 +285,22 @@ class _OnDevice:
             torch.cuda.current_stream().synchronize()      # zeroed whatever stream the calls run on
         self._flag = self.status_flag.data_ptr()
 
-    def _enqueue(self, name, args, stream):
-        """Calls the library with the device current; args already marshalled, the stream goes in at None."""
+    def _enqueue(self, name, args, stream, at):
+        """Calls the library with the device current; args are marshalled but for the stream, which goes in at `at`."""
         if torch.cuda.current_device() != self.device.index:
             with torch.cuda.device(self.device):
-                return self._enqueue(name, args, stream)
+                return self._enqueue(name, args, stream, at)
         if stream is None:
-            stream = torch.cuda.current_stream(self.device)
-        raw = stream if isinstance(stream, int) else stream.cuda_stream
-        status = getattr(ac.lib(), name)(*[raw if a is _STREAM else a for a in args])
+            args[at] = _raw_stream(self.device.index)
+        else:
+            args[at] = stream if isinstance(stream, int) else stream.cuda_stream
+        status = getattr(ac.lib(), name)(*args)
         if status != 0:
             raise ac.AcError(status, name)
 
 
-_STREAM = object()                             # stands for the stream in a list of arguments
+# the current stream's handle without the wrapper object (a microsecond per call)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda i: torch.cuda.current_stream(i).cuda_stream)
 
 
 class _Rows(_OnDevice):
@@ -364,7 +367,7 @@ class PagedAttention(_Rows):
         self._strides = (k_cache.stride(0), k_cache.stride(token), k_cache.stride(head))
         self._rows(block_table, context_lens, k_cache.shape[token], k_cache.shape[0], Hq, k_cache.shape[head],
                    k_cache.shape[3])
-        self._q_shape = (self.B, self.Hq, self.d)
+        self._q_shape = torch.Size((self.B, self.Hq, self.d))
         self.plan(lens_host, max_context_len, num_splits, row_order)
 
     def _choose(self, counts, span):
@@ -377,7 +380,7 @@ class PagedAttention(_Rows):
                       self.block_table.data_ptr(), self.max_pages_per_seq, self.context_lens.data_ptr(),
                       self.new_tokens, self.softmax_scale, self.num_splits, self.workspace.data_ptr(),
                       self.workspace_bytes, None, self.B, self.Hq, self.Hkv, self.d, self.page_size, self.num_pages,
-                      self.max_context_len, self._flag, _STREAM, self._options]
+                      self.max_context_len, self._flag, None, self._options]
 
     def attention(self, q, out=None, stream=None):
         """q: rotated queries [B, Hq, d] bf16; returns out [B, Hq, d] bf16 (allocated unless given)."""
@@ -386,8 +389,9 @@ class PagedAttention(_Rows):
             out = torch.empty_like(q)
         else:
             _want(out, "out", self._q_shape, _BF16, self.device)
-        self._args[0], self._args[14] = q.data_ptr(), out.data_ptr()
-        self._enqueue("ac_paged_decode_attn_ex", self._args, stream)
+        args = self._args.copy()
+        args[0], args[14] = q.data_ptr(), out.data_ptr()
+        self._enqueue("ac_paged_decode_attn_ex", args, stream, -2)
         return out
 
 
@@ -440,9 +444,9 @@ class Q4Cache(_OnDevice):
         _want(block_table, "block_table", (B, block_table.shape[-1]), (torch.int32,), self.device)
         if total == 0:
             return
-        self._enqueue(name, (k.data_ptr(), v.data_ptr(), self.struct, block_table.data_ptr(), block_table.shape[1],
+        self._enqueue(name, [k.data_ptr(), v.data_ptr(), self.struct, block_table.data_ptr(), block_table.shape[1],
                              start_pos.data_ptr(), row_offsets.data_ptr(), total, B, self.Hkv, self.d, self.page_size,
-                             self.num_pages, self._flag, _STREAM), stream)
+                             self.num_pages, self._flag, None], stream, -1)
 
     def store(self, k, v, block_table, start_pos, row_offsets, stream=None):
         """Quantises k, v (bf16 [tokens, Hkv, d], keys rotated): row b's tokens row_offsets[b] .. row_offsets[b+1] - 1
@@ -474,7 +478,7 @@ class Q4DecodeStep(_Rows):
         self.cache, self.window, self.sinks = cache, int(window), int(sinks)
         self.softmax_scale, self.new_tokens = float(softmax_scale), int(new_tokens)
         self._rows(block_table, context_lens, cache.page_size, cache.num_pages, Hq, cache.Hkv, cache.d)
-        self._q_shape, self._kv_shape = (self.B, self.Hq, self.d), (self.B, self.Hkv, self.d)
+        self._q_shape, self._kv_shape = (torch.Size((self.B, h, self.d)) for h in (self.Hq, self.Hkv))
         self.rope_cos, self.rope_sin = rope_cos, rope_sin
         variants = dict(rope_variants or {})
         self._norms = (variants.get("q_norm_weight"), variants.get("k_norm_weight"))      # kept alive
@@ -493,10 +497,10 @@ class Q4DecodeStep(_Rows):
         table = [self.cache.struct, self.block_table.data_ptr(), self.max_pages_per_seq, self.context_lens.data_ptr()]
         self._attn_args = [None, *table, self.new_tokens, self.softmax_scale, self.num_splits,
                            self.workspace.data_ptr(), self.workspace_bytes, None, *shape, self.max_context_len,
-                           self._flag, _STREAM, self._options]
+                           self._flag, None, self._options]
         if self.rope_cos is not None:
             self._append_args = [None, None, None, None, *table, self.rope_cos.data_ptr(), self.rope_sin.data_ptr(),
-                                 self.rope_cos.shape[0], *shape, self._flag, _STREAM, self._rope]
+                                 self.rope_cos.shape[0], *shape, self._flag, None, self._rope]
 
     def append(self, q_in, k_new, v_new, q_out=None, stream=None):
         """Rotates q_in [B, Hq, d] into q_out (allocated unless given, may be q_in) and writes k_new, v_new
@@ -510,8 +514,9 @@ class Q4DecodeStep(_Rows):
             q_out = torch.empty_like(q_in)
         elif q_out is not q_in:
             _want(q_out, "q_out", self._q_shape, _BF16, self.device)
-        self._append_args[:4] = q_in.data_ptr(), q_out.data_ptr(), k_new.data_ptr(), v_new.data_ptr()
-        self._enqueue("ac_rope_kv_append_q4", self._append_args, stream)
+        args = self._append_args.copy()
+        args[:4] = q_in.data_ptr(), q_out.data_ptr(), k_new.data_ptr(), v_new.data_ptr()
+        self._enqueue("ac_rope_kv_append_q4", args, stream, -2)
         return q_out
 
     def attention(self, q, out=None, stream=None):
@@ -521,8 +526,9 @@ class Q4DecodeStep(_Rows):
             out = torch.empty_like(q)
         else:
             _want(out, "out", self._q_shape, _BF16, self.device)
-        self._attn_args[0], self._attn_args[10] = q.data_ptr(), out.data_ptr()
-        self._enqueue("ac_paged_decode_attn_q4", self._attn_args, stream)
+        args = self._attn_args.copy()
+        args[0], args[10] = q.data_ptr(), out.data_ptr()
+        self._enqueue("ac_paged_decode_attn_q4", args, stream, -2)
         return out
 
     def step(self, q_in, k_new, v_new, q_rot=None, out=None, stream=None):
@@ -561,9 +567,9 @@ class CachePages(_OnDevice):
     def reserve(self, new_tokens, stream=None):
         """Pages for new_tokens more tokens of every active row, lowest free page first, rows in order."""
         self._enqueue("ac_cache_reserve",
-                      (self.block_table.data_ptr(), self.max_pages_per_seq, self.context_lens.data_ptr(),
+                      [self.block_table.data_ptr(), self.max_pages_per_seq, self.context_lens.data_ptr(),
                        self.ref_counts.data_ptr(), int(new_tokens), self.rows, self.page_size, self.num_pages,
-                       *self._room, self._flag, _STREAM), stream)
+                       *self._room, self._flag, None], stream, -1)
 
     def fork(self, pairs, stream=None):
         """pairs: int32 [n, 2] (parent row, child row); at most as many as the table has rows."""
@@ -574,9 +580,9 @@ class CachePages(_OnDevice):
         if n == 0:
             return
         self._enqueue("ac_cache_fork",
-                      (self._pools, len(self.pools), self.block_table.data_ptr(), self.max_pages_per_seq,
+                      [self._pools, len(self.pools), self.block_table.data_ptr(), self.max_pages_per_seq,
                        self.context_lens.data_ptr(), self.ref_counts.data_ptr(), pairs.data_ptr(), n, self.rows,
-                       self.page_size, self.num_pages, *self._room, self._flag, _STREAM), stream)
+                       self.page_size, self.num_pages, *self._room, self._flag, None], stream, -1)
 
     def release(self, row_list, stream=None):
         """row_list: int32 [n]; unused and repeated rows are no-ops."""
@@ -585,9 +591,9 @@ class CachePages(_OnDevice):
         if n == 0:
             return
         self._enqueue("ac_cache_release",
-                      (self.block_table.data_ptr(), self.max_pages_per_seq, self.context_lens.data_ptr(),
+                      [self.block_table.data_ptr(), self.max_pages_per_seq, self.context_lens.data_ptr(),
                        self.ref_counts.data_ptr(), row_list.data_ptr(), n, self.rows, self.page_size, self.num_pages,
-                       self._flag, _STREAM), stream)
+                       self._flag, None], stream, -1)
 
     def copy(self, pairs, stream=None):
         """Copies whole pages: pairs int32 [n, 2] (source, destination)."""
@@ -595,8 +601,8 @@ class CachePages(_OnDevice):
         _want(pairs, "pairs", (n, 2), (torch.int32,), self.device)
         if n == 0 or not self.pools:
             return
-        self._enqueue("ac_cache_copy_pages", (self._pools, len(self.pools), pairs.data_ptr(), n, self.num_pages,
-                                              self._flag, _STREAM), stream)
+        self._enqueue("ac_cache_copy_pages", [self._pools, len(self.pools), pairs.data_ptr(), n, self.num_pages,
+                                              self._flag, None], stream, -1)
 
     def compact(self, table_out=None, refs_out=None, live_out=None, stream=None):
         """Moves the live pages to the lowest ids.  In place, or (both given) into another table and counts, so that
@@ -610,8 +616,8 @@ class CachePages(_OnDevice):
         if live_out is not None:
             _want(live_out, "live_out", (1,), (torch.int32,), self.device)
         self._enqueue("ac_cache_compact",
-                      (self._pools, len(self.pools), self.block_table.data_ptr(), table_out.data_ptr(),
+                      [self._pools, len(self.pools), self.block_table.data_ptr(), table_out.data_ptr(),
                        self.max_pages_per_seq, self.context_lens.data_ptr(), self.ref_counts.data_ptr(),
                        refs_out.data_ptr(), self.rows, self.page_size, self.num_pages,
-                       live_out.data_ptr() if live_out is not None else None, *self._room, self._flag, _STREAM),
-                      stream)
+                       live_out.data_ptr() if live_out is not None else None, *self._room, self._flag, None],
+                      stream, -1)

@@ -170,6 +170,34 @@ def test_store_and_load(rt, d, group, layout, total_heads, ps, lens):
         assert (np.abs(got - want)[~np.isnan(want)] <= (2.0**-8 * (1 + 2.0**-8) * np.abs(want) + 2.0**-134)[~np.isnan(want)]).all()
 
 
+@pytest.mark.parametrize("d,group", [(128, 64), (64, 32), (128, 128)])
+@pytest.mark.parametrize("kind", ["normal", "ranges", "integers", "offset"])
+def test_store_decides_every_code_as_the_definition_does(rt, d, group, kind):
+    # many vectors: of every magnitude, of small integers (many quotients at a half), far from zero (few codes apart)
+    import torch
+    rng = np.random.default_rng(11)
+    T, H, ps = 3000, 4, 64
+    x = rng.standard_normal((T, H, d))
+    if kind == "ranges":
+        x = np.ldexp(x, rng.integers(-140, 127, (T, H, 1)))
+    elif kind == "integers":
+        x = np.rint(x * rng.integers(1, 40, (T, H, 1))) * np.ldexp(1.0, rng.integers(-20, 20, (T, H, 1)))
+    elif kind == "offset":
+        x = x + rng.integers(-200, 200, (T, H, 1))
+    x = O.f64_to_bf16_rne(x)
+    cache = rt.Q4Cache.empty(T // ps + 1, ps, H, d, group)
+    table = np.arange(T // ps + 1, dtype=np.int32)[None]
+    cache.store(dev(x), dev(x), dev(table), dev(np.zeros(1, np.int32)), dev(np.array([0, T], np.int32)))
+    torch.cuda.synchronize()
+    codes, s, m = Q.quantise(x, group)
+    for side, pool in enumerate((cache.k_codes, cache.v_codes)):
+        got = Q.unpack(host(pool).reshape(-1, H, d // 2)[:T])
+        at = np.argwhere(got != codes)
+        assert not len(at), (len(at), at[:3].tolist(), got[tuple(at[0])], codes[tuple(at[0])])
+        p = host(cache.params)[:, :, :, side].transpose(0, 2, 1, 3, 4).reshape(-1, H, d // group, 2)[:T]
+        assert np.array_equal(p[..., 0], s) and np.array_equal(p[..., 1], m)
+
+
 def test_store_beyond_the_table_and_bad_pages(rt):
     import torch
     from paper_2606_07665_b200 import binding as ac
