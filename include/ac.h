@@ -497,7 +497,7 @@ int ac_kv_store_q4(const void* k, const void* v, const ac_q4_cache* cache, const
                    int total_tokens, int B, int Hkv, int d, int page_size, int num_pages,
                    int32_t* status_flag, void* stream);
 
-/* The reverse: reads the same tokens back as bf16(fp32(c * s + m)) into dense k, v [total_tokens, Hkv, d].
+/* The reverse: reads the same tokens back as bf16(c * s + m), rounded once, into dense k, v [total_tokens, Hkv, d].
  * Tokens of inactive rows, at or past row_offsets[B], or out of range (status bits set) read as +0. */
 int ac_kv_load_q4(void* k, void* v, const ac_q4_cache* cache, const int32_t* block_table,
                   int max_pages_per_seq, const int32_t* start_pos, const int32_t* row_offsets,

@@ -89,17 +89,21 @@ __global__ void __launch_bounds__(128) rope_kv_append_q4_kernel(
 // Bound: HBM, 2 dense and 0.56 packed bytes per element at group 64.
 constexpr int kTokens = 32;
 constexpr int kStoreThreads = 256;                         // workers; one more warp looks up
-constexpr int kStoreCtas = 3;                              // per SM
-constexpr int kInHand = 4;
-
-struct TokenSlot {
-    int page;             // -1: no slot
-    int slot;
+template <bool STORE>
+struct Bulk {
+    static constexpr int kCtas = STORE ? 3 : 4;            // per SM
+    static constexpr int kInHand = STORE ? 4 : 8;          // a packed vector is a quarter of a dense one
 };
 
-__device__ __forceinline__ TokenSlot find_slot(long long token, const int32_t* block_table, int max_pages_per_seq,
-                                               const int32_t* start_pos, const int32_t* row_offsets, int B,
-                                               int page_size, int num_pages, int32_t* status_flag) {
+struct TokenSlot {
+    int64_t code;         // byte offset of the token's slot in the code pools; -1: no slot
+    int64_t param;        // word offset of head 0's parameters
+};
+
+__device__ __forceinline__ TokenSlot find_slot(long long token, const Q4View& cache, int words, const int32_t* block_table,
+                                               int max_pages_per_seq, const int32_t* start_pos,
+                                               const int32_t* row_offsets, int B, int Hkv, int page_size, int num_pages,
+                                               int32_t* status_flag) {
     TokenSlot r{-1, 0};
     if (token >= row_offsets[B]) return r;
     int lo = 0, hi = B;                                    // the last row whose offset is <= token
@@ -120,19 +124,22 @@ __device__ __forceinline__ TokenSlot find_slot(long long token, const int32_t* b
         if (status_flag != nullptr) atomicOr(status_flag, AC_FLAG_PAGE_OOB);
         return r;
     }
-    r.page = page;
-    r.slot = static_cast<int>(pos - idx * page_size);
+    const int slot = static_cast<int>(pos - idx * page_size);
+    r.code = page * cache.stride_page + slot * cache.stride_token;
+    r.param = (static_cast<int64_t>(page) * Hkv * page_size + slot) * words;
     return r;
 }
 
-template <int D, int G, bool STORE>
-__global__ void __launch_bounds__(kStoreThreads + 32, kStoreCtas) kv_bulk_q4_kernel(
+// FIXED: a pass of the CTA is a whole number of tokens (the number of heads divides it), so a lane keeps its head.
+template <int D, int G, bool STORE, bool FIXED>
+__global__ void __launch_bounds__(kStoreThreads + 32, Bulk<STORE>::kCtas) kv_bulk_q4_kernel(
     uint16_t* k, uint16_t* v, const Q4View cache, const int32_t* __restrict__ block_table, int max_pages_per_seq,
     const int32_t* __restrict__ start_pos, const int32_t* __restrict__ row_offsets, int total_tokens, int B, int Hkv,
     int page_size, int num_pages, int32_t* status_flag) {
     constexpr int LPV = D / 8;                             // lanes per vector
     constexpr int VECS = kStoreThreads / LPV;              // vectors per pass of the CTA
     constexpr int LANES = LPV / G;                         // lanes per group
+    constexpr int kInHand = Bulk<STORE>::kInHand;
     __shared__ TokenSlot s_slot[2][kTokens];
     const int blocks = static_cast<int>((static_cast<long long>(total_tokens) + kTokens - 1) / kTokens);
     const bool lookup = threadIdx.x >= kStoreThreads;
@@ -141,7 +148,8 @@ __global__ void __launch_bounds__(kStoreThreads + 32, kStoreCtas) kv_bulk_q4_ker
         const long long token = static_cast<long long>(block) * kTokens + lane;
         TokenSlot r{-1, 0};
         if (token < total_tokens)
-            r = find_slot(token, block_table, max_pages_per_seq, start_pos, row_offsets, B, page_size, num_pages, status_flag);
+            r = find_slot(token, cache, 2 * G, block_table, max_pages_per_seq, start_pos, row_offsets, B, Hkv, page_size,
+                          num_pages, status_flag);
         s_slot[buffer][lane] = r;
     };
     if (lookup && static_cast<int>(blockIdx.x) < blocks) look_up(blockIdx.x, 0);
@@ -152,6 +160,8 @@ __global__ void __launch_bounds__(kStoreThreads + 32, kStoreCtas) kv_bulk_q4_ker
     // (token, head) of a lane's vectors is stepped instead of divided
     const int first_t = (threadIdx.x / LPV) / Hkv, first_h = threadIdx.x / LPV - first_t * Hkv;
     const int step_t = VECS / Hkv, step_h = VECS - step_t * Hkv;
+    const int64_t head_words = static_cast<int64_t>(page_size) * 2 * G;    // parameters of a page and head
+    const int64_t first_code = first_h * cache.stride_head, first_param = first_h * head_words;
     int buffer = 0;
     for (int block = blockIdx.x; block < blocks; block += gridDim.x, buffer ^= 1) {
         if (lookup) {
@@ -163,11 +173,12 @@ __global__ void __launch_bounds__(kStoreThreads + 32, kStoreCtas) kv_bulk_q4_ker
         const int tokens = total_tokens - t0 < kTokens ? static_cast<int>(total_tokens - t0) : kTokens;
         const int vecs = tokens * Hkv;                     // (token, head), head fastest: dense order
         for (int side = 0; side < 2; ++side) {
-            uint16_t* const dense = (side ? v : k) + t0 * Hkv * D + sub * 8;
-            uint8_t* const codes = (side ? cache.v_codes : cache.k_codes) + sub * 4;
-            uint32_t* const params = cache.params + side * G + sub / LANES;
+            uint16_t* dense = (side ? v : k) + (t0 * Hkv + threadIdx.x / LPV) * D + sub * 8;
+            uint8_t* const codes = (side ? cache.v_codes : cache.k_codes) + sub * 4 + first_code;
+            uint32_t* const params = cache.params + side * G + sub / LANES + first_param;
             int t = first_t, h = first_h;
-            for (int i = threadIdx.x / LPV; i < vecs; i += kInHand * VECS) {
+            int64_t code_step = 0, param_step = 0;         // from the first head to head h
+            for (int i = threadIdx.x / LPV; i < vecs; i += kInHand * VECS, dense += kInHand * VECS * D) {
                 bool live[kInHand];
                 uint8_t* code_at[kInHand];
                 uint32_t* param_at[kInHand];
@@ -177,23 +188,24 @@ __global__ void __launch_bounds__(kStoreThreads + 32, kStoreCtas) kv_bulk_q4_ker
                 for (int u = 0; u < kInHand; ++u) {
                     const bool on = i + u * VECS < vecs;
                     const TokenSlot at = s_slot[buffer][on ? t : 0];
-                    live[u] = on && at.page >= 0;
-                    const int64_t pg = live[u] ? at.page : 0;
-                    const int slot = live[u] ? at.slot : 0;
-                    const int hh = live[u] ? h : 0;
-                    code_at[u] = codes + pg * cache.stride_page + slot * cache.stride_token + hh * cache.stride_head;
-                    param_at[u] = params + ((pg * Hkv + hh) * page_size + slot) * (2 * G);
+                    live[u] = on && at.code >= 0;
+                    code_at[u] = codes + (at.code + code_step);
+                    param_at[u] = params + (at.param + param_step);
                     if (STORE) {
-                        if (live[u]) raw[u] = __ldcs(reinterpret_cast<const uint4*>(dense + static_cast<int64_t>(i + u * VECS) * D));
+                        if (live[u]) raw[u] = __ldcs(reinterpret_cast<const uint4*>(dense + u * VECS * D));
                     } else if (live[u]) {
                         word[u] = *reinterpret_cast<const uint32_t*>(code_at[u]);
                         sm[u] = *param_at[u];
                     }
                     t += step_t;
-                    h += step_h;
-                    if (h >= Hkv) {
-                        h -= Hkv;
-                        ++t;
+                    if (!FIXED) {
+                        h += step_h;
+                        if (h >= Hkv) {
+                            h -= Hkv;
+                            ++t;
+                        }
+                        code_step = (h - first_h) * cache.stride_head;
+                        param_step = (h - first_h) * head_words;
                     }
                 }
 #pragma unroll
@@ -207,16 +219,8 @@ __global__ void __launch_bounds__(kStoreThreads + 32, kStoreCtas) kv_bulk_q4_ker
                         if (sub % LANES == 0) *param_at[u] = p;
                     } else if (i + u * VECS < vecs) {
                         uint4 o = make_uint4(0u, 0u, 0u, 0u);
-                        if (live[u]) {
-                            const float s = __uint_as_float(sm[u] << 16), m = __uint_as_float(sm[u] & 0xFFFF0000u);
-                            float y[8];
-#pragma unroll
-                            for (int e = 0; e < 8; ++e)    // 2^23 + c, whose low bits are the code, minus 2^23
-                                y[e] = fmaf(__uint_as_float(((word[u] >> (4 * e)) & 15u) | 0x4B000000u) - 8388608.0f, s, m);
-                            o = make_uint4(pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3]), pack_bf16x2(y[4], y[5]),
-                                           pack_bf16x2(y[6], y[7]));
-                        }
-                        __stcs(reinterpret_cast<uint4*>(dense + static_cast<int64_t>(i + u * VECS) * D), o);
+                        if (live[u]) o = q4_values(word[u], sm[u]);
+                        __stcs(reinterpret_cast<uint4*>(dense + u * VECS * D), o);
                     }
                 }
             }
@@ -233,17 +237,21 @@ cudaError_t launch_bulk(void* k, void* v, const Q4View& cache, const int32_t* bl
     // Ordinary launches: what follows them in the stream may read the cache before its own synchronisation, which
     // is safe only behind kernels that do not signal early.
     const long long blocks = (static_cast<long long>(total_tokens) + kTokens - 1) / kTokens;
-    const unsigned grid = static_cast<unsigned>(blocks < kStoreCtas * sms ? blocks : kStoreCtas * sms);
+    const int ctas = (store ? Bulk<true>::kCtas : Bulk<false>::kCtas) * sms;
+    const unsigned grid = static_cast<unsigned>(blocks < ctas ? blocks : ctas);
     uint16_t* kk = static_cast<uint16_t*>(k);
     uint16_t* vv = static_cast<uint16_t*>(v);
-    if (store)
-        kv_bulk_q4_kernel<D, G, true><<<grid, kStoreThreads + 32, 0, stream>>>(
-            kk, vv, cache, block_table, max_pages_per_seq, start_pos, row_offsets, total_tokens, B, Hkv, page_size,
-            num_pages, status_flag);
-    else
-        kv_bulk_q4_kernel<D, G, false><<<grid, kStoreThreads + 32, 0, stream>>>(
-            kk, vv, cache, block_table, max_pages_per_seq, start_pos, row_offsets, total_tokens, B, Hkv, page_size,
-            num_pages, status_flag);
+#define AC_Q4_BULK_LAUNCH(STORE_, FIXED_)                                                                            \
+    kv_bulk_q4_kernel<D, G, STORE_, FIXED_><<<grid, kStoreThreads + 32, 0, stream>>>(                                \
+        kk, vv, cache, block_table, max_pages_per_seq, start_pos, row_offsets, total_tokens, B, Hkv, page_size,       \
+        num_pages, status_flag)
+    const bool fixed = kStoreThreads / (D / 8) % Hkv == 0;
+    if (store) {
+        if (fixed) AC_Q4_BULK_LAUNCH(true, true); else AC_Q4_BULK_LAUNCH(true, false);
+    } else {
+        if (fixed) AC_Q4_BULK_LAUNCH(false, true); else AC_Q4_BULK_LAUNCH(false, false);
+    }
+#undef AC_Q4_BULK_LAUNCH
     return cudaGetLastError();
 }
 

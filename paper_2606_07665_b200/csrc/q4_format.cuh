@@ -40,9 +40,11 @@ __device__ __noinline__ inline float q4_code_f64(float x, float lo, float s) {
 //   scale  s32 = fl(fl(max - min) / 15) is within 2^-22 relative (four of its own ulps) of the quotient, so the bf16
 //          next to it is the right one unless the 16 bits cut off lie within 8 of the tie; tiny and overflowing
 //          ranges are left to fp64;
-//   codes  with t = fl(x - m) and r the approximate reciprocal of s, t * r is within 2^-21 relative of the
-//          quotient, so below 16 within 8e-6: the integer nearest to it is the right code unless it is within
-//          2^-10 of a half (checked on the exact residual fma(t, r, -code)), or s is subnormal.
+//   codes  t = fl(x - m) times the approximate reciprocal of s gives a candidate c; d = t - c s (one fma, so exact up to
+//          t's own 2^-24 of 15 s) decides: c is right where |d| is below s / 2 by 2^-15 relative.  Halves are common (s has
+//          eight bits: about one element in 300), so they are resolved in fp32 too where t is exact, which makes d exact:
+//          beyond s / 2 the neighbour is nearer, at s / 2 the even one of the two counts.  fp64 is left for an inexact t
+//          and for tiny or overflowing ranges.
 template <int W, int LANES>
 __device__ __forceinline__ uint32_t q4_quantise(const uint32_t (&x)[W], uint32_t& packed, uint32_t mask) {
     uint32_t top = x[0], bottom = x[0];
@@ -68,26 +70,42 @@ __device__ __forceinline__ uint32_t q4_quantise(const uint32_t (&x)[W], uint32_t
     float r;
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(s));
     constexpr float kMagic = 12582912.0f;                  // 1.5 * 2^23: adding it rounds to an integer
-    float c[2 * W], worst = 0.0f;
+    const float half = 0.5f * s;
+    float c[2 * W], d[2 * W], worst = 0.0f;                // c: code + kMagic
 #pragma unroll
     for (int e = 0; e < 2 * W; ++e) {
         const float f = __uint_as_float((e & 1) ? (x[e >> 1] & 0xFFFF0000u) : (x[e >> 1] << 16));
         const float t = __fsub_rn(f, lo);
-        c[e] = __fsub_rn(__fmaf_rn(t, r, kMagic), kMagic);
-        worst = fmaxf(worst, fabsf(__fmaf_rn(t, r, -c[e])));
+        c[e] = __fmaf_rn(t, r, kMagic);
+        d[e] = __fmaf_rn(__fsub_rn(kMagic, c[e]), s, t);
+        worst = fmaxf(worst, fabsf(d[e]));
     }
-    if (!(worst < 0.5f - 0x1p-10f && s >= 0x1p-100f && s32 < INFINITY)) {   // near a half, or s tiny, or t beyond fp32
+    const float near = half * (1.0f - 0x1p-15f);
+    bool exact = s >= 0x1p-100f && s32 < INFINITY;
+    if (!(worst < near && exact)) {
 #pragma unroll
-        for (int e = 0; e < 2 * W; ++e)
-            c[e] = q4_code_f64(__uint_as_float((e & 1) ? (x[e >> 1] & 0xFFFF0000u) : (x[e >> 1] << 16)), lo, s);
-    }
-    // codes side by side, four at a time as an fp32 integer below 2^16
+        for (int e = 0; e < 2 * W; ++e) {
+            if (fabsf(d[e]) < near) continue;              // seldom more than one of them
+            const float f = __uint_as_float((e & 1) ? (x[e >> 1] & 0xFFFF0000u) : (x[e >> 1] << 16));
+            const float t = __fsub_rn(f, lo), back = __fsub_rn(t, f);       // TwoSum: what t lost
+            exact = exact && __fadd_rn(__fsub_rn(f, __fsub_rn(t, back)), __fsub_rn(-lo, back)) == 0.0f;
+            const bool odd = __float_as_uint(c[e]) & 1u;
+            if (fabsf(d[e]) > half || (fabsf(d[e]) == half && odd)) c[e] += d[e] > 0.0f ? 1.0f : -1.0f;
+        }
+        if (!exact) {
 #pragma unroll
-    for (int e = 0; e < 2 * W; e += 4) {
-        float v = fmaf(c[e + 1], 16.0f, c[e]);
-        if (2 * W >= e + 4) v = fmaf(fmaf(c[(e + 3) % (2 * W)], 16.0f, c[(e + 2) % (2 * W)]), 256.0f, v);
-        packed |= (__float_as_uint(v + 8388608.0f) & 0xFFFFu) << (4 * e);
+            for (int e = 0; e < 2 * W; ++e)
+                c[e] = kMagic + q4_code_f64(__uint_as_float((e & 1) ? (x[e >> 1] & 0xFFFF0000u) : (x[e >> 1] << 16)), lo, s);
+        }
     }
+    // Codes side by side: the bits of c are those of kMagic plus the code, whose multiples come off at the end.
+    uint32_t sum = 0u, magics = 0u;
+#pragma unroll
+    for (int e = 0; e < 2 * W; ++e) {
+        sum += __float_as_uint(c[e]) << (4 * e);
+        magics += 0x4B400000u << (4 * e);
+    }
+    packed = sum - magics;
     // -0 and +0 compare equal, so the minimum of a group that holds both is either; it is kept as +0
     const uint32_t m16 = lo == 0.0f ? 0u : __float_as_uint(lo) >> 16;
     return s16 | (m16 << 16);
@@ -106,6 +124,22 @@ __device__ __forceinline__ uint32_t q4_tile_offset(int row, int chunk) {
     }
     const int line = row >> 2;
     return line * 128 + ((((row & 3) * 2 + chunk) ^ ((line & 1) * 3)) << 4);
+}
+
+// Eight codes -> eight bf16 values c s + m, each rounded once (a bf16 fma), in order: sm = (s, m).  A nibble under the
+// exponent of 128 is 128 + c, exact in bf16.
+__device__ __forceinline__ uint4 q4_values(uint32_t codes, uint32_t sm) {
+    const uint32_t s2 = __byte_perm(sm, sm, 0x1010), m2 = __byte_perm(sm, sm, 0x3232);
+    uint32_t y[4];                                         // elements (i, i + 4)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t c128 = ((codes >> (4 * i)) & 0x000F000Fu) | 0x43004300u;
+        uint32_t c;
+        asm("add.rn.bf16x2 %0, %1, %2;" : "=r"(c) : "r"(c128), "r"(0xC300C300u));     // - 128
+        asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(y[i]) : "r"(c), "r"(s2), "r"(m2));
+    }
+    return make_uint4(__byte_perm(y[0], y[1], 0x5410), __byte_perm(y[2], y[3], 0x5410),
+                      __byte_perm(y[0], y[1], 0x7632), __byte_perm(y[2], y[3], 0x7632));
 }
 
 // cp.async of 16 bytes with zero fill: copies src_bytes (16 or 0) and clears the rest.

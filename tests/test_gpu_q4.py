@@ -166,7 +166,7 @@ def test_store_and_load(rt, d, group, layout, total_heads, ps, lens):
     for got, want in ((kb, want_k), (vb, want_v)):
         got = f64(got)
         assert np.array_equal(np.isnan(got), np.isnan(want))
-        # one fp32 and one bf16 rounding (half a bf16 subnormal step at the bottom)
+        # one bf16 rounding (half a bf16 subnormal step at the bottom)
         assert (np.abs(got - want)[~np.isnan(want)] <= (2.0**-8 * (1 + 2.0**-8) * np.abs(want) + 2.0**-134)[~np.isnan(want)]).all()
 
 
