@@ -165,16 +165,16 @@ __global__ void __launch_bounds__(NW * 32, CTAS) paged_decode_attn_q4_kernel(con
         const int idx = locate(j0, sub);
         return idx >= 0 ? bt_row[idx] : -1;
     };
-    int64_t gr_off = 0;                            // byte offset of this lane's granule in the code pools
-    int gr_param = 0;                              // its index among the parameter granules
+    uint32_t gr_off = 0;                           // this lane's granule in the code pools, in units of 16 bytes
+    uint32_t gr_param = 0;                         // its index among the parameter granules
     uint32_t gr_ok = 0;                            // bit per lane: the granule has a page (otherwise it reads as zeros)
     auto settle_pages = [&](int j0, int page) {
         int sub;
         locate(j0, sub);
         const bool on = page >= 0 && page < p.num_pages;
         gr_ok = __ballot_sync(0xffffffffu, on);
-        gr_off = on ? static_cast<int64_t>(page) * p.cache.stride_page + sub * GRAN * p.cache.stride_token : 0;
-        gr_param = on ? static_cast<int>((static_cast<int64_t>(page) * p.Hkv + h) * p.gpp) + sub : 0;
+        gr_off = on ? static_cast<uint32_t>((page * p.cache.stride_page + sub * GRAN * p.cache.stride_token) >> 4) : 0u;
+        gr_param = on ? (static_cast<uint32_t>(page) * p.Hkv + h) * p.gpp + sub : 0u;
     };
 
     // This lane's share of a granule: row lane / CPR (and 8 further at D = 128), chunk lane % CPR.
@@ -184,34 +184,41 @@ __global__ void __launch_bounds__(NW * 32, CTAS) paged_decode_attn_q4_kernel(con
     const uint8_t* const k_lane = p.cache.k_codes + lane_off;
     const uint8_t* const v_lane = p.cache.v_codes + lane_off;
     const int64_t next_rows = static_cast<int64_t>(RPI) * p.cache.stride_token;
+    const uint8_t* const k_lane8 = k_lane + next_rows;      // the second pass at D = 128
+    const uint8_t* const v_lane8 = v_lane + next_rows;
     const uint32_t ring = smem_addr(smem) + warp * L::RING_BYTES;
     const uint32_t code_dst = ring + q4_tile_offset<RB>(lane / CPR, lane % CPR);
     constexpr int PC = GRAN * PB / 16;             // parameter chunks per granule: 8, 16 or 32
+    const uint8_t* const p_lane = reinterpret_cast<const uint8_t*>(p.cache.params) + lane % PC * 16;
+    // Each address is one widening multiply-add on a lane's base pointer (the FMA pipe: the integer pipe is the
+    // busy one here).
     auto issue = [&](int j, uint32_t stage) {      // stage = byte offset of the stage in the ring
         const int src = 2 * (j & 15);
+        const uint32_t ok = (gr_ok >> src) & 3u;
+        auto load = [&](auto copy) {
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            const int64_t off = __shfl_sync(0xffffffffu, gr_off, src + half);
-            const int bytes = (gr_ok >> (src + half)) & 1u ? 16 : 0;
+            for (int half = 0; half < 2; ++half) {
+                const uint64_t off = static_cast<uint64_t>(__shfl_sync(0xffffffffu, gr_off, src + half)) * 16u;
+                const bool on = (ok >> half) & 1u;
 #pragma unroll
-            for (int i = 0; i < GRAN / RPI; ++i) {
-                const uint32_t dst = code_dst + stage + (half * GRAN + i * RPI) * RB;   // whole lines: same swizzle
-                const int64_t o = off + (i ? next_rows : 0);
-                cp_async_16(dst, k_lane + o, bytes, policy);
-                cp_async_16(dst + L::K_BYTES, v_lane + o, bytes, policy);
+                for (int i = 0; i < GRAN / RPI; ++i) {
+                    const uint32_t dst = code_dst + stage + (half * GRAN + i * RPI) * RB;   // whole lines: same swizzle
+                    copy(dst, (i ? k_lane8 : k_lane) + off, on);
+                    copy(dst + L::K_BYTES, (i ? v_lane8 : v_lane) + off, on);
+                }
             }
-        }
 #pragma unroll
-        for (int i = 0; i < (2 * PC + 31) / 32; ++i) {
-            const int c = i * 32 + lane;
-            const int half = (c / PC) & 1;
-            const int granule = __shfl_sync(0xffffffffu, gr_param, src + half);
-            if (2 * PC >= 32 || c < 2 * PC)
-                cp_async_16(ring + stage + 2 * L::K_BYTES + c * 16,
-                            reinterpret_cast<const uint8_t*>(p.cache.params) +
-                                static_cast<int64_t>(granule) * (GRAN * PB) + (c - half * PC) * 16,
-                            (gr_ok >> (src + half)) & 1u ? 16 : 0, policy);
-        }
+            for (int i = 0; i < (2 * PC + 31) / 32; ++i) {
+                const int c = i * 32 + lane;
+                const int half = (c / PC) & 1;
+                const uint32_t granule = __shfl_sync(0xffffffffu, gr_param, src + half);
+                if (2 * PC >= 32 || c < 2 * PC)
+                    copy(ring + stage + 2 * L::K_BYTES + c * 16, p_lane + static_cast<uint64_t>(granule) * (GRAN * PB),
+                         (ok >> half) & 1u);
+            }
+        };
+        if (ok == 3u) load([&](uint32_t dst, const uint8_t* from, bool) { cp_async_16(dst, from, policy); });
+        else load([&](uint32_t dst, const uint8_t* from, bool on) { cp_async_16_or_zero(dst, from, on, policy); });
     };
 
     // ---- prologue: fill the ring; tiles that hold slot ctx - 1 or later wait for the preceding kernel ---------
@@ -313,6 +320,9 @@ __global__ void __launch_bounds__(NW * 32, CTAS) paged_decode_attn_q4_kernel(con
     // 3 of the next.
     const uint32_t mat_off = q4_tile_offset<RB>(((lane >> 3) & 1) * 8 + (lane & 7), lane >> 4);
 
+    // tiles before j_hole may hold masked tokens of the hole, those from j_tail on may lie past the end
+    const int j_hole = hole_hi > tok_begin ? ((hole_hi - tok_begin + TILE - 1) / TILE - warp + WARPS - 1) / WARPS : 0;
+    const int j_tail = (tok_end - tok_begin) % TILE != 0 ? n_my - 1 : n_my;
     uint32_t stage = 0;
     for (int j = 0; j < n_my; ++j) {
         cp_async_wait<STAGES - 1>();
@@ -321,10 +331,9 @@ __global__ void __launch_bounds__(NW * 32, CTAS) paged_decode_attn_q4_kernel(con
         const uint8_t* pt = smem + warp * L::RING_BYTES + stage + 2 * L::K_BYTES;
 
         // Which of the tile's tokens count: those before the end, and not between the sinks and the window.
-        const int r0 = range0(j);
         uint32_t valid = 0xffffffffu;
-        if (r0 + TILE > tok_end || (r0 < hole_hi && r0 + TILE > hole_lo)) {
-            const int r = r0 + lane;
+        if (j >= j_tail || j < j_hole) {
+            const int r = range0(j) + lane;
             valid = __ballot_sync(0xffffffffu, r < tok_end && !(r >= hole_lo && r < hole_hi));
         }
 
@@ -395,13 +404,13 @@ __global__ void __launch_bounds__(NW * 32, CTAS) paged_decode_attn_q4_kernel(con
                         for (int gq = 0; gq < G; ++gq) pr[sb][r][G + gq] = 0u;
                     }
         }
+        // the largest V scale of the tile: each lane looks at one token
+        uint32_t own[G];
+        load_words(own, pt + lane * PB + 4 * G);
         float v_max = 0.0f;
 #pragma unroll
-        for (int sb = 0; sb < 2; ++sb)
-#pragma unroll
-            for (int r = 0; r < 2; ++r)
-#pragma unroll
-                for (int gq = 0; gq < G; ++gq) v_max = fmaxf(v_max, __uint_as_float(pr[sb][r][G + gq] << 16));
+        for (int gq = 0; gq < G; ++gq) v_max = fmaxf(v_max, __uint_as_float(own[gq] << 16));
+        if (!((valid >> lane) & 1u)) v_max = 0.0f;
         bool move = v_max * vf >= 128.0f;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
@@ -412,8 +421,9 @@ __global__ void __launch_bounds__(NW * 32, CTAS) paged_decode_attn_q4_kernel(con
             }
         if (__any_sync(0xffffffffu, move)) {
 #pragma unroll
-            for (int off = 4; off < 32; off <<= 1) {
+            for (int off = 1; off < 32; off <<= 1) {
                 v_max = fmaxf(v_max, __shfl_xor_sync(0xffffffffu, v_max, off));
+                if (off < 4) continue;             // lanes (g, t) of one t hold the same heads
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll

@@ -142,10 +142,14 @@ __device__ __forceinline__ uint4 q4_values(uint32_t codes, uint32_t sm) {
                       __byte_perm(y[0], y[1], 0x7632), __byte_perm(y[2], y[3], 0x7632));
 }
 
-// cp.async of 16 bytes with zero fill: copies src_bytes (16 or 0) and clears the rest.
-__device__ __forceinline__ void cp_async_16(uint32_t dst, const void* src, int src_bytes, uint64_t policy) {
+// cp.async of 16 bytes; the second form clears the destination instead where `on` is false.
+__device__ __forceinline__ void cp_async_16(uint32_t dst, const void* src, uint64_t policy) {
+    asm volatile("cp.async.cg.shared.global.L2::cache_hint [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "l"(policy)
+                 : "memory");
+}
+__device__ __forceinline__ void cp_async_16_or_zero(uint32_t dst, const void* src, bool on, uint64_t policy) {
     asm volatile("cp.async.cg.shared.global.L2::cache_hint [%0], [%1], 16, %2, %3;" ::"r"(dst), "l"(src),
-                 "r"(src_bytes), "l"(policy)
+                 "r"(on ? 16 : 0), "l"(policy)
                  : "memory");
 }
 __device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
