@@ -986,18 +986,55 @@ int ac_decode_plan_q4(const int32_t* token_counts_host, int B, int Hq, int Hkv, 
     if (st != AC_OK) return st;
     if (max_context_len <= 0) return AC_ERR_SHAPE;
     if (sm_count <= 0) sm_count = g_last_sm_count > 0 ? g_last_sm_count : 148;
-    long long tokens = static_cast<long long>(B) * max_context_len;
+    // Every split count is priced by what the launch it gives (q4_attn.cu) was measured to do: the whole GPU moves
+    // 5.6 TB/s of this cache (its arithmetic keeps it below HBM's rate), one CTA alone on its SM 43 GB/s with twelve warps
+    // and 32 with six, two sharing an SM 19 each, in a ragged batch 25; a wave costs 4 us of start and end, a further one
+    // 3, the merge through the workspace 1.6 and the partial results' traffic.  (d/2 + 4 d/group bytes per token, side
+    // and head; the plan does not know the group and takes 64.)
+    const double bytes_per_token = 2.0 * (d / 2 + d / 16), gpu = 5.6e12 * sm_count / 148.0;
+    auto tokens_of = [&](int b) {
+        const int t = token_counts_host == nullptr ? max_context_len : token_counts_host[b];
+        return t <= 0 ? 0 : t < max_context_len ? t : max_context_len;
+    };
+    double total = static_cast<double>(B) * max_context_len;
     if (token_counts_host != nullptr) {
-        tokens = 0;
-        for (int b = 0; b < B; ++b)
-            if (token_counts_host[b] > 0)
-                tokens += token_counts_host[b] < max_context_len ? token_counts_host[b] : max_context_len;
+        total = 0.0;
+        for (int b = 0; b < B; ++b) total += tokens_of(b);
     }
-    // Two CTAs are resident per SM; aim at two waves of equal chunks of at least 256 tokens.
-    long long chunk = tokens * Hkv / (4ll * sm_count);
-    if (chunk < 256) chunk = 256;
-    long long S = (max_context_len + chunk - 1) / chunk;
-    if (S > 65535) S = 65535;
+    total *= Hkv * bytes_per_token;
+    long long S = 1;
+    double best = 0.0;
+    long long most = (max_context_len + 255) / 256;                  // splits of at least 256 tokens
+    if (most > 4096) most = 4096;
+    if (most > 1 + 8ll * sm_count / (static_cast<long long>(B) * Hkv)) most = 1 + 8ll * sm_count / (static_cast<long long>(B) * Hkv);
+    for (int cand = 1; cand <= most; ++cand) {
+        const int chunk = split_tokens_for(max_context_len, cand);
+        if (static_cast<long long>(chunk) * (cand - 1) >= max_context_len) continue;      // an empty split
+        double n = static_cast<double>(B) * cand;                                          // CTAs with tokens, per head
+        int longest = chunk < max_context_len ? chunk : max_context_len;
+        if (token_counts_host != nullptr) {
+            long long pieces = 0;
+            longest = 0;
+            for (int b = 0; b < B; ++b) {
+                const int t = tokens_of(b);
+                pieces += (t + chunk - 1) / chunk;
+                const int piece = t < chunk ? t : chunk;
+                longest = piece > longest ? piece : longest;
+            }
+            n = static_cast<double>(pieces);
+        }
+        n *= Hkv;
+        const bool fat = static_cast<long long>(B) * Hkv * cand <= sm_count;
+        const double rate = fat ? 43e9 : n <= sm_count ? 32e9 : n * longest * bytes_per_token > 1.25 * total ? 25e9 : 19e9;
+        const double alone = longest * bytes_per_token / rate, together = total / gpu;
+        double t = (alone > together ? alone : together) + 4e-6;
+        if (n > 2.0 * sm_count) t += (ceil(n / (2.0 * sm_count)) - 1.0) * 3e-6;
+        if (cand > 1) t += 1.6e-6 + 2.0 * n * (Hq / Hkv) * (d + 1.0) * 4.0 / gpu;
+        if (best == 0.0 || t < best) {
+            best = t;
+            S = cand;
+        }
+    }
     const int len = split_tokens_for(max_context_len, static_cast<int>(S));
     S = (static_cast<long long>(max_context_len) + len - 1) / len;
     *num_splits_out = static_cast<int>(S);

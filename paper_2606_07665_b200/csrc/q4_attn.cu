@@ -611,25 +611,37 @@ __global__ void __launch_bounds__(NW * 32, CTAS) paged_decode_attn_q4_kernel(con
     __syncthreads();
     if (!s_is_last) return;
     const size_t hq0 = static_cast<size_t>(b) * p.Hq + h * HG;
-    const int items = HG * C4;                     // at most 16 * 32 of them
+    const int items = HG * C4;                     // at most 16 * 32 of them, four per thread
     if (items <= THREADS) merge_splits_from_workspace<D, THREADS, 1, 16>(p, hq0, items, S, n_active);
     else if (items <= 2 * THREADS) merge_splits_from_workspace<D, THREADS, 2, 8>(p, hq0, items, S, n_active);
-    else merge_splits_from_workspace<D, THREADS, 3, 5>(p, hq0, items, S, n_active);
+    else merge_splits_from_workspace<D, THREADS, 4, 4>(p, hq0, items, S, n_active);
 }
 
-// Shapes of the CTA: warps, ring stages and CTAs per SM by group and head_dim.
-template <int D, int G, int NT>
-struct Q4Shape {
-    static constexpr int NW = NT == 2 || G == 4 ? 6 : 8;
-    static constexpr int STAGES = D == 64 ? 4 : 3;
-    static constexpr int CTAS = 2;
-    using Smem = Q4Smem<D, G, NW, STAGES>;
-    static_assert(16 * (D / 4) <= 3 * NW * 32, "the merge's items per thread");
-};
+// Shapes of the CTA, all of 8 or 12 warps per SM (the registers of the arithmetic allow no more):
+//   FAT    one CTA per SM, for grids of at most that many;
+//   BASE   two CTAs per SM: the second one's stream covers the first one's start and end;
+//   SLIM   three CTAs of four warps for grids of more than two waves' worth of short splits, where starts and ends are much
+//          of a CTA's life (256 rows of 512 to 2048 tokens: 45.3 -> 40.3 us; rows of up to 8192 unsplit: 57.4 -> 80, a
+//          long row's CTA is alone at the end).
+// Measured against BASE: eight warps per CTA at 128 registers are 6 % slower (4 rows of 131072 tokens: 115.7 against
+// 109.1 us).  With more than eight heads per KV head the accumulators double: four warps, 255 registers.
+enum class Fit { FAT, BASE, SLIM };
+constexpr int kSlimMaxSplitTokens = 2560;
 
-template <int D, int G, int NT>
-cudaError_t launch_q4(const Q4AttnParams& p, int B, cudaStream_t stream) {
-    using Shape = Q4Shape<D, G, NT>;
+template <int D, int G, int NT, Fit F>
+struct Q4Shape {
+    static constexpr int NW = NT == 2 ? (F == Fit::FAT ? 8 : 4) : F == Fit::FAT ? 12 : F == Fit::BASE ? 6 : 4;
+    static constexpr int STAGES = D == 64 ? 4 : 3;
+    static constexpr int CTAS = F == Fit::FAT ? 1 : F == Fit::BASE || NT == 2 ? 2 : 3;
+    using Smem = Q4Smem<D, G, NW, STAGES>;
+};
+#define AC_Q4_KERNEL(D_, G_, NT_, F_)                                                                                \
+    paged_decode_attn_q4_kernel<D_, G_, NT_, Q4Shape<D_, G_, NT_, F_>::NW, Q4Shape<D_, G_, NT_, F_>::STAGES,          \
+                                Q4Shape<D_, G_, NT_, F_>::CTAS>
+
+template <int D, int G, int NT, Fit F>
+cudaError_t launch_q4_shape(const Q4AttnParams& p, int B, cudaStream_t stream) {
+    using Shape = Q4Shape<D, G, NT, F>;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(p.Hkv, B, p.num_splits);
     cfg.blockDim = dim3(Shape::NW * 32);
@@ -640,15 +652,30 @@ cudaError_t launch_q4(const Q4AttnParams& p, int B, cudaStream_t stream) {
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, paged_decode_attn_q4_kernel<D, G, NT, Shape::NW, Shape::STAGES, Shape::CTAS>, p);
+    return cudaLaunchKernelEx(&cfg, AC_Q4_KERNEL(D, G, NT, F), p);
+}
+
+template <int D, int G, int NT>
+cudaError_t launch_q4(const Q4AttnParams& p, int B, int sms, cudaStream_t stream) {
+    const long long ctas = static_cast<long long>(B) * p.Hkv * p.num_splits;
+    if (ctas <= sms) return launch_q4_shape<D, G, NT, Fit::FAT>(p, B, stream);
+    if (NT == 1 && ctas > 2ll * sms && p.split_tokens <= kSlimMaxSplitTokens) return launch_q4_shape<D, G, NT, Fit::SLIM>(p, B, stream);
+    return launch_q4_shape<D, G, NT, Fit::BASE>(p, B, stream);
+}
+
+template <int D, int G, int NT, Fit F>
+cudaError_t set_q4_shape(int smem_optin) {
+    constexpr int bytes = Q4Shape<D, G, NT, F>::Smem::TOTAL;
+    if (bytes > smem_optin) return cudaErrorInvalidConfiguration;
+    return cudaFuncSetAttribute(AC_Q4_KERNEL(D, G, NT, F), cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
 }
 
 template <int D, int G, int NT>
 cudaError_t set_q4(int smem_optin) {
-    using Shape = Q4Shape<D, G, NT>;
-    if (Shape::Smem::TOTAL > smem_optin) return cudaErrorInvalidConfiguration;
-    return cudaFuncSetAttribute(paged_decode_attn_q4_kernel<D, G, NT, Shape::NW, Shape::STAGES, Shape::CTAS>,
-                                cudaFuncAttributeMaxDynamicSharedMemorySize, Shape::Smem::TOTAL);
+    cudaError_t e = set_q4_shape<D, G, NT, Fit::FAT>(smem_optin);
+    if (e == cudaSuccess) e = set_q4_shape<D, G, NT, Fit::BASE>(smem_optin);
+    if (e == cudaSuccess) e = set_q4_shape<D, G, NT, Fit::SLIM>(smem_optin);
+    return e;
 }
 
 }  // namespace
@@ -697,15 +724,18 @@ cudaError_t launch_paged_decode_attn_q4(const void* q_rot, const Q4View& cache, 
     p.num_pages = num_pages;
     p.window = window > 0 ? window : 0;
     p.sinks = window > 0 ? sinks : 0;
+    int dev = 0;
+    cudaGetDevice(&dev);
+    const int sms = device_state(dev).sm_count;
     const int groups = d / cache.group;
     const bool wide = Hq / Hkv > 8;
     if (d == 128) {
-        if (groups == 1) return wide ? launch_q4<128, 1, 2>(p, B, stream) : launch_q4<128, 1, 1>(p, B, stream);
-        if (groups == 2) return wide ? launch_q4<128, 2, 2>(p, B, stream) : launch_q4<128, 2, 1>(p, B, stream);
-        return wide ? launch_q4<128, 4, 2>(p, B, stream) : launch_q4<128, 4, 1>(p, B, stream);
+        if (groups == 1) return wide ? launch_q4<128, 1, 2>(p, B, sms, stream) : launch_q4<128, 1, 1>(p, B, sms, stream);
+        if (groups == 2) return wide ? launch_q4<128, 2, 2>(p, B, sms, stream) : launch_q4<128, 2, 1>(p, B, sms, stream);
+        return wide ? launch_q4<128, 4, 2>(p, B, sms, stream) : launch_q4<128, 4, 1>(p, B, sms, stream);
     }
-    if (groups == 1) return wide ? launch_q4<64, 1, 2>(p, B, stream) : launch_q4<64, 1, 1>(p, B, stream);
-    return wide ? launch_q4<64, 2, 2>(p, B, stream) : launch_q4<64, 2, 1>(p, B, stream);
+    if (groups == 1) return wide ? launch_q4<64, 1, 2>(p, B, sms, stream) : launch_q4<64, 1, 1>(p, B, sms, stream);
+    return wide ? launch_q4<64, 2, 2>(p, B, sms, stream) : launch_q4<64, 2, 1>(p, B, sms, stream);
 }
 
 }  // namespace ac
