@@ -17,10 +17,12 @@ constexpr int kStep = kPlanThreads * kPagesPerThread;
 constexpr int kCopyThreads = 256;
 constexpr int kPiece = 4096;                  // bytes a warp moves at a time
 
-// Exclusive prefix sum over the CTA; *total is the sum.  Every thread calls it.
-template <class T>
+// Exclusive prefix sum over the THREADS threads of the CTA; *total is the sum.  Every thread calls it.
+template <int THREADS = kPlanThreads, class T>
 __device__ __forceinline__ T block_scan(T v, T* total) {
-    __shared__ T s_warp[kPlanThreads / 32];
+    constexpr int WARPS = THREADS / 32;
+    static_assert(WARPS <= 32, "one warp scans the warps' sums");
+    __shared__ T s_warp[WARPS];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     T x = v;
 #pragma unroll
@@ -30,7 +32,7 @@ __device__ __forceinline__ T block_scan(T v, T* total) {
     }
     if (lane == 31) s_warp[warp] = x;
     __syncthreads();
-    T w = s_warp[lane];                        // kPlanThreads / 32 == 32 warps
+    T w = lane < WARPS ? s_warp[lane] : T(0);
 #pragma unroll
     for (int off = 1; off < 32; off <<= 1) {
         const T y = __shfl_up_sync(0xffffffffu, w, off);
@@ -204,6 +206,7 @@ __global__ void __launch_bounds__(kPlanThreads) fork_plan_kernel(const int32_t* 
                                                                  const int2* pairs, int n, int rows, int page_size,
                                                                  int num_pages, int2* jobs, int32_t* used,
                                                                  int32_t* list, int32_t* status_flag) {
+    cudaTriggerProgrammaticLaunchCompletion();             // the next kernel waits for this one before it reads
     int need = 0;
     for (int at = 0; at < n; at += kPlanThreads) {
         const int i = at + threadIdx.x;
@@ -252,6 +255,7 @@ __global__ void __launch_bounds__(kCopyThreads) fork_apply_kernel(const __grid_c
                                                                   const int2* pairs, const int2* jobs,
                                                                   const int32_t* used, int n, int rows, int page_size,
                                                                   int num_pages, int32_t* status_flag) {
+    cudaGridDependencySynchronize();           // no early signal: what follows may read the tables before its own wait
     if (blockIdx.y > 0) {
         run_copies(pools.pool[blockIdx.y - 1], jobs, used, n, page_size, num_pages, nullptr);
         return;
@@ -320,55 +324,73 @@ __global__ void __launch_bounds__(kCopyThreads) release_kernel(const int32_t* bl
 
 // ---- compact ---------------------------------------------------------------------------------------------
 
-// head[0] = moves, head[1] = live pages; moves[k] = (from, to); place[p] for p >= live: the page's new id, or -1.
-__global__ void __launch_bounds__(kPlanThreads) compact_plan_kernel(const int32_t* refs, int num_pages, int32_t* head,
-                                                                    int2* moves, int32_t* place, int32_t* live_out) {
-    int live = 0;
-    for (int at = 0; at < num_pages; at += kStep) {
-        const int base = at + threadIdx.x * kPagesPerThread;
-        int mine = 0, total;
-        if (base < num_pages)
-            mine = min(kPagesPerThread, num_pages - base) - __popc(free_bits(refs, base, num_pages));
-        block_scan(mine, &total);
-        live += total;
-    }
-    // holes below `live` and live pages from there on, each in order: equally many
-    int holes = 0, movers = 0;
-    for (int at = 0; at < num_pages; at += kStep) {
-        const int base = at + threadIdx.x * kPagesPerThread;
-        uint32_t hole = 0, mover = 0;
-        if (base < num_pages) {
-            const uint32_t exist = num_pages - base >= kPagesPerThread ? 0xffffu : (1u << (num_pages - base)) - 1u;
-            const uint32_t below = base >= live ? 0u : live - base >= kPagesPerThread ? 0xffffu : (1u << (live - base)) - 1u;
-            const uint32_t open = free_bits(refs, base, num_pages);
-            hole = open & below;
-            mover = ~open & exist & ~below;
-            for (int i = 0; i < kPagesPerThread; ++i)
-                if (((exist & ~below) >> i) & 1u) place[base + i] = -1;
+// Ranks without a scan over the whole pool in one CTA: chunks of kChunk pages are counted, and each chunk's CTA then adds up
+// the counts it needs.  (One CTA that walked 40000 pages took 35 us; these two take 6.)
+constexpr int kChunkThreads = 256;
+constexpr int kChunk = kChunkThreads * kPagesPerThread;
+
+__global__ void __launch_bounds__(kChunkThreads) compact_count_kernel(const int32_t* refs, int num_pages, int32_t* counts) {
+    cudaTriggerProgrammaticLaunchCompletion();             // the next kernel waits for this one before it reads
+    const int base = blockIdx.x * kChunk + threadIdx.x * kPagesPerThread;
+    int live = 0, total;
+    if (base < num_pages) live = min(kPagesPerThread, num_pages - base) - __popc(free_bits(refs, base, num_pages));
+    block_scan<kChunkThreads>(live, &total);
+    if (threadIdx.x == 0) counts[blockIdx.x] = total;
+}
+
+// head[0] = moves, head[1] = live pages; moves[k] = (from, to): the k-th live page from id `live` on and the k-th hole
+// below; place[p] for p >= live: its k, or -1 where it is free.
+__global__ void __launch_bounds__(kChunkThreads) compact_rank_kernel(const int32_t* refs, int num_pages,
+                                                                     const int32_t* counts, int32_t* head, int2* moves,
+                                                                     int32_t* place, int32_t* live_out) {
+    cudaGridDependencySynchronize();
+    cudaTriggerProgrammaticLaunchCompletion();             // the next kernel waits for this one before it reads
+    const int chunks = gridDim.x, base = blockIdx.x * kChunk + threadIdx.x * kPagesPerThread;
+    const uint32_t exist = base >= num_pages ? 0u : num_pages - base >= kPagesPerThread ? 0xffffu : (1u << (num_pages - base)) - 1u;
+    const uint32_t open = base < num_pages ? free_bits(refs, base, num_pages) : 0u;
+    int mine, live;
+    const int inside = block_scan<kChunkThreads>(__popc(exist & ~open), &mine);
+    int before = 0;                                        // live pages in the chunks before this one
+    if (chunks == 1) {
+        live = mine;
+    } else {
+        int all = 0, ahead = 0;
+        for (int c = threadIdx.x; c < chunks; c += kChunkThreads) {
+            const int n = counts[c];
+            all += n;
+            if (c < static_cast<int>(blockIdx.x)) ahead += n;
         }
-        int hole_total, mover_total;
-        int hr = holes + block_scan(__popc(hole), &hole_total);
-        int mr = movers + block_scan(__popc(mover), &mover_total);
-        while (hole != 0) {
-            moves[hr++].y = base + __ffs(hole) - 1;
-            hole &= hole - 1;
-        }
-        while (mover != 0) {
-            moves[mr++].x = base + __ffs(mover) - 1;
-            mover &= mover - 1;
-        }
-        holes += hole_total;
-        movers += mover_total;
+        block_scan<kChunkThreads>(all, &live);
+        block_scan<kChunkThreads>(ahead, &before);
     }
-    __syncthreads();
-    for (int k = threadIdx.x; k < movers; k += kPlanThreads) {
-        const int2 m = moves[k];
-        place[m.x] = m.y;
+    // live pages below id `live`
+    int below_live = 0, part = 0;
+    const int edge = live / kChunk;                        // the chunk that holds that border
+    for (int c = threadIdx.x; c < edge; c += kChunkThreads) part += chunks == 1 ? mine : counts[c];
+    const int edge_base = edge * kChunk + threadIdx.x * kPagesPerThread;
+    if (edge_base < live) {
+        const int n = min(kPagesPerThread, live - edge_base);
+        part += __popc(~free_bits(refs, edge_base, num_pages) & ((1u << n) - 1u));
     }
-    if (threadIdx.x == 0) {
-        head[0] = movers;
+    block_scan<kChunkThreads>(part, &below_live);
+    if (blockIdx.x == 0 && threadIdx.x == 0) {
+        head[0] = live - below_live;
         head[1] = live;
         if (live_out != nullptr) *live_out = live;
+    }
+    int rank = before + inside;                            // live pages before this thread's
+#pragma unroll
+    for (int i = 0; i < kPagesPerThread; ++i) {
+        if (!((exist >> i) & 1u)) break;
+        const int page = base + i;
+        const bool is_free = (open >> i) & 1u;
+        if (page < live) {
+            if (is_free) moves[page - rank].y = page;
+        } else {
+            place[page] = is_free ? -1 : rank - below_live;
+            if (!is_free) moves[rank - below_live].x = page;
+        }
+        rank += is_free ? 0 : 1;
     }
 }
 
@@ -380,6 +402,7 @@ __global__ void __launch_bounds__(kCopyThreads) compact_apply_kernel(const __gri
                                                                      int page_size, int num_pages, const int32_t* head,
                                                                      const int2* moves, const int32_t* place,
                                                                      int32_t* status_flag) {
+    cudaGridDependencySynchronize();           // no early signal: what follows may read the tables before its own wait
     const int n = head[0], live = head[1];
     if (blockIdx.y > 0) {
         run_copies(pools.pool[blockIdx.y - 1], moves, nullptr, n, 1, num_pages, nullptr);
@@ -405,8 +428,8 @@ __global__ void __launch_bounds__(kCopyThreads) compact_apply_kernel(const __gri
                 if (page < 0 || page >= num_pages) {
                     raise(status_flag, AC_FLAG_PAGE_OOB);
                 } else if (page >= live) {
-                    const int to = place[page];
-                    if (to >= 0) page = to; else raise(status_flag, AC_FLAG_REF_COUNT);
+                    const int k = place[page];
+                    if (k >= 0) page = moves[k].y; else raise(status_flag, AC_FLAG_REF_COUNT);
                 }
             }
             table_out[row + k] = page;
@@ -467,10 +490,18 @@ cudaError_t launch_fork(const ac_page_pool* pools, int n_pools, int32_t* block_t
     unsigned x = copy_grid(pools, n_pools, n, sms);
     const unsigned forks = n < 8 * sms ? n : 8 * sms;
     if (x < forks) x = forks;
-    fork_apply_kernel<<<dim3(x, n_pools + 1), kCopyThreads, 0, stream>>>(
-        pool_args(pools, n_pools), block_table, max_pages_per_seq, context_lens, refs, pc, jobs, used, n, rows, page_size,
-        num_pages, status_flag);
-    return cudaGetLastError();
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(x, n_pools + 1);
+    cfg.blockDim = dim3(kCopyThreads);
+    cfg.stream = stream;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, fork_apply_kernel, pool_args(pools, n_pools), block_table, max_pages_per_seq,
+                              context_lens, refs, pc, static_cast<const int2*>(jobs), static_cast<const int32_t*>(used), n,
+                              rows, page_size, num_pages, status_flag);
 }
 
 cudaError_t launch_release(const int32_t* block_table, int max_pages_per_seq, int32_t* context_lens, int32_t* refs,
@@ -485,20 +516,39 @@ cudaError_t launch_compact(const ac_page_pool* pools, int n_pools, const int32_t
                            int max_pages_per_seq, const int32_t* context_lens, const int32_t* refs, int32_t* refs_out,
                            int rows, int page_size, int num_pages, int32_t* live_out, void* workspace,
                            int32_t* status_flag, int sms, cudaStream_t stream) {
+    const int chunks = (num_pages + kChunk - 1) / kChunk;
     int32_t* head = static_cast<int32_t*>(workspace);
     int2* moves = reinterpret_cast<int2*>(head + 4);
     int32_t* place = reinterpret_cast<int32_t*>(moves + num_pages / 2 + 1);
-    compact_plan_kernel<<<1, kPlanThreads, 0, stream>>>(refs, num_pages, head, moves, place, live_out);
-    cudaError_t e = cudaGetLastError();
+    int32_t* counts = place + num_pages;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(chunks);
+    cfg.blockDim = dim3(kChunkThreads);
+    cfg.stream = stream;
+    cudaError_t e;
+    if (chunks > 1) {
+        compact_count_kernel<<<chunks, kChunkThreads, 0, stream>>>(refs, num_pages, counts);
+        if ((e = cudaGetLastError()) != cudaSuccess) return e;
+        cfg.attrs = attr;                      // only behind the counting kernel: otherwise after everything before it
+        cfg.numAttrs = 1;
+    }
+    e = cudaLaunchKernelEx(&cfg, compact_rank_kernel, refs, num_pages, static_cast<const int32_t*>(counts), head, moves,
+                           place, live_out);
     if (e != cudaSuccess) return e;
     // how many pages move is known on the device only: at most half of them
     unsigned x = copy_grid(pools, n_pools, num_pages / 2 + 1, sms);
     const unsigned table = static_cast<unsigned>(rows < 2 * sms ? rows : 2 * sms);
     if (x < table) x = table;
-    compact_apply_kernel<<<dim3(x, n_pools + 1), kCopyThreads, 0, stream>>>(
-        pool_args(pools, n_pools), block_table, table_out, max_pages_per_seq, context_lens, refs, refs_out, rows,
-        page_size, num_pages, head, moves, place, status_flag);
-    return cudaGetLastError();
+    cfg.gridDim = dim3(x, n_pools + 1);
+    cfg.blockDim = dim3(kCopyThreads);
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, compact_apply_kernel, pool_args(pools, n_pools), block_table, table_out, max_pages_per_seq,
+                              context_lens, refs, refs_out, rows, page_size, num_pages, static_cast<const int32_t*>(head),
+                              static_cast<const int2*>(moves), static_cast<const int32_t*>(place), status_flag);
 }
 
 }  // namespace ac
