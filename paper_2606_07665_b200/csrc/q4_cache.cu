@@ -65,15 +65,15 @@ __global__ void __launch_bounds__(128) rope_kv_append_q4_kernel(
         return;
     }
     constexpr int LANES = 32 / G;
-    uint32_t words[EPL / 2], packed;
+    uint32_t words[EPL / 2], packed[1];
 #pragma unroll
     for (int w = 0; w < EPL / 2; ++w) words[w] = x[2 * w] | (static_cast<uint32_t>(x[2 * w + 1]) << 16);
     const uint32_t sm = q4_quantise<EPL / 2, LANES>(words, packed, 0xffffffffu);
     const int slot = p - page_idx * page_size;
     uint8_t* dst = (is_v ? cache.v_codes : cache.k_codes) + static_cast<int64_t>(page) * cache.stride_page +
                    slot * cache.stride_token + h * cache.stride_head + lane * (EPL / 2);
-    if (EPL == 4) *reinterpret_cast<uint16_t*>(dst) = static_cast<uint16_t>(packed);
-    else *dst = static_cast<uint8_t>(packed);
+    if (EPL == 4) *reinterpret_cast<uint16_t*>(dst) = static_cast<uint16_t>(packed[0]);
+    else *dst = static_cast<uint8_t>(packed[0]);
     if (lane % LANES == 0) {
         uint32_t* prm = cache.params + ((static_cast<int64_t>(page) * Hkv + h) * page_size + slot) * (2 * G);
         prm[(is_v ? G : 0) + lane / LANES] = sm;
@@ -84,15 +84,16 @@ __global__ void __launch_bounds__(128) rope_kv_append_q4_kernel(
 //
 // Persistent CTAs take blocks of kTokens consecutive tokens in turn.  One warp does nothing but find the next block's
 // slots (row by binary search in row_offsets, position, page; a chain of dependent loads) while the others work on this
-// block's (token, head) vectors, K then V: D/8 lanes of 16 dense bytes (4 packed ones) per vector, kInHand vectors
-// per lane at a time so that their loads overlap.
+// block's (token, head) vectors, K then V: D/16 lanes of 2 x 16 dense bytes (2 x 4 packed ones) per vector,
+// kInHand vectors per lane at a time so that their loads overlap.  (A lane's two pieces lie half a group apart, so that
+// lanes side by side read and write side by side.)
 // Bound: HBM, 2 dense and 0.56 packed bytes per element at group 64.
 constexpr int kTokens = 32;
 constexpr int kStoreThreads = 256;                         // workers; one more warp looks up
 template <bool STORE>
 struct Bulk {
     static constexpr int kCtas = STORE ? 3 : 4;            // per SM
-    static constexpr int kInHand = STORE ? 4 : 8;          // a packed vector is a quarter of a dense one
+    static constexpr int kInHand = STORE ? 2 : 4;          // a packed vector is a quarter of a dense one
 };
 
 struct TokenSlot {
@@ -136,7 +137,7 @@ __global__ void __launch_bounds__(kStoreThreads + 32, Bulk<STORE>::kCtas) kv_bul
     uint16_t* k, uint16_t* v, const Q4View cache, const int32_t* __restrict__ block_table, int max_pages_per_seq,
     const int32_t* __restrict__ start_pos, const int32_t* __restrict__ row_offsets, int total_tokens, int B, int Hkv,
     int page_size, int num_pages, int32_t* status_flag) {
-    constexpr int LPV = D / 8;                             // lanes per vector
+    constexpr int LPV = D / 16;                            // lanes per vector
     constexpr int VECS = kStoreThreads / LPV;              // vectors per pass of the CTA
     constexpr int LANES = LPV / G;                         // lanes per group
     constexpr int kInHand = Bulk<STORE>::kInHand;
@@ -155,8 +156,9 @@ __global__ void __launch_bounds__(kStoreThreads + 32, Bulk<STORE>::kCtas) kv_bul
     if (lookup && static_cast<int>(blockIdx.x) < blocks) look_up(blockIdx.x, 0);
     __syncthreads();
 
-    const int sub = threadIdx.x % LPV;
-    const uint32_t lanes = LPV == 16 ? 0xffffu << (threadIdx.x & 16) : 0xffu << (threadIdx.x & 24);
+    const int group = threadIdx.x % LPV / LANES, rank = threadIdx.x % LANES;
+    const int piece = group * 2 * LANES + rank;            // this lane's first 16 dense bytes; LANES further the second
+    const uint32_t lanes = LPV == 8 ? 0xffu << (threadIdx.x & 24) : 0xfu << (threadIdx.x & 28);
     // (token, head) of a lane's vectors is stepped instead of divided
     const int first_t = (threadIdx.x / LPV) / Hkv, first_h = threadIdx.x / LPV - first_t * Hkv;
     const int step_t = VECS / Hkv, step_h = VECS - step_t * Hkv;
@@ -173,17 +175,17 @@ __global__ void __launch_bounds__(kStoreThreads + 32, Bulk<STORE>::kCtas) kv_bul
         const int tokens = total_tokens - t0 < kTokens ? static_cast<int>(total_tokens - t0) : kTokens;
         const int vecs = tokens * Hkv;                     // (token, head), head fastest: dense order
         for (int side = 0; side < 2; ++side) {
-            uint16_t* dense = (side ? v : k) + (t0 * Hkv + threadIdx.x / LPV) * D + sub * 8;
-            uint8_t* const codes = (side ? cache.v_codes : cache.k_codes) + sub * 4 + first_code;
-            uint32_t* const params = cache.params + side * G + sub / LANES + first_param;
+            uint16_t* dense = (side ? v : k) + (t0 * Hkv + threadIdx.x / LPV) * D + piece * 8;
+            uint8_t* const codes = (side ? cache.v_codes : cache.k_codes) + piece * 4 + first_code;
+            uint32_t* const params = cache.params + side * G + group + first_param;
             int t = first_t, h = first_h;
             int64_t code_step = 0, param_step = 0;         // from the first head to head h
             for (int i = threadIdx.x / LPV; i < vecs; i += kInHand * VECS, dense += kInHand * VECS * D) {
                 bool live[kInHand];
                 uint8_t* code_at[kInHand];
                 uint32_t* param_at[kInHand];
-                uint4 raw[kInHand];
-                uint32_t word[kInHand], sm[kInHand];
+                uint4 raw[kInHand][2];
+                uint32_t word[kInHand][2], sm[kInHand];
 #pragma unroll
                 for (int u = 0; u < kInHand; ++u) {
                     const bool on = i + u * VECS < vecs;
@@ -192,9 +194,13 @@ __global__ void __launch_bounds__(kStoreThreads + 32, Bulk<STORE>::kCtas) kv_bul
                     code_at[u] = codes + (at.code + code_step);
                     param_at[u] = params + (at.param + param_step);
                     if (STORE) {
-                        if (live[u]) raw[u] = __ldcs(reinterpret_cast<const uint4*>(dense + u * VECS * D));
+                        if (live[u]) {
+                            raw[u][0] = __ldcs(reinterpret_cast<const uint4*>(dense + u * VECS * D));
+                            raw[u][1] = __ldcs(reinterpret_cast<const uint4*>(dense + u * VECS * D) + LANES);
+                        }
                     } else if (live[u]) {
-                        word[u] = *reinterpret_cast<const uint32_t*>(code_at[u]);
+                        word[u][0] = *reinterpret_cast<const uint32_t*>(code_at[u]);
+                        word[u][1] = *reinterpret_cast<const uint32_t*>(code_at[u] + 4 * LANES);
                         sm[u] = *param_at[u];
                     }
                     t += step_t;
@@ -212,15 +218,18 @@ __global__ void __launch_bounds__(kStoreThreads + 32, Bulk<STORE>::kCtas) kv_bul
                 for (int u = 0; u < kInHand; ++u) {
                     if (STORE) {
                         if (!live[u]) continue;            // uniform over the vector's lanes
-                        const uint32_t x[4] = {raw[u].x, raw[u].y, raw[u].z, raw[u].w};
-                        uint32_t packed;
-                        const uint32_t p = q4_quantise<4, LANES>(x, packed, lanes);
-                        *reinterpret_cast<uint32_t*>(code_at[u]) = packed;
-                        if (sub % LANES == 0) *param_at[u] = p;
+                        const uint32_t x[8] = {raw[u][0].x, raw[u][0].y, raw[u][0].z, raw[u][0].w,
+                                               raw[u][1].x, raw[u][1].y, raw[u][1].z, raw[u][1].w};
+                        uint32_t packed[2];
+                        const uint32_t p = q4_quantise<8, LANES>(x, packed, lanes);
+                        *reinterpret_cast<uint32_t*>(code_at[u]) = packed[0];
+                        *reinterpret_cast<uint32_t*>(code_at[u] + 4 * LANES) = packed[1];
+                        if (rank == 0) *param_at[u] = p;
                     } else if (i + u * VECS < vecs) {
-                        uint4 o = make_uint4(0u, 0u, 0u, 0u);
-                        if (live[u]) o = q4_values(word[u], sm[u]);
-                        __stcs(reinterpret_cast<uint4*>(dense + u * VECS * D), o);
+                        uint4* to = reinterpret_cast<uint4*>(dense + u * VECS * D);
+                        const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
+                        __stcs(to, live[u] ? q4_values(word[u][0], sm[u]) : zero);
+                        __stcs(to + LANES, live[u] ? q4_values(word[u][1], sm[u]) : zero);
                     }
                 }
             }
@@ -245,7 +254,7 @@ cudaError_t launch_bulk(void* k, void* v, const Q4View& cache, const int32_t* bl
     kv_bulk_q4_kernel<D, G, STORE_, FIXED_><<<grid, kStoreThreads + 32, 0, stream>>>(                                \
         kk, vv, cache, block_table, max_pages_per_seq, start_pos, row_offsets, total_tokens, B, Hkv, page_size,       \
         num_pages, status_flag)
-    const bool fixed = kStoreThreads / (D / 8) % Hkv == 0;
+    const bool fixed = kStoreThreads / (D / 16) % Hkv == 0;
     if (store) {
         if (fixed) AC_Q4_BULK_LAUNCH(true, true); else AC_Q4_BULK_LAUNCH(true, false);
     } else {

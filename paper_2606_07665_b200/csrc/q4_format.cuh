@@ -31,8 +31,9 @@ __device__ __noinline__ inline float q4_code_f64(float x, float lo, float s) {
 }
 
 // Quantises W words of two bf16 per lane.  A group is the elements of LANES consecutive, aligned lanes, all of
-// which must call this together with `mask` the lanes that execute it.  On return `packed` holds the lane's codes,
-// the first in the low nibble, and every lane of the group gets its (s, m) as two bf16, s in the low half.
+// which must call this together with `mask` the lanes that execute it.  On return `packed` holds the lane's codes in
+// order, eight to a word from the low nibble on, and every lane of the group gets its (s, m) as two bf16, s in the
+// low half.
 //
 // Arithmetic.  Minimum and maximum are exact (kept as the pair (max, -min), one shuffle and one instruction a step;
 // NaN comes through, an infinity shows in them).  The format's fp64 quotients are evaluated in fp32 wherever
@@ -40,18 +41,21 @@ __device__ __noinline__ inline float q4_code_f64(float x, float lo, float s) {
 //   scale  s32 = fl(fl(max - min) / 15) is within 2^-22 relative (four of its own ulps) of the quotient, so the bf16
 //          next to it is the right one unless the 16 bits cut off lie within 8 of the tie; tiny and overflowing
 //          ranges are left to fp64;
-//   codes  t = fl(x - m) times the approximate reciprocal of s gives a candidate c; d = t - c s (one fma, so exact up to
-//          t's own 2^-24 of 15 s) decides: c is right where |d| is below s / 2 by 2^-15 relative.  Halves are common (s has
-//          eight bits: about one element in 300), so they are resolved in fp32 too where t is exact, which makes d exact:
-//          beyond s / 2 the neighbour is nearer, at s / 2 the even one of the two counts.  fp64 is left for an inexact t
-//          and for tiny or overflowing ranges.
+//   codes  q = t r + (t - (t r) s) r with t = fl(x - m) and r the approximate reciprocal of s is t / s rounded to fp32 but
+//          for 2^-44 (one Newton step on a reciprocal good to 2^-22; the residual is exact).  Where every nonzero |x| of the
+//          lane, and m, is at least 2^-12 s, x - m and halves of s are multiples of 2^-20 s: t is exact, a quotient that is
+//          not a half is at least 2^-20 from it and q stays on its side, and one that is a half comes out as exactly
+//          that; rounding q to an integer is then rounding the quotient.  A lane with a smaller element (one in
+//          30 warps of normal values) or a zero decides by d = t - c s instead: beyond s / 2 the neighbour is nearer, at s / 2
+//          the even one of the two counts, provided t lost nothing; else, and for tiny or overflowing ranges, fp64.
 template <int W, int LANES>
-__device__ __forceinline__ uint32_t q4_quantise(const uint32_t (&x)[W], uint32_t& packed, uint32_t mask) {
-    uint32_t top = x[0], bottom = x[0];
+__device__ __forceinline__ uint32_t q4_quantise(const uint32_t (&x)[W], uint32_t (&packed)[(W + 3) / 4], uint32_t mask) {
+    uint32_t top = x[0], bottom = x[0], least = x[0] & 0x7FFF7FFFu;
 #pragma unroll
     for (int w = 1; w < W; ++w) {
         top = bf16x2_max_nan(top, x[w]);
         bottom = bf16x2_min_nan(bottom, x[w]);
+        least = bf16x2_min_nan(least, x[w] & 0x7FFF7FFFu);
     }
     bottom ^= 0x80008000u;
     // (max, -min) of the lane: both halves against each other
@@ -60,7 +64,8 @@ __device__ __forceinline__ uint32_t q4_quantise(const uint32_t (&x)[W], uint32_t
     for (int off = 1; off < LANES; off <<= 1) both = bf16x2_max_nan(both, __shfl_xor_sync(mask, both, off));
     const float hi = __uint_as_float(both << 16);
     const float lo = -__uint_as_float(both & 0xFFFF0000u);
-    packed = 0u;
+#pragma unroll
+    for (int w = 0; w < (W + 3) / 4; ++w) packed[w] = 0u;
     if (!(fabsf(hi) < INFINITY && fabsf(lo) < INFINITY)) return 0x7FC00000u;   // s = 0, m = NaN
     const float s32 = __fmul_rn(__fsub_rn(hi, lo), 0x1.111112p-4f);            // 1/15 and one rounding
     const uint32_t u = __float_as_uint(s32);
@@ -70,27 +75,26 @@ __device__ __forceinline__ uint32_t q4_quantise(const uint32_t (&x)[W], uint32_t
     float r;
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(s));
     constexpr float kMagic = 12582912.0f;                  // 1.5 * 2^23: adding it rounds to an integer
-    const float half = 0.5f * s;
-    float c[2 * W], d[2 * W], worst = 0.0f;                // c: code + kMagic
+    float c[2 * W];                                        // code + kMagic
 #pragma unroll
     for (int e = 0; e < 2 * W; ++e) {
         const float f = __uint_as_float((e & 1) ? (x[e >> 1] & 0xFFFF0000u) : (x[e >> 1] << 16));
-        const float t = __fsub_rn(f, lo);
-        c[e] = __fmaf_rn(t, r, kMagic);
-        d[e] = __fmaf_rn(__fsub_rn(kMagic, c[e]), s, t);
-        worst = fmaxf(worst, fabsf(d[e]));
+        const float t = __fsub_rn(f, lo), q = __fmul_rn(t, r);
+        c[e] = __fadd_rn(__fmaf_rn(__fmaf_rn(-q, s, t), r, q), kMagic);
     }
-    const float near = half * (1.0f - 0x1p-15f);
-    bool exact = s >= 0x1p-100f && s32 < INFINITY;
-    if (!(worst < near && exact)) {
+    const float small = fminf(__uint_as_float(least << 16), __uint_as_float(least & 0xFFFF0000u));
+    const bool plain = s >= 0x1p-100f && s32 < INFINITY;
+    if (!(plain && fminf(small, lo == 0.0f ? INFINITY : fabsf(lo)) >= s * 0x1p-12f)) {
+        const float half = 0.5f * s;
+        bool exact = plain;
 #pragma unroll
         for (int e = 0; e < 2 * W; ++e) {
-            if (fabsf(d[e]) < near) continue;              // seldom more than one of them
             const float f = __uint_as_float((e & 1) ? (x[e >> 1] & 0xFFFF0000u) : (x[e >> 1] << 16));
             const float t = __fsub_rn(f, lo), back = __fsub_rn(t, f);       // TwoSum: what t lost
             exact = exact && __fadd_rn(__fsub_rn(f, __fsub_rn(t, back)), __fsub_rn(-lo, back)) == 0.0f;
+            const float d = __fmaf_rn(__fsub_rn(kMagic, c[e]), s, t);
             const bool odd = __float_as_uint(c[e]) & 1u;
-            if (fabsf(d[e]) > half || (fabsf(d[e]) == half && odd)) c[e] += d[e] > 0.0f ? 1.0f : -1.0f;
+            if (fabsf(d) > half || (fabsf(d) == half && odd)) c[e] += d > 0.0f ? 1.0f : -1.0f;
         }
         if (!exact) {
 #pragma unroll
@@ -99,13 +103,16 @@ __device__ __forceinline__ uint32_t q4_quantise(const uint32_t (&x)[W], uint32_t
         }
     }
     // Codes side by side: the bits of c are those of kMagic plus the code, whose multiples come off at the end.
-    uint32_t sum = 0u, magics = 0u;
 #pragma unroll
-    for (int e = 0; e < 2 * W; ++e) {
-        sum += __float_as_uint(c[e]) << (4 * e);
-        magics += 0x4B400000u << (4 * e);
+    for (int w = 0; w < (W + 3) / 4; ++w) {
+        uint32_t sum = 0u, magics = 0u;
+#pragma unroll
+        for (int e = 0; e < 8 && 8 * w + e < 2 * W; ++e) {
+            sum += __float_as_uint(c[8 * w + e]) << (4 * e);
+            magics += 0x4B400000u << (4 * e);
+        }
+        packed[w] = sum - magics;
     }
-    packed = sum - magics;
     // -0 and +0 compare equal, so the minimum of a group that holds both is either; it is kept as +0
     const uint32_t m16 = lo == 0.0f ? 0u : __float_as_uint(lo) >> 16;
     return s16 | (m16 << 16);
