@@ -116,7 +116,9 @@ struct AttnParams {
 // and the fused step with the prelude variants (per-head RMSNorm, partial rotary, interleaved pairing).
 constexpr int ROPE_NONE = 0, ROPE_PLAIN = 1, ROPE_VARIANT = 2;
 
-template <int D, bool WIDE, int ROPE, int NW>
+// SINKS: the row's first tokens stay visible beside the window.  An instantiation of its own: the bookkeeping costs the
+// launches without sinks 2-3 % (graph sweep, batch 8: 9.01 against 9.27 us per step).
+template <int D, bool WIDE, int ROPE, int NW, bool SINKS>
 __global__ void __launch_bounds__(NW * 32, NW == kFatWarps ? 1 : 2) paged_decode_attn_kernel(
     const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map,
     const AttnParams p) {
@@ -174,15 +176,16 @@ __global__ void __launch_bounds__(NW * 32, NW == kFatWarps ? 1 : 2) paged_decode
     // written is independent of that kernel, so with a programmatic dependent launch it overlaps the
     // preceding kernel's execution.  The preceding kernel is either the RoPE + append kernel of this
     // step (writes slot ctx) or the fused step of the previous token (wrote slot ctx - 1).
-    // The splits partition the row's attended tokens laid end to end ("range" positions): without a window
-    // that is the row itself; with one, range position r is token r + window_base; with sinks in front, the
-    // first tiles (j < j_window of a warp's tiles) are the row's own and only those behind them move up.
-    int tok_begin = split * p.split_tokens;          // range position; moves up when a sliding window applies
+    // The splits partition the row's tokens, from the window's start on where one applies.  With sinks they partition the
+    // attended tokens laid end to end: tok_begin, tok_end and the tile numbers then count in that range, whose first tiles
+    // (j < j_window of a warp's tiles) are the row's own and whose others lie window_base tokens further.
+    int tok_begin = split * p.split_tokens;          // moves up when a sliding window applies
     int tile_begin = tok_begin / TILE;
-    int window_base = 0;                             // multiple of TILE
+    int window_base = 0;
     int j_window = 0;
     auto tile_token0 = [&](int j) {
-        return (tile_begin + warp + j * WARPS) * TILE + (j >= j_window ? window_base : 0);
+        const int at = (tile_begin + warp + j * WARPS) * TILE;
+        return SINKS && j >= j_window ? at + window_base : at;
     };
     const int32_t* bt_row = p.block_table + static_cast<size_t>(b) * p.max_pages_per_seq;
     auto load_page_id = [&](int j) {
@@ -198,30 +201,33 @@ __global__ void __launch_bounds__(NW * 32, NW == kFatWarps ? 1 : 2) paged_decode
     int n_tokens = ctx < 0 ? 0 : ctx + p.new_tokens;
     const long long table_tokens = static_cast<long long>(p.max_pages_per_seq) * p.page_size;
     if (n_tokens > table_tokens) n_tokens = static_cast<int>(table_tokens);
-    // Sliding window: the row attends over tokens [tok_lo, n_tokens).  The range starts at tok_lo rounded
-    // down to a multiple of 64; tiles wholly below tok_lo are skipped and the first tile masks its
-    // leading tokens.  With sinks the row also attends over [0, sinks): the range is the sinks' tiles
-    // followed by the tiles from the one that holds tok_lo, so no tile of it is masked wholly; where the
+    // Sliding window: the row attends over tokens [tok_lo, n_tokens).  The splits partition the range
+    // that starts at tok_lo rounded down to a multiple of 64; tiles wholly below tok_lo are skipped
+    // and the first tile masks its leading tokens.  With sinks the row also attends over [0, sinks): the range is the
+    // sinks' tiles followed by the tiles from the one that holds tok_lo, so no tile of it is masked wholly; where the
     // two pieces meet or overlap nothing moves and the mask alone does the work.
     int tok_lo = 0;
-    if (p.window > 0) {
+    if (SINKS) {
         tok_lo = max(0, n_tokens - p.window);
-        if (p.sinks == 0) {
-            window_base = tok_lo / 64 * 64;
-            tok_begin = max(split * p.split_tokens, tok_lo / TILE * TILE - window_base);
-            tile_begin = tok_begin / TILE;
-        } else if (p.sinks >= tok_lo) {
+        if (p.sinks >= tok_lo) {
             tok_lo = 0;                                  // sinks and window cover the whole row
         } else {
             const int sink_tiles = (p.sinks + TILE - 1) / TILE;
             window_base = max(0, tok_lo / TILE - sink_tiles) * TILE;
             j_window = max(0, sink_tiles - tile_begin - warp + WARPS - 1) / WARPS;
+#pragma unroll
+            for (int s = 0; s < STAGES; ++s) page_first[s] = load_page_id(s);     // the range moved
         }
+    } else if (p.window > 0) {
+        tok_lo = max(0, n_tokens - p.window);
+        window_base = tok_lo / 64 * 64;
+        tok_begin = max(window_base + split * p.split_tokens, tok_lo / TILE * TILE);
+        tile_begin = tok_begin / TILE;
 #pragma unroll
         for (int s = 0; s < STAGES; ++s) page_first[s] = load_page_id(s);     // the range moved
     }
-    const int range_tokens = n_tokens - window_base;
-    const int tok_end = min((split + 1) * p.split_tokens, range_tokens);
+    const int tok_end = SINKS ? min((split + 1) * p.split_tokens, n_tokens - window_base)
+                              : min(window_base + (split + 1) * p.split_tokens, n_tokens);
 
     // Programmatic launch completion is signalled only AFTER this CTA has synchronised on the
     // preceding kernel (dependency_sync below).  The next kernel of the stream (launched with the
@@ -283,9 +289,10 @@ __global__ void __launch_bounds__(NW * 32, NW == kFatWarps ? 1 : 2) paged_decode
     const uint64_t policy = l2_policy_evict_first();
     // Tiles from the one holding slot ctx - 1 onwards must not be fetched before the preceding kernel
     // has completed; new_token_tile is where this step's own token lives.
-    // (Both as tiles of the range; slot ctx - 1 may lie below a window's range, which only waits earlier.)
-    const int new_token_tile = p.new_tokens > 0 ? (ctx - window_base) / TILE : -1;
-    const int first_dependent_tile = ((ctx > 0 ? ctx - 1 : 0) - window_base) / TILE;
+    // (With sinks both count in the range; slot ctx - 1 may then lie between its pieces, which only waits earlier.)
+    const int range_shift = SINKS ? window_base : 0;
+    const int new_token_tile = p.new_tokens > 0 ? (ctx - range_shift) / TILE : -1;
+    const int first_dependent_tile = ((ctx > 0 ? ctx - 1 : 0) - range_shift) / TILE;
 
     auto issue_at = [&](int j, int slot, int page) {      // lane 0 only; slot = first token's slot inside its page
         const int stage = j % STAGES;
@@ -545,9 +552,9 @@ __global__ void __launch_bounds__(NW * 32, NW == kFatWarps ? 1 : 2) paged_decode
         }
         bool wrote_stage = false;                              // ordinary stores went into this stage
         const int tok0 = tile_token0(j);
-        const int n_valid = tok_end - (tile_begin + warp + j * WARPS) * TILE;   // >= 1; < 16 only on the last tile
-        const int lo_valid = tok_lo - tok0;                    // > 0 only on a window's first tile and on sinks
-        const int sink_valid = p.sinks - tok0;                 // < 16 on every tile but the sinks' full ones
+        const int n_valid = tok_end - (SINKS ? (tile_begin + warp + j * WARPS) * TILE : tok0);   // >= 1; < 16 only on the last tile
+        const int lo_valid = tok_lo - tok0;                    // > 0 only on the first tile of a window, and on sinks
+        const int sink_valid = SINKS ? p.sinks - tok0 : 0;     // tokens of the tile that are sinks
 
         if (ROPE && j == append_j && append_ok) {
             // The tile just loaded still has the stale slot of the new token: overwrite that row with
@@ -596,7 +603,7 @@ __global__ void __launch_bounds__(NW * 32, NW == kFatWarps ? 1 : 2) paged_decode
             }
         }
 
-        if (n_valid < TILE || (lo_valid > 0 && sink_valid < TILE)) {
+        if (n_valid < TILE || (lo_valid > 0 && (!SINKS || sink_valid < TILE))) {
             // Slots past the request's length hold arbitrary bits, and tokens between the sinks and a
             // sliding window's start are not attended: mask their scores and clear their V rows (0 * NaN
             // would poison the product).
@@ -605,13 +612,13 @@ __global__ void __launch_bounds__(NW * 32, NW == kFatWarps ? 1 : 2) paged_decode
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const int col = nt * 8 + 2 * t + (e & 1);
-                    if (col >= n_valid || (col < lo_valid && col >= sink_valid)) s[nt][e] = -INFINITY;
+                    if (col >= n_valid || (col < lo_valid && (!SINKS || col >= sink_valid))) s[nt][e] = -INFINITY;
                 }
             const int chunks_per_row = L::HALVES * 8;
             for (int idx = lane; idx < TILE * chunks_per_row; idx += 32) {
                 const int row = idx / chunks_per_row;
                 const int rem = idx % chunks_per_row;
-                if (row >= n_valid || (row < lo_valid && row >= sink_valid)) {
+                if (row >= n_valid || (row < lo_valid && (!SINKS || row >= sink_valid))) {
                     uint4* dstz = reinterpret_cast<uint4*>(smem_gen + (vbase - smem_base) +
                                                            (rem >> 3) * L::HALF_BYTES + row * 128 + (rem & 7) * 16);
                     *dstz = make_uint4(0u, 0u, 0u, 0u);
@@ -677,7 +684,7 @@ __global__ void __launch_bounds__(NW * 32, NW == kFatWarps ? 1 : 2) paged_decode
                 next_slot -= p.page_size;
                 ++next_idx;
             }
-            if (issued + 1 == j_window) {                      // from the sinks' tiles to the window's
+            if (SINKS && issued + 1 == j_window) {             // from the sinks' tiles to the window's
                 next_idx = tile_token0(j_window) / p.page_size;
                 next_slot = tile_token0(j_window) - next_idx * p.page_size;
             }
@@ -782,7 +789,7 @@ __global__ void __launch_bounds__(NW * 32, NW == kFatWarps ? 1 : 2) paged_decode
         // their shared memory.  No global round trip, no ticket; CTAs whose split has no tokens pass
         // through the same two barriers and nothing else.
         // splits with tokens, <= 16 (a row longer than the split grid covers still has S of them)
-        const int n_active = min(S, (range_tokens + p.split_tokens - 1) / p.split_tokens);
+        const int n_active = min(S, (n_tokens - window_base + p.split_tokens - 1) / p.split_tokens);
         cluster_sync_all();                              // every staged result is written and visible
         if (split == 0) {
             constexpr int D4 = D / 4;
@@ -833,7 +840,7 @@ __global__ void __launch_bounds__(NW * 32, NW == kFatWarps ? 1 : 2) paged_decode
     // Nobody waits for anybody: CTAs that are not last simply exit.
     __shared__ int s_is_last;
     // splits with tokens (a row longer than the split grid covers still has S of them)
-    const int n_active = min(S, (range_tokens + p.split_tokens - 1) / p.split_tokens);
+    const int n_active = min(S, (n_tokens - window_base + p.split_tokens - 1) / p.split_tokens);
     // One acquire-release atomic by one thread, bracketed by CTA barriers: the release orders the
     // partials that every thread of this CTA stored before the first barrier ahead of the ticket, the
     // acquire orders the ticket ahead of the partial loads that follow the second barrier.
@@ -854,7 +861,7 @@ __global__ void __launch_bounds__(NW * 32, NW == kFatWarps ? 1 : 2) paged_decode
     else merge_splits_from_workspace<D, THREADS, 3, 5>(p, hq0, items, S, n_active);
 }
 
-template <int D, bool WIDE, int ROPE, int NW>
+template <int D, bool WIDE, int ROPE, int NW, bool SINKS>
 cudaError_t launch_one_staged(const CUtensorMap& k_map, const CUtensorMap& v_map, const AttnParams& p_in, int B,
                        cudaStream_t stream) {
     AttnParams p = p_in;
@@ -886,7 +893,7 @@ cudaError_t launch_one_staged(const CUtensorMap& k_map, const CUtensorMap& v_map
         if (known == 0) {
             int n = 0;
             cfg.numAttrs = 2;
-            const cudaError_t qe = cudaOccupancyMaxActiveClusters(&n, paged_decode_attn_kernel<D, WIDE, ROPE, NW>, &cfg);
+            const cudaError_t qe = cudaOccupancyMaxActiveClusters(&n, paged_decode_attn_kernel<D, WIDE, ROPE, NW, SINKS>, &cfg);
             if (qe != cudaSuccess) {
                 cudaGetLastError();
                 n = 0;
@@ -896,7 +903,7 @@ cudaError_t launch_one_staged(const CUtensorMap& k_map, const CUtensorMap& v_map
         if (static_cast<long long>(B) * p.Hkv > known) p.cluster_merge = 0;
     }
     cfg.numAttrs = p.cluster_merge ? 2 : 1;
-    return cudaLaunchKernelEx(&cfg, paged_decode_attn_kernel<D, WIDE, ROPE, NW>, k_map, v_map, p);
+    return cudaLaunchKernelEx(&cfg, paged_decode_attn_kernel<D, WIDE, ROPE, NW, SINKS>, k_map, v_map, p);
 }
 
 // Grids of at most one CTA per SM leave half of each SM's shared memory and warp slots unused: when a
@@ -904,15 +911,15 @@ cudaError_t launch_one_staged(const CUtensorMap& k_map, const CUtensorMap& v_map
 // (the same bytes in flight per SM as two resident CTAs, and twice the warps to hide a warp's
 // latency-bound time per tile).  Shorter splits keep the small footprint, which lets the next kernel of
 // a chain become resident beside this one.
-template <int D, bool WIDE, int ROPE>
-cudaError_t launch_one(const CUtensorMap& k_map, const CUtensorMap& v_map, const AttnParams& p, int B,
+template <int D, bool WIDE, int ROPE, bool SINKS>
+cudaError_t launch_shaped(const CUtensorMap& k_map, const CUtensorMap& v_map, const AttnParams& p, int B,
                        cudaStream_t stream) {
     int dev = 0;
     cudaGetDevice(&dev);
     const long long ctas = static_cast<long long>(B) * p.Hkv * p.num_splits;
     const int sms = device_state(dev).sm_count;
     const bool fat = ctas <= sms && p.split_tokens > kStages * kWarps * TILE;
-    if (fat) return launch_one_staged<D, WIDE, ROPE, kFatWarps>(k_map, v_map, p, B, stream);
+    if (fat) return launch_one_staged<D, WIDE, ROPE, kFatWarps, SINKS>(k_map, v_map, p, B, stream);
     // One wave of very long splits, two CTAs per SM: every CTA streams for the whole launch, nothing
     // ramps beside it, and HBM delivers more with fewer requests outstanding per SM (a compute-free
     // loop with this kernel's loads: 6.59 TB/s at 192 KB in flight per SM, 6.64 at 128 KB, 6.8 at 96 KB).
@@ -921,8 +928,15 @@ cudaError_t launch_one(const CUtensorMap& k_map, const CUtensorMap& v_map, const
     // wave is uniform by construction and shorter splits qualify (rows of 4096: 86.3 -> 82.2 us).
     const int slim_min_tokens = p.window > 0 ? kSlimMinWindowSplitTokens : kSlimMinSplitTokens;
     const bool slim = ctas > sms && ctas <= 2ll * sms && p.split_tokens >= slim_min_tokens;
-    return slim ? launch_one_staged<D, WIDE, ROPE, kSlimWarps>(k_map, v_map, p, B, stream)
-                : launch_one_staged<D, WIDE, ROPE, kWarps>(k_map, v_map, p, B, stream);
+    return slim ? launch_one_staged<D, WIDE, ROPE, kSlimWarps, SINKS>(k_map, v_map, p, B, stream)
+                : launch_one_staged<D, WIDE, ROPE, kWarps, SINKS>(k_map, v_map, p, B, stream);
+}
+
+template <int D, bool WIDE, int ROPE>
+cudaError_t launch_one(const CUtensorMap& k_map, const CUtensorMap& v_map, const AttnParams& p, int B,
+                       cudaStream_t stream) {
+    return p.sinks > 0 ? launch_shaped<D, WIDE, ROPE, true>(k_map, v_map, p, B, stream)
+                       : launch_shaped<D, WIDE, ROPE, false>(k_map, v_map, p, B, stream);
 }
 
 }  // namespace
@@ -930,13 +944,15 @@ cudaError_t launch_one(const CUtensorMap& k_map, const CUtensorMap& v_map, const
 cudaError_t attn_set_attributes(int smem_optin) {
     if (Smem<128, kFatWarps>::TOTAL > smem_optin) return cudaErrorInvalidConfiguration;
     cudaError_t e;
-#define AC_SET_STAGED(D_, W_, R_, S_)                                                              \
-    e = cudaFuncSetAttribute(paged_decode_attn_kernel<D_, W_, R_, S_>,                             \
+#define AC_SET_STAGED_ONE(D_, W_, R_, S_, K_)                                                      \
+    e = cudaFuncSetAttribute(paged_decode_attn_kernel<D_, W_, R_, S_, K_>,                         \
                              cudaFuncAttributeMaxDynamicSharedMemorySize, Smem<D_, S_>::TOTAL);    \
     if (e != cudaSuccess) return e;                                                                \
-    e = cudaFuncSetAttribute(paged_decode_attn_kernel<D_, W_, R_, S_>,                             \
+    e = cudaFuncSetAttribute(paged_decode_attn_kernel<D_, W_, R_, S_, K_>,                         \
                              cudaFuncAttributeNonPortableClusterSizeAllowed, 1);                   \
     if (e != cudaSuccess) return e;
+#define AC_SET_STAGED(D_, W_, R_, S_)                                                              \
+    AC_SET_STAGED_ONE(D_, W_, R_, S_, false) AC_SET_STAGED_ONE(D_, W_, R_, S_, true)
 #define AC_SET_ONE(D_, W_, R_)                                                                    \
     AC_SET_STAGED(D_, W_, R_, kWarps) AC_SET_STAGED(D_, W_, R_, kFatWarps) AC_SET_STAGED(D_, W_, R_, kSlimWarps)
 #define AC_SET(D_, W_)                                                                             \
@@ -947,6 +963,7 @@ cudaError_t attn_set_attributes(int smem_optin) {
     AC_SET(64, true)
 #undef AC_SET_ONE
 #undef AC_SET_STAGED
+#undef AC_SET_STAGED_ONE
 #undef AC_SET
     return cudaSuccess;
 }
