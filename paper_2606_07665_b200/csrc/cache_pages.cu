@@ -138,8 +138,11 @@ __global__ void __launch_bounds__(kPlanThreads) reserve_kernel(int32_t* block_ta
 
 // ---- page copies -----------------------------------------------------------------------------------------
 
+// The pools as a kernel argument, in two sizes: 3 KB of arguments cost a small launch about half a microsecond.
+constexpr int kFewPools = 8;
+template <int N>
 struct PoolArgs {
-    ac_page_pool pool[AC_MAX_PAGE_POOLS];
+    ac_page_pool pool[N];
 };
 
 // A warp copies bytes [lo, hi) of a piece (hi - lo <= kPiece, lo a multiple of 16, addresses 16-byte aligned).
@@ -191,7 +194,8 @@ __device__ __forceinline__ void run_copies(const ac_page_pool& pool, const int2*
     }
 }
 
-__global__ void __launch_bounds__(kCopyThreads) copy_pages_kernel(const __grid_constant__ PoolArgs pools,
+template <int N>
+__global__ void __launch_bounds__(kCopyThreads) copy_pages_kernel(const __grid_constant__ PoolArgs<N> pools,
                                                                   const int2* pairs, int n, int num_pages,
                                                                   int32_t* status_flag) {
     run_copies(pools.pool[blockIdx.y], pairs, nullptr, n, 1, num_pages, status_flag);
@@ -249,7 +253,8 @@ __global__ void __launch_bounds__(kPlanThreads) fork_plan_kernel(const int32_t* 
 }
 
 // grid.y = 0: the tables, one CTA per fork in turn; grid.y >= 1: the copies in pool grid.y - 1.
-__global__ void __launch_bounds__(kCopyThreads) fork_apply_kernel(const __grid_constant__ PoolArgs pools,
+template <int N>
+__global__ void __launch_bounds__(kCopyThreads) fork_apply_kernel(const __grid_constant__ PoolArgs<N> pools,
                                                                   int32_t* block_table, int max_pages_per_seq,
                                                                   int32_t* context_lens, int32_t* refs,
                                                                   const int2* pairs, const int2* jobs,
@@ -395,7 +400,8 @@ __global__ void __launch_bounds__(kChunkThreads) compact_rank_kernel(const int32
 }
 
 // grid.y = 0: block table and reference counts; grid.y >= 1: the moves in pool grid.y - 1.
-__global__ void __launch_bounds__(kCopyThreads) compact_apply_kernel(const __grid_constant__ PoolArgs pools,
+template <int N>
+__global__ void __launch_bounds__(kCopyThreads) compact_apply_kernel(const __grid_constant__ PoolArgs<N> pools,
                                                                      const int32_t* block_table, int32_t* table_out,
                                                                      int max_pages_per_seq, const int32_t* context_lens,
                                                                      const int32_t* refs, int32_t* refs_out, int rows,
@@ -437,9 +443,10 @@ __global__ void __launch_bounds__(kCopyThreads) compact_apply_kernel(const __gri
     }
 }
 
-PoolArgs pool_args(const ac_page_pool* pools, int n_pools) {
-    PoolArgs a;
-    for (int i = 0; i < AC_MAX_PAGE_POOLS; ++i) a.pool[i] = i < n_pools ? pools[i] : ac_page_pool{nullptr, 0, 1, 0};
+template <int N>
+PoolArgs<N> pool_args(const ac_page_pool* pools, int n_pools) {
+    PoolArgs<N> a;
+    for (int i = 0; i < N; ++i) a.pool[i] = i < n_pools ? pools[i] : ac_page_pool{nullptr, 0, 1, 0};
     return a;
 }
 
@@ -462,8 +469,12 @@ unsigned copy_grid(const ac_page_pool* pools, int n_pools, long long jobs, int s
 cudaError_t launch_copy_pages(const ac_page_pool* pools, int n_pools, const int32_t* pairs, int n, int num_pages,
                               int32_t* status_flag, int sms, cudaStream_t stream) {
     const dim3 grid(copy_grid(pools, n_pools, n, sms), n_pools);
-    copy_pages_kernel<<<grid, kCopyThreads, 0, stream>>>(pool_args(pools, n_pools), reinterpret_cast<const int2*>(pairs),
-                                                         n, num_pages, status_flag);
+    const int2* sd = reinterpret_cast<const int2*>(pairs);
+    if (n_pools <= kFewPools)
+        copy_pages_kernel<<<grid, kCopyThreads, 0, stream>>>(pool_args<kFewPools>(pools, n_pools), sd, n, num_pages, status_flag);
+    else
+        copy_pages_kernel<<<grid, kCopyThreads, 0, stream>>>(pool_args<AC_MAX_PAGE_POOLS>(pools, n_pools), sd, n, num_pages,
+                                                             status_flag);
     return cudaGetLastError();
 }
 
@@ -499,9 +510,12 @@ cudaError_t launch_fork(const ac_page_pool* pools, int n_pools, int32_t* block_t
     cfg.stream = stream;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, fork_apply_kernel, pool_args(pools, n_pools), block_table, max_pages_per_seq,
-                              context_lens, refs, pc, static_cast<const int2*>(jobs), static_cast<const int32_t*>(used), n,
-                              rows, page_size, num_pages, status_flag);
+#define AC_FORK_APPLY(N_)                                                                                            \
+    cudaLaunchKernelEx(&cfg, fork_apply_kernel<N_>, pool_args<N_>(pools, n_pools), block_table, max_pages_per_seq,   \
+                       context_lens, refs, pc, static_cast<const int2*>(jobs), static_cast<const int32_t*>(used), n, \
+                       rows, page_size, num_pages, status_flag)
+    return n_pools <= kFewPools ? AC_FORK_APPLY(kFewPools) : AC_FORK_APPLY(AC_MAX_PAGE_POOLS);
+#undef AC_FORK_APPLY
 }
 
 cudaError_t launch_release(const int32_t* block_table, int max_pages_per_seq, int32_t* context_lens, int32_t* refs,
@@ -546,9 +560,13 @@ cudaError_t launch_compact(const ac_page_pool* pools, int n_pools, const int32_t
     cfg.blockDim = dim3(kCopyThreads);
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, compact_apply_kernel, pool_args(pools, n_pools), block_table, table_out, max_pages_per_seq,
-                              context_lens, refs, refs_out, rows, page_size, num_pages, static_cast<const int32_t*>(head),
-                              static_cast<const int2*>(moves), static_cast<const int32_t*>(place), status_flag);
+#define AC_COMPACT_APPLY(N_)                                                                                         \
+    cudaLaunchKernelEx(&cfg, compact_apply_kernel<N_>, pool_args<N_>(pools, n_pools), block_table, table_out,        \
+                       max_pages_per_seq, context_lens, refs, refs_out, rows, page_size, num_pages,                  \
+                       static_cast<const int32_t*>(head), static_cast<const int2*>(moves),                           \
+                       static_cast<const int32_t*>(place), status_flag)
+    return n_pools <= kFewPools ? AC_COMPACT_APPLY(kFewPools) : AC_COMPACT_APPLY(AC_MAX_PAGE_POOLS);
+#undef AC_COMPACT_APPLY
 }
 
 }  // namespace ac

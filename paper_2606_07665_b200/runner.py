@@ -278,7 +278,7 @@ class _OnDevice:
     def _bind(self, device):
         if device.type != "cuda":
             raise ValueError(f"tensors on {device}, expected a CUDA device")
-        self.device = device
+        self.device, self._index, self._lib = device, device.index, ac.lib()
         with torch.cuda.device(device):
             ac.ac_init(device.index)
             self.status_flag = torch.zeros(1, dtype=torch.int32, device=device)
@@ -287,19 +287,20 @@ class _OnDevice:
 
     def _enqueue(self, name, args, stream, at):
         """Calls the library with the device current; args are marshalled but for the stream, which goes in at `at`."""
-        if torch.cuda.current_device() != self.device.index:
+        if _current_device() != self._index:
             with torch.cuda.device(self.device):
                 return self._enqueue(name, args, stream, at)
         if stream is None:
-            args[at] = _raw_stream(self.device.index)
+            args[at] = _raw_stream(self._index)
         else:
             args[at] = stream if isinstance(stream, int) else stream.cuda_stream
-        status = getattr(ac.lib(), name)(*args)
+        status = getattr(self._lib, name)(*args)
         if status != 0:
             raise ac.AcError(status, name)
 
 
-# the current stream's handle without the wrapper object (a microsecond per call)
+# the current device and stream without the wrappers (a microsecond per call)
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda i: torch.cuda.current_stream(i).cuda_stream)
 
 
