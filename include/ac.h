@@ -512,12 +512,13 @@ int ac_decode_plan_q4(const int32_t* token_counts_host, int B, int Hq, int Hkv, 
                       size_t* workspace_bytes_out);
 
 /* Paged decode attention over the 4-bit cache, merge included: ac_paged_decode_attn_ex with fused_merge
- * set (grid, splits, workspace, inactive rows, window, sinks, row_order, max_context_len and status bits as
- * there; options->rope must be NULL).  K and V enter as the exact values c * s + m; q is bf16, products
- * and sums are fp32, and the softmax weights times a V group's scale are rounded to fp16 (2^-11 relative, or
- * 2^-31 of the largest V scale seen, whichever is more) for the second product.  Queries of magnitude 2^116
- * and more are outside the supported range.  Slots at or past n_b, unreferenced pages and unused
- * block-table entries never influence the result; a page id outside [0, num_pages) reads as zeros. */
+ * set (splits, workspace, inactive rows, window, sinks, row_order and max_context_len as there; options->rope must
+ * be NULL; no status bit is set).  K and V enter as the exact values c * s + m; q is bf16, products and sums are
+ * fp32, and the softmax weights times a V group's scale are rounded to fp16 (2^-11 relative, or 2^-31 of the
+ * largest V scale seen, whichever is more) for the second product.  Slots at or past n_b, unreferenced pages and
+ * unused block-table entries never influence the result; a page id outside [0, num_pages) reads as zeros.
+ * Outside the supported range: queries of magnitude 2^116 and more, and (AC_ERR_UNSUPPORTED) code pools that
+ * span more than 2^36 bytes.  The workspace belongs to one call at a time: calls that may overlap need one each. */
 int ac_paged_decode_attn_q4(const void* q_rot, const ac_q4_cache* cache, const int32_t* block_table,
                             int max_pages_per_seq, const int32_t* context_lens, int new_tokens,
                             float softmax_scale, int num_splits, void* workspace, size_t workspace_bytes,
@@ -553,7 +554,8 @@ typedef struct ac_page_pool {
 int ac_cache_copy_pages(const ac_page_pool* pools, int n_pools, const int32_t* pairs, int n, int num_pages,
                         int32_t* status_flag, void* stream);
 
-/* Bytes of workspace the next three calls need: host only, pure. */
+/* Bytes of workspace that reserve, fork (n = forks of the call) and compact need; n = 0 but for fork.  It holds
+ * nothing from one call to the next; calls that may overlap need one each.  Host only, pure. */
 size_t ac_cache_workspace_bytes(int rows, int num_pages, int n);
 
 /* Gives every active row room for new_tokens more tokens: pages ceil(n/page_size) .. ceil((n + new_tokens) /

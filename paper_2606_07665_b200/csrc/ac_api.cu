@@ -1049,7 +1049,7 @@ int ac_paged_decode_attn_q4(const void* q_rot, const ac_q4_cache* cache, const i
                             void* out, int B, int Hq, int Hkv, int d, int page_size, int num_pages,
                             int max_context_len, int32_t* status_flag, void* stream,
                             const ac_attn_options* options) {
-    (void)status_flag;                                     // no wait of this kernel can run out
+    (void)status_flag;                                     // no wait of this kernel can run out, and it appends nothing
     const int window = options != nullptr ? options->window : 0;
     const int sinks = options != nullptr ? options->sinks : 0;
     const int32_t* row_order = options != nullptr ? options->row_order : nullptr;
@@ -1065,6 +1065,10 @@ int ac_paged_decode_attn_q4(const void* q_rot, const ac_q4_cache* cache, const i
     st = parse_q4_cache(cache, s, &view);
     if (st != AC_OK) return st;
     if (!aligned16(q_rot) || !aligned16(out)) return AC_ERR_ALIGN;
+    // the kernel keeps a granule's place as 32 bits: 16-byte units in the code pools, granules in the parameters
+    if (view.stride_page > (1ll << 36) / num_pages ||
+        static_cast<long long>(num_pages) * Hkv * (page_size / 16) > 0xffffffffll)
+        return AC_ERR_UNSUPPORTED;
     float* partial_o = nullptr;
     float* partial_lse = nullptr;
     int32_t* arrivals = nullptr;

@@ -352,7 +352,8 @@ class _Rows(_OnDevice):
 class PagedAttention(_Rows):
     """Decode attention over a bf16 cache of the caller's, with an optional sliding window and sinks.
 
-    ``k_cache``, ``v_cache``: [num_pages, page_size, Hkv, d] ("token_major") or [num_pages, Hkv, page_size, d]."""
+    ``k_cache``, ``v_cache``: [num_pages, page_size, Hkv, d] ("token_major") or [num_pages, Hkv, page_size, d].  The
+    object owns its workspace: its calls must not overlap on the GPU (one object per stream)."""
 
     def __init__(self, k_cache, v_cache, block_table, context_lens, Hq, lens_host=None, window=0, sinks=0,
                  max_context_len=None, num_splits=None, row_order="auto", layout="token_major", softmax_scale=0.0,
@@ -470,7 +471,8 @@ class Q4DecodeStep(_Rows):
     """One decode step over a 4-bit cache: RoPE + quantised append, then attention (two launches).
 
     ``rope_variants``: rotary_dim, interleaved, q_norm_weight, k_norm_weight, norm_eps as in
-    ``ac_rope_kv_append_ex``; the rope tables are only needed for ``append`` and ``step``."""
+    ``ac_rope_kv_append_ex``; the rope tables are only needed for ``append`` and ``step``.  The object owns its
+    workspace: its calls must not overlap on the GPU (one object per stream)."""
 
     def __init__(self, cache, block_table, context_lens, Hq, lens_host=None, window=0, sinks=0, rope_cos=None,
                  rope_sin=None, max_context_len=None, num_splits=None, row_order="auto", rope_variants=None,
@@ -543,7 +545,8 @@ class CachePages(_OnDevice):
     ``pools``: contiguous tensors [num_pages, ...], each alone or with the number of segments of its page ([page,
     slot, ...]: 1; [page, head, slot, ...]: the heads).  ``block_table`` int32 [rows, max_pages_per_seq],
     ``context_lens`` int32 [rows] (< 0: unused), ``ref_counts`` int32 [num_pages] (0: free); all are updated in place.
-    ``status_flag`` collects what went wrong on the device (AC_FLAG_...)."""
+    ``status_flag`` collects what went wrong on the device (AC_FLAG_...).  The object owns its workspace: its calls must
+    not overlap on the GPU."""
 
     def __init__(self, pools, block_table, context_lens, ref_counts, page_size):
         self._bind(block_table.device)

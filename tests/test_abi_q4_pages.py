@@ -84,6 +84,8 @@ def test_q4_call_refusals(ac):
     assert attn(shape=(1, 34, 2, 64, 16, 64)) == UNSUPPORTED and attn(shape=(1, 8, 3, 64, 16, 64)) == SHAPE
     assert attn(splits=4) == WORKSPACE and attn(splits=4, ws=P, wb=100) == WORKSPACE
     assert attn(splits=4, ws=P + 4, wb=1 << 20) == ALIGN and attn(q=P + 2) == ALIGN
+    far = cache(ac, stride_page=1 << 31)                                        # 64 pages of 2 GB: more than 2^36 bytes
+    assert L.ac_paged_decode_attn_q4(P, far, P, 33, P, 1, 0.0, 1, None, 0, P, *SHAPE6, 513, None, None, None) == UNSUPPORTED
     assert attn(opt=ac._options(window=-1)) == SHAPE and attn(opt=ac._options(window=4, sinks=-1)) == SHAPE
     assert attn(opt=ac._options(rope=ac._rope_options(rotary_dim=32))) == UNSUPPORTED
     assert L.ac_kv_store_q4(P, P, c, P, 33, P, P, -1, 1, 2, 64, 16, 64, None, None) == SHAPE

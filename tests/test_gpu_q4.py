@@ -320,6 +320,45 @@ def test_attention_new_tokens_and_plan(rt, new_tokens):
     run_attention(rt, c, new_tokens=new_tokens)
 
 
+@pytest.mark.parametrize("lens,Hq,Hkv,splits", [
+    ([40000], 4, 1, None), ([300 + 37 * i for i in range(60)], 8, 4, None), ([(i * 7) % 70 - 1 for i in range(700)], 6, 3, 2),
+    ([100, 3000], 4, 2, 47),                                # as many splits as fit; most of the short row's are empty
+    ([2000] * 40, 64, 4, None),                             # sixteen heads, more than one CTA per SM
+    ([500 + i for i in range(120)], 16, 4, 1)])             # four-warp CTAs
+def test_attention_launch_shapes(rt, lens, Hq, Hkv, splits):
+    run_attention(rt, Case(rt, 49, lens, Hq, Hkv, 64, 16, 32), splits=splits)
+
+
+def test_attention_two_objects_on_two_streams(rt):
+    # each object has its workspace, so their calls may overlap
+    import torch
+    c = Case(rt, 48, [5000, 100, 3000], 8, 2, 128, 16, 64)
+    cache, q = c.upload(rt), dev(bits(c.rng, 3, 8, 128))
+    table, lens = dev(c.table), dev(c.lens)
+    objects = [rt.Q4DecodeStep(cache, table, lens, 8, lens_host=c.lens, num_splits=5) for _ in range(2)]
+    want = objects[0].attention(q)
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    outs = [[torch.empty_like(q) for _ in range(30)] for _ in range(2)]
+    for i in range(30):
+        for h, st, o in zip(objects, streams, outs):
+            h.attention(q, out=o[i], stream=st)
+    torch.cuda.synchronize()
+    assert all(torch.equal(o, want) for os in outs for o in os)
+
+
+def test_append_in_place_rotates_the_queries_where_they_are(rt):
+    import torch
+    c = Case(rt, 50, [5, 40], 4, 2, 128, 16, 64)
+    cos, sin = W.rope_table(64, 128, 10000.0)
+    h = rt.Q4DecodeStep(c.upload(rt), dev(c.table), dev(c.lens), 4, lens_host=c.lens, rope_cos=dev(cos), rope_sin=dev(sin))
+    q, k, v = (dev(bits(c.rng, 2, n, 128)) for n in (4, 2, 2))
+    want = h.append(q, k, v).clone()
+    h.append(q, k, v, q_out=q)
+    torch.cuda.synchronize()
+    assert torch.equal(q, want)
+
+
 def test_attention_row_order(rt):
     c = Case(rt, 42, [10, 500, 200, 700], 8, 2, 128, 16, 64)
     a = run_attention(rt, c, q=(q := bits(c.rng, 4, 8, 128)))[2]
