@@ -18,14 +18,31 @@ __device__ __forceinline__ uint32_t bf16x2_min_nan(uint32_t a, uint32_t b) {
     return r;
 }
 
-// The definition in fp64, for what the fast path below cannot decide; out of line, it is rare.
+// min(|a|, |b|) of two bf16 at a time; the sign of the result means nothing.
+__device__ __forceinline__ uint32_t bf16x2_min_abs_nan(uint32_t a, uint32_t b) {
+    uint32_t r;
+    asm("min.NaN.xorsign.abs.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+
+// What the fast path below cannot decide; out of line, so that it costs the fast path no registers.
 __device__ __noinline__ inline uint32_t q4_scale_f64(float lo, float hi) {
     const double range = __dsub_rn(static_cast<double>(hi), static_cast<double>(lo));
     const float s32 = __double2float_rn(__ddiv_rn(range, 15.0));
     return pack_bf16x2(s32, 0.0f) & 0x7FFFu;               // a group of both zeros may give -0: the scale is +0
 }
-__device__ __noinline__ inline float q4_code_f64(float x, float lo, float s) {
+__device__ __noinline__ inline float q4_code_slow(float x, float lo, float s, float r) {
     if (!(s > 0.0f)) return 0.0f;
+    const float t = __fsub_rn(x, lo), back = __fsub_rn(t, x);               // TwoSum: what t lost
+    const float lost = __fadd_rn(__fsub_rn(x, __fsub_rn(t, back)), __fsub_rn(-lo, back));
+    if (s >= 0x1p-100f && lost == 0.0f) {                                   // (lost is NaN where t overflowed)
+        // c is off by one at most; d = t - c s is exact
+        float c = rintf(__fmul_rn(t, r));
+        const float d = __fmaf_rn(-c, s, t), half = 0.5f * s;
+        const bool odd = static_cast<int>(c) & 1;
+        if (fabsf(d) > half || (fabsf(d) == half && odd)) c += d > 0.0f ? 1.0f : -1.0f;
+        return c;
+    }
     const double q = __ddiv_rn(__dsub_rn(static_cast<double>(x), static_cast<double>(lo)), static_cast<double>(s));
     return fminf(static_cast<float>(rint(q)), 15.0f);
 }
@@ -50,12 +67,12 @@ __device__ __noinline__ inline float q4_code_f64(float x, float lo, float s) {
 //          the even one of the two counts, provided t lost nothing; else, and for tiny or overflowing ranges, fp64.
 template <int W, int LANES>
 __device__ __forceinline__ uint32_t q4_quantise(const uint32_t (&x)[W], uint32_t (&packed)[(W + 3) / 4], uint32_t mask) {
-    uint32_t top = x[0], bottom = x[0], least = x[0] & 0x7FFF7FFFu;
+    uint32_t top = x[0], bottom = x[0], least = x[0];
 #pragma unroll
     for (int w = 1; w < W; ++w) {
         top = bf16x2_max_nan(top, x[w]);
         bottom = bf16x2_min_nan(bottom, x[w]);
-        least = bf16x2_min_nan(least, x[w] & 0x7FFF7FFFu);
+        least = bf16x2_min_abs_nan(least, x[w]);
     }
     bottom ^= 0x80008000u;
     // (max, -min) of the lane: both halves against each other
@@ -82,25 +99,12 @@ __device__ __forceinline__ uint32_t q4_quantise(const uint32_t (&x)[W], uint32_t
         const float t = __fsub_rn(f, lo), q = __fmul_rn(t, r);
         c[e] = __fadd_rn(__fmaf_rn(__fmaf_rn(-q, s, t), r, q), kMagic);
     }
-    const float small = fminf(__uint_as_float(least << 16), __uint_as_float(least & 0xFFFF0000u));
+    const float small = fminf(fabsf(__uint_as_float(least << 16)), fabsf(__uint_as_float(least & 0xFFFF0000u)));
     const bool plain = s >= 0x1p-100f && s32 < INFINITY;
     if (!(plain && fminf(small, lo == 0.0f ? INFINITY : fabsf(lo)) >= s * 0x1p-12f)) {
-        const float half = 0.5f * s;
-        bool exact = plain;
 #pragma unroll
-        for (int e = 0; e < 2 * W; ++e) {
-            const float f = __uint_as_float((e & 1) ? (x[e >> 1] & 0xFFFF0000u) : (x[e >> 1] << 16));
-            const float t = __fsub_rn(f, lo), back = __fsub_rn(t, f);       // TwoSum: what t lost
-            exact = exact && __fadd_rn(__fsub_rn(f, __fsub_rn(t, back)), __fsub_rn(-lo, back)) == 0.0f;
-            const float d = __fmaf_rn(__fsub_rn(kMagic, c[e]), s, t);
-            const bool odd = __float_as_uint(c[e]) & 1u;
-            if (fabsf(d) > half || (fabsf(d) == half && odd)) c[e] += d > 0.0f ? 1.0f : -1.0f;
-        }
-        if (!exact) {
-#pragma unroll
-            for (int e = 0; e < 2 * W; ++e)
-                c[e] = kMagic + q4_code_f64(__uint_as_float((e & 1) ? (x[e >> 1] & 0xFFFF0000u) : (x[e >> 1] << 16)), lo, s);
-        }
+        for (int e = 0; e < 2 * W; ++e)
+            c[e] = kMagic + q4_code_slow(__uint_as_float((e & 1) ? (x[e >> 1] & 0xFFFF0000u) : (x[e >> 1] << 16)), lo, s, r);
     }
     // Codes side by side: the bits of c are those of kMagic plus the code, whose multiples come off at the end.
 #pragma unroll
