@@ -11,8 +11,8 @@
 // exact and without bias.  The 2^24 and the 1/16 of the odd codes are powers of two and are taken back in q (odd
 // elements of the fragment are divided by 16) and in the result.  For V a whole byte (c0 + 16 c1) * 2^-24 and its
 // high nibble 16 c1 * 2^-24 are the operands instead, and the even element of the result is the difference of the two
-// fp32 sums, formed once at the end: a byte is one permutation away, which saves the shift.  ldmatrix brings both in
-// place: plain for K, transposed (as 16-bit halves, four codes of one token) for V.
+// sums: a byte is one permutation away, which saves the shift.  ldmatrix brings both in place: plain for K, transposed
+// (as 16-bit halves, four codes of one token) for V.
 //
 // Tiles.  The codes are the 16-row A operand of mma.m16n8k16 and the query heads its 8 columns (two column
 // blocks for groups of 9-16 heads), S^T = K Q^T and O^T = V^T P^T: a KV tile costs half the instructions that it
@@ -295,22 +295,25 @@ __global__ void __launch_bounds__(NW * 32, CTAS) paged_decode_attn_q4_kernel(con
         cs[nt][1] = __shfl_sync(0xffffffffu, factor, 8 * t + 4);
     }
 
-    float o[NC][2][NT][4];                         // O^T: columns = heads 2t, 2t + 1; tile (c, i): bytes 2g + i of chunk c, whole
-                                                   // in rows 0-7 and their high nibbles in rows 8-15
-    float mo[NT][G][2], m_run[NT][2], l_run[NT][2];
+    // O^T, heads 2t and 2t + 1 as pairs: [chunk][byte 2g + i of it][.][even element, odd element * 16]
+    uint64_t o[NC][2][NT][2];
+    float mo[NT][G][2], m_run[NT][2];
+    uint64_t l_run[NT];
+    const uint64_t minus_one = f32x2(-1.0f, -1.0f);
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
+    for (int nt = 0; nt < NT; ++nt) {
+        l_run[nt] = 0ull;
 #pragma unroll
         for (int hh = 0; hh < 2; ++hh) {
             m_run[nt][hh] = kLowest;
-            l_run[nt][hh] = 0.0f;
 #pragma unroll
             for (int gq = 0; gq < G; ++gq) mo[nt][gq][hh] = 0.0f;
-#pragma unroll
-            for (int c = 0; c < NC; ++c)
-#pragma unroll
-                for (int i = 0; i < 2; ++i) o[c][i][nt][hh] = o[c][i][nt][2 + hh] = 0.0f;
         }
+#pragma unroll
+        for (int c = 0; c < NC; ++c)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) o[c][i][nt][0] = o[c][i][nt][1] = 0ull;
+    }
     // power of two on V's scales: the largest one seen * vf is in [64, 128); before any, so high that one moves it
     float vf = 1.329227995784916e36f;              // 2^120
     float v_top = 0.0f;
@@ -442,24 +445,26 @@ __global__ void __launch_bounds__(NW * 32, CTAS) paged_decode_attn_q4_kernel(con
                 vf = next;
             }
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
+            for (int nt = 0; nt < NT; ++nt) {
+                float alpha[2];
 #pragma unroll
                 for (int hh = 0; hh < 2; ++hh) {
                     const float m_new = fmaxf(m_run[nt][hh], top[nt][hh]);
-                    const float alpha = ex2_approx(m_run[nt][hh] - m_new);
+                    alpha[hh] = ex2_approx(m_run[nt][hh] - m_new);
                     m_run[nt][hh] = m_new;
-                    l_run[nt][hh] *= alpha;
-                    const float both = alpha * vr;
 #pragma unroll
-                    for (int gq = 0; gq < G; ++gq) mo[nt][gq][hh] *= alpha;
-#pragma unroll
-                    for (int c = 0; c < NC; ++c)
-#pragma unroll
-                        for (int i = 0; i < 2; ++i) {
-                            o[c][i][nt][hh] *= both;
-                            o[c][i][nt][2 + hh] *= both;
-                        }
+                    for (int gq = 0; gq < G; ++gq) mo[nt][gq][hh] *= alpha[hh];
                 }
+                l_run[nt] = f32x2_mul(l_run[nt], f32x2(alpha[0], alpha[1]));
+                const uint64_t both = f32x2(alpha[0] * vr, alpha[1] * vr);
+#pragma unroll
+                for (int c = 0; c < NC; ++c)
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        o[c][i][nt][0] = f32x2_mul(o[c][i][nt][0], both);
+                        o[c][i][nt][1] = f32x2_mul(o[c][i][nt][1], both);
+                    }
+            }
         }
 
         // ---- weights ------------------------------------------------------------------------------------------------
@@ -467,12 +472,17 @@ __global__ void __launch_bounds__(NW * 32, CTAS) paged_decode_attn_q4_kernel(con
 #pragma unroll
         for (int sb = 0; sb < 2; ++sb) {
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
+            for (int nt = 0; nt < NT; ++nt) {
+                const uint64_t factor = f32x2(cs[nt][0], cs[nt][1]), less = f32x2(-m_run[nt][0], -m_run[nt][1]);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    sc[sb][nt][e] = ex2_approx(fmaf(sc[sb][nt][e], cs[nt][e & 1], -m_run[nt][e & 1]));
-                    l_run[nt][e & 1] += sc[sb][nt][e];
+                for (int r = 0; r < 2; ++r) {
+                    float a, b;
+                    f32x2_split(f32x2_fma(f32x2(sc[sb][nt][2 * r], sc[sb][nt][2 * r + 1]), factor, less), a, b);
+                    sc[sb][nt][2 * r] = ex2_approx(a);
+                    sc[sb][nt][2 * r + 1] = ex2_approx(b);
+                    l_run[nt] = f32x2_add(l_run[nt], f32x2(sc[sb][nt][2 * r], sc[sb][nt][2 * r + 1]));
                 }
+            }
 #pragma unroll
             for (int gq = 0; gq < G; ++gq)
 #pragma unroll
@@ -525,12 +535,11 @@ __global__ void __launch_bounds__(NW * 32, CTAS) paged_decode_attn_q4_kernel(con
 #pragma unroll
                 for (int i = 0; i < 2; ++i)
 #pragma unroll
-                    for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                        for (int hh = 0; hh < 2; ++hh) {
-                            o[c][i][nt][hh] += sum[i][nt][hh] - sum[i][nt][2 + hh];       // byte less high nibble
-                            o[c][i][nt][2 + hh] += sum[i][nt][2 + hh];
-                        }
+                    for (int nt = 0; nt < NT; ++nt) {
+                        const uint64_t byte = f32x2(sum[i][nt][0], sum[i][nt][1]), high = f32x2(sum[i][nt][2], sum[i][nt][3]);
+                        o[c][i][nt][0] = f32x2_add(o[c][i][nt][0], f32x2_fma(high, minus_one, byte));
+                        o[c][i][nt][1] = f32x2_add(o[c][i][nt][1], high);
+                    }
             }
         }
 
@@ -562,7 +571,9 @@ __global__ void __launch_bounds__(NW * 32, CTAS) paged_decode_attn_q4_kernel(con
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
         for (int hh = 0; hh < 2; ++hh) {
-            float l = l_run[nt][hh];
+            float l_pair[2];
+            f32x2_split(l_run[nt], l_pair[0], l_pair[1]);
+            float l = l_pair[hh];
 #pragma unroll
             for (int off = 4; off < 32; off <<= 1) l += __shfl_xor_sync(0xffffffffu, l, off);
             const int row = 8 * nt + 2 * t + hh;
@@ -581,8 +592,11 @@ __global__ void __launch_bounds__(NW * 32, CTAS) paged_decode_attn_q4_kernel(con
                     float val[4];
 #pragma unroll
                     for (int i = 0; i < 2; ++i) {
-                        val[2 * i] = o[c][i][nt][hh] * back * unscale + m;
-                        val[2 * i + 1] = o[c][i][nt][2 + hh] * (back * 0.0625f) * unscale + m;
+                        float even[2], odd[2];
+                        f32x2_split(o[c][i][nt][0], even[0], even[1]);
+                        f32x2_split(o[c][i][nt][1], odd[0], odd[1]);
+                        val[2 * i] = even[hh] * back * unscale + m;
+                        val[2 * i + 1] = odd[hh] * (back * 0.0625f) * unscale + m;
                     }
                     *reinterpret_cast<float4*>(wo + row * WSTRIDE + c * 32 + g * 4) = make_float4(val[0], val[1], val[2], val[3]);
                 }

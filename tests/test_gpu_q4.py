@@ -314,6 +314,25 @@ def test_attention_long_rows(rt, splits):
     run_attention(rt, c, splits=splits)
 
 
+@pytest.mark.parametrize("Hq", [4, 12])
+@pytest.mark.parametrize("splits", [1, 7])
+def test_attention_of_equal_weights_does_not_drift(rt, Hq, splits):
+    """With q = 0 every weight is exactly 1 and a weight times a scale (8 bits times a power of two) exact in fp16, so
+    only the sums err.  Twelve warps share the row in the widest launch, eight in that of more than eight heads: at most
+    512 tiles a warp.  Running sums of n terms of one sign are off by at most n 2^-24 of themselves; there are two (the
+    codes and the minima, |m| below 8 s, as large as |c s| on average): 2 * 512 * 2^-24 = 2^-14.  A tile's two steps on
+    the tensor pipe lose at most 2^-22 each of a byte sum that is 17 times the even code's: 2^-17.  Joining 12 warps, 8
+    lanes and 7 splits: 27 * 2^-24.  Together below 2^-13 of sum_t p_t |c s|; the result's own rounding is 2^-8."""
+    import torch
+    c = Case(rt, 31, [131071], Hq, 1, 64, 32, 64)
+    h = rt.Q4DecodeStep(c.upload(rt), dev(c.table), dev(c.lens), c.Hq, lens_host=c.lens, num_splits=splits)
+    q = np.zeros((1, Hq, 64), dtype=np.uint16)
+    out = f64(h.attention(dev(q)))
+    torch.cuda.synchronize()
+    ref, room = Q.attention(q, c.fetch, c.lens + 1, 1, 0, 0, slack=True)
+    assert (np.abs(out - ref) <= 2.0**-8 * np.abs(ref) + 2.0**-13 * room).all(), float((np.abs(out - ref) / room).max())
+
+
 @pytest.mark.parametrize("new_tokens", [0, 1])
 def test_attention_new_tokens_and_plan(rt, new_tokens):
     c = Case(rt, 41, [0, 64, 1500, -1], 16, 4, 128, 16, 64)
