@@ -297,7 +297,8 @@ __global__ void __launch_bounds__(NW * 32, CTAS) paged_decode_attn_q4_kernel(con
 
     // O^T, heads 2t and 2t + 1 as pairs: [chunk][byte 2g + i of it][.][even element, odd element * 16]
     uint64_t o[NC][2][NT][2];
-    float mo[NT][G][2], m_run[NT][2];
+    float m_run[NT][2];
+    uint64_t mo[NT][G];
     uint64_t l_run[NT];
     const uint64_t minus_one = f32x2(-1.0f, -1.0f);
 #pragma unroll
@@ -307,7 +308,7 @@ __global__ void __launch_bounds__(NW * 32, CTAS) paged_decode_attn_q4_kernel(con
         for (int hh = 0; hh < 2; ++hh) {
             m_run[nt][hh] = kLowest;
 #pragma unroll
-            for (int gq = 0; gq < G; ++gq) mo[nt][gq][hh] = 0.0f;
+            for (int gq = 0; gq < G; ++gq) mo[nt][gq] = 0ull;
         }
 #pragma unroll
         for (int c = 0; c < NC; ++c)
@@ -378,10 +379,13 @@ __global__ void __launch_bounds__(NW * 32, CTAS) paged_decode_attn_q4_kernel(con
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const uint32_t u = pr[sb][e >> 1][gq];
-                        sc[sb][nt][e] = fmaf(__uint_as_float(u & 0xFFFF0000u), qs[nt][gq][e & 1],
-                                             fmaf(__uint_as_float(u << 16), acc[nt][e], sc[sb][nt][e]));
+                    for (int r = 0; r < 2; ++r) {
+                        const uint32_t u = pr[sb][r][gq];
+                        const float ks = __uint_as_float(u << 16), km = __uint_as_float(u & 0xFFFF0000u);
+                        const uint64_t part = f32x2_fma(f32x2(ks, ks), f32x2(acc[nt][2 * r], acc[nt][2 * r + 1]),
+                                                        f32x2(sc[sb][nt][2 * r], sc[sb][nt][2 * r + 1]));
+                        f32x2_split(f32x2_fma(f32x2(km, km), f32x2(qs[nt][gq][0], qs[nt][gq][1]), part), sc[sb][nt][2 * r],
+                                    sc[sb][nt][2 * r + 1]);
                     }
             }
             if (valid != 0xffffffffu) {
@@ -452,10 +456,11 @@ __global__ void __launch_bounds__(NW * 32, CTAS) paged_decode_attn_q4_kernel(con
                     const float m_new = fmaxf(m_run[nt][hh], top[nt][hh]);
                     alpha[hh] = ex2_approx(m_run[nt][hh] - m_new);
                     m_run[nt][hh] = m_new;
-#pragma unroll
-                    for (int gq = 0; gq < G; ++gq) mo[nt][gq][hh] *= alpha[hh];
                 }
-                l_run[nt] = f32x2_mul(l_run[nt], f32x2(alpha[0], alpha[1]));
+                const uint64_t fade = f32x2(alpha[0], alpha[1]);
+                l_run[nt] = f32x2_mul(l_run[nt], fade);
+#pragma unroll
+                for (int gq = 0; gq < G; ++gq) mo[nt][gq] = f32x2_mul(mo[nt][gq], fade);
                 const uint64_t both = f32x2(alpha[0] * vr, alpha[1] * vr);
 #pragma unroll
                 for (int c = 0; c < NC; ++c)
@@ -491,9 +496,11 @@ __global__ void __launch_bounds__(NW * 32, CTAS) paged_decode_attn_q4_kernel(con
                     for (int r = 0; r < 2; ++r) {
                         const float f = __uint_as_float(pr[sb][r][G + gq] << 16) * vf;
                         const float vm = __uint_as_float(pr[sb][r][G + gq] & 0xFFFF0000u);
-                        pb[sb][gq][nt][r] = movmatrix_trans(pack_f16x2(sc[sb][nt][2 * r] * f, sc[sb][nt][2 * r + 1] * f));
-                        mo[nt][gq][0] = fmaf(sc[sb][nt][2 * r], vm, mo[nt][gq][0]);
-                        mo[nt][gq][1] = fmaf(sc[sb][nt][2 * r + 1], vm, mo[nt][gq][1]);
+                        const uint64_t pair = f32x2(sc[sb][nt][2 * r], sc[sb][nt][2 * r + 1]);
+                        float a, b;
+                        f32x2_split(f32x2_mul(pair, f32x2(f, f)), a, b);
+                        pb[sb][gq][nt][r] = movmatrix_trans(pack_f16x2(a, b));
+                        mo[nt][gq] = f32x2_fma(pair, f32x2(vm, vm), mo[nt][gq]);
                     }
         }
 
@@ -583,7 +590,9 @@ __global__ void __launch_bounds__(NW * 32, CTAS) paged_decode_attn_q4_kernel(con
             }
 #pragma unroll
             for (int gq = 0; gq < G; ++gq) {
-                float m = mo[nt][gq][hh];
+                float m_pair[2];
+                f32x2_split(mo[nt][gq], m_pair[0], m_pair[1]);
+                float m = m_pair[hh];
 #pragma unroll
                 for (int off = 4; off < 32; off <<= 1) m += __shfl_xor_sync(0xffffffffu, m, off);
 #pragma unroll
