@@ -82,14 +82,13 @@ __global__ void __launch_bounds__(128) rope_kv_append_q4_kernel(
 
 // ---- bulk store and load ---------------------------------------------------------------------------------
 //
-// Persistent CTAs take blocks of kTokens consecutive tokens in turn.  One warp does nothing but find the next block's
-// slots (row by binary search in row_offsets, position, page; a chain of dependent loads) while the others work on this
-// block's (token, head) vectors, K then V: D/16 lanes of 2 x 16 dense bytes (2 x 4 packed ones) per vector,
-// kInHand vectors per lane at a time so that their loads overlap.  (A lane's two pieces lie half a group apart, so that
-// lanes side by side read and write side by side.)
+// Every warp takes runs of consecutive tokens in turn and works by itself: its lanes find the slots of one token each (row
+// by binary search in row_offsets, position, page), then it goes through the run's (token, head) vectors, K then V, with
+// D/16 lanes of 2 x 16 dense bytes (2 x 4 packed ones) per vector and kInHand vectors per lane at a time, so that their
+// loads overlap.  (A lane's two pieces lie half a group apart, so that lanes side by side read and write side by side.)
 // Bound: HBM, 2 dense and 0.56 packed bytes per element at group 64.
-constexpr int kTokens = 32;
-constexpr int kStoreThreads = 256;                         // workers; one more warp looks up
+constexpr int kBulkThreads = 256;
+constexpr int kRunVectors = 32;                            // vectors of a run, at least, where there are tokens enough
 template <bool STORE>
 struct Bulk {
     static constexpr int kCtas = STORE ? 3 : 4;            // per SM
@@ -131,56 +130,47 @@ __device__ __forceinline__ TokenSlot find_slot(long long token, const Q4View& ca
     return r;
 }
 
-// FIXED: a pass of the CTA is a whole number of tokens (the number of heads divides it), so a lane keeps its head.
-template <int D, int G, bool STORE, bool FIXED>
-__global__ void __launch_bounds__(kStoreThreads + 32, Bulk<STORE>::kCtas) kv_bulk_q4_kernel(
+template <int D, int G, bool STORE>
+__global__ void __launch_bounds__(kBulkThreads, Bulk<STORE>::kCtas) kv_bulk_q4_kernel(
     uint16_t* k, uint16_t* v, const Q4View cache, const int32_t* __restrict__ block_table, int max_pages_per_seq,
-    const int32_t* __restrict__ start_pos, const int32_t* __restrict__ row_offsets, int total_tokens, int B, int Hkv,
-    int page_size, int num_pages, int32_t* status_flag) {
+    const int32_t* __restrict__ start_pos, const int32_t* __restrict__ row_offsets, int total_tokens, int run, int B,
+    int Hkv, int page_size, int num_pages, int32_t* status_flag) {
     constexpr int LPV = D / 16;                            // lanes per vector
-    constexpr int VECS = kStoreThreads / LPV;              // vectors per pass of the CTA
+    constexpr int VECS = 32 / LPV;                         // vectors per pass of the warp
     constexpr int LANES = LPV / G;                         // lanes per group
     constexpr int kInHand = Bulk<STORE>::kInHand;
-    __shared__ TokenSlot s_slot[2][kTokens];
-    const int blocks = static_cast<int>((static_cast<long long>(total_tokens) + kTokens - 1) / kTokens);
-    const bool lookup = threadIdx.x >= kStoreThreads;
-    auto look_up = [&](int block, int buffer) {
-        const int lane = threadIdx.x & 31;
-        const long long token = static_cast<long long>(block) * kTokens + lane;
-        TokenSlot r{-1, 0};
-        if (token < total_tokens)
-            r = find_slot(token, cache, 2 * G, block_table, max_pages_per_seq, start_pos, row_offsets, B, Hkv, page_size,
-                          num_pages, status_flag);
-        s_slot[buffer][lane] = r;
-    };
-    if (lookup && static_cast<int>(blockIdx.x) < blocks) look_up(blockIdx.x, 0);
-    __syncthreads();
+    constexpr int WARPS = kBulkThreads / 32;
+    __shared__ TokenSlot s_slots[WARPS][32];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    TokenSlot* const s_slot = s_slots[warp];
 
-    const int group = threadIdx.x % LPV / LANES, rank = threadIdx.x % LANES;
-    const int piece = group * 2 * LANES + rank;            // this lane's first 16 dense bytes; LANES further the second
-    const uint32_t lanes = LPV == 8 ? 0xffu << (threadIdx.x & 24) : 0xfu << (threadIdx.x & 28);
-    // (token, head) of a lane's vectors is stepped instead of divided
-    const int first_t = (threadIdx.x / LPV) / Hkv, first_h = threadIdx.x / LPV - first_t * Hkv;
+    const int first = lane / LPV;                          // this lane's first vector of the run
+    const int group = lane % LPV / LANES, rank = lane % LANES;
+    const int piece = group * 2 * LANES + rank;            // its first 16 dense bytes; LANES further the second
+    const uint32_t lanes = LPV == 8 ? 0xffu << (lane & 24) : 0xfu << (lane & 28);
+    // (token, head) of a lane's vectors is stepped instead of divided, and with it the head's place in a slot
+    const int first_t = first / Hkv, first_h = first - first_t * Hkv;
     const int step_t = VECS / Hkv, step_h = VECS - step_t * Hkv;
     const int64_t head_words = static_cast<int64_t>(page_size) * 2 * G;    // parameters of a page and head
-    const int64_t first_code = first_h * cache.stride_head, first_param = first_h * head_words;
-    int buffer = 0;
-    for (int block = blockIdx.x; block < blocks; block += gridDim.x, buffer ^= 1) {
-        if (lookup) {
-            if (block + static_cast<int>(gridDim.x) < blocks) look_up(block + gridDim.x, buffer ^ 1);
-            __syncthreads();
-            continue;
-        }
-        const long long t0 = static_cast<long long>(block) * kTokens;
-        const int tokens = total_tokens - t0 < kTokens ? static_cast<int>(total_tokens - t0) : kTokens;
+    const int64_t code_step = step_h * cache.stride_head, code_wrap = Hkv * cache.stride_head;
+    const int64_t param_step = step_h * head_words, param_wrap = Hkv * head_words;
+
+    const unsigned runs = (static_cast<unsigned>(total_tokens) + run - 1) / run;
+    for (unsigned r = warp * gridDim.x + blockIdx.x; r < runs; r += gridDim.x * WARPS) {
+        const long long t0 = static_cast<long long>(r) * run;
+        const int tokens = total_tokens - t0 < run ? static_cast<int>(total_tokens - t0) : run;
         const int vecs = tokens * Hkv;                     // (token, head), head fastest: dense order
+        __syncwarp();
+        if (lane < tokens)
+            s_slot[lane] = find_slot(t0 + lane, cache, 2 * G, block_table, max_pages_per_seq, start_pos, row_offsets, B,
+                                     Hkv, page_size, num_pages, status_flag);
+        __syncwarp();
         for (int side = 0; side < 2; ++side) {
-            uint16_t* dense = (side ? v : k) + (t0 * Hkv + threadIdx.x / LPV) * D + piece * 8;
-            uint8_t* const codes = (side ? cache.v_codes : cache.k_codes) + piece * 4 + first_code;
-            uint32_t* const params = cache.params + side * G + group + first_param;
+            uint16_t* dense = (side ? v : k) + (t0 * Hkv + first) * D + piece * 8;
+            uint8_t* codes = (side ? cache.v_codes : cache.k_codes) + piece * 4 + first_h * cache.stride_head;
+            uint32_t* params = cache.params + side * G + group + first_h * head_words;
             int t = first_t, h = first_h;
-            int64_t code_step = 0, param_step = 0;         // from the first head to head h
-            for (int i = threadIdx.x / LPV; i < vecs; i += kInHand * VECS, dense += kInHand * VECS * D) {
+            for (int i = first; i < vecs; i += kInHand * VECS, dense += kInHand * VECS * D) {
                 bool live[kInHand];
                 uint8_t* code_at[kInHand];
                 uint32_t* param_at[kInHand];
@@ -189,10 +179,10 @@ __global__ void __launch_bounds__(kStoreThreads + 32, Bulk<STORE>::kCtas) kv_bul
 #pragma unroll
                 for (int u = 0; u < kInHand; ++u) {
                     const bool on = i + u * VECS < vecs;
-                    const TokenSlot at = s_slot[buffer][on ? t : 0];
+                    const TokenSlot at = s_slot[on ? t : 0];
                     live[u] = on && at.code >= 0;
-                    code_at[u] = codes + (at.code + code_step);
-                    param_at[u] = params + (at.param + param_step);
+                    code_at[u] = codes + at.code;
+                    param_at[u] = params + at.param;
                     if (STORE) {
                         if (live[u]) {
                             raw[u][0] = __ldcs(reinterpret_cast<const uint4*>(dense + u * VECS * D));
@@ -204,14 +194,14 @@ __global__ void __launch_bounds__(kStoreThreads + 32, Bulk<STORE>::kCtas) kv_bul
                         sm[u] = *param_at[u];
                     }
                     t += step_t;
-                    if (!FIXED) {
-                        h += step_h;
-                        if (h >= Hkv) {
-                            h -= Hkv;
-                            ++t;
-                        }
-                        code_step = (h - first_h) * cache.stride_head;
-                        param_step = (h - first_h) * head_words;
+                    h += step_h;
+                    codes += code_step;
+                    params += param_step;
+                    if (h >= Hkv) {
+                        h -= Hkv;
+                        ++t;
+                        codes -= code_wrap;
+                        params -= param_wrap;
                     }
                 }
 #pragma unroll
@@ -234,7 +224,6 @@ __global__ void __launch_bounds__(kStoreThreads + 32, Bulk<STORE>::kCtas) kv_bul
                 }
             }
         }
-        __syncthreads();                                   // this block's slots are free, the next one's are there
     }
 }
 
@@ -245,22 +234,23 @@ cudaError_t launch_bulk(void* k, void* v, const Q4View& cache, const int32_t* bl
                         cudaStream_t stream) {
     // Ordinary launches: what follows them in the stream may read the cache before its own synchronisation, which
     // is safe only behind kernels that do not signal early.
-    const long long blocks = (static_cast<long long>(total_tokens) + kTokens - 1) / kTokens;
     const int ctas = (store ? Bulk<true>::kCtas : Bulk<false>::kCtas) * sms;
-    const unsigned grid = static_cast<unsigned>(blocks < ctas ? blocks : ctas);
+    // Shorter runs where there would not be one for every warp of the GPU, but no shorter than what a warp has in hand.
+    const int in_hand = 32 / (D / 16) * (store ? Bulk<true>::kInHand : Bulk<false>::kInHand);
+    int run = kRunVectors > Hkv ? kRunVectors / Hkv : 1;
+    while (run > 1 && total_tokens / run < ctas * (kBulkThreads / 32) && run / 2 * Hkv >= in_hand) run /= 2;
+    const long long runs = (static_cast<long long>(total_tokens) + run - 1) / run;
+    const unsigned grid = static_cast<unsigned>(runs < ctas ? runs : ctas);
     uint16_t* kk = static_cast<uint16_t*>(k);
     uint16_t* vv = static_cast<uint16_t*>(v);
-#define AC_Q4_BULK_LAUNCH(STORE_, FIXED_)                                                                            \
-    kv_bulk_q4_kernel<D, G, STORE_, FIXED_><<<grid, kStoreThreads + 32, 0, stream>>>(                                \
-        kk, vv, cache, block_table, max_pages_per_seq, start_pos, row_offsets, total_tokens, B, Hkv, page_size,       \
-        num_pages, status_flag)
-    const bool fixed = kStoreThreads / (D / 16) % Hkv == 0;
-    if (store) {
-        if (fixed) AC_Q4_BULK_LAUNCH(true, true); else AC_Q4_BULK_LAUNCH(true, false);
-    } else {
-        if (fixed) AC_Q4_BULK_LAUNCH(false, true); else AC_Q4_BULK_LAUNCH(false, false);
-    }
-#undef AC_Q4_BULK_LAUNCH
+    if (store)
+        kv_bulk_q4_kernel<D, G, true><<<grid, kBulkThreads, 0, stream>>>(
+            kk, vv, cache, block_table, max_pages_per_seq, start_pos, row_offsets, total_tokens, run, B, Hkv, page_size,
+            num_pages, status_flag);
+    else
+        kv_bulk_q4_kernel<D, G, false><<<grid, kBulkThreads, 0, stream>>>(
+            kk, vv, cache, block_table, max_pages_per_seq, start_pos, row_offsets, total_tokens, run, B, Hkv, page_size,
+            num_pages, status_flag);
     return cudaGetLastError();
 }
 

@@ -25,26 +25,63 @@ __device__ __forceinline__ uint32_t bf16x2_min_abs_nan(uint32_t a, uint32_t b) {
     return r;
 }
 
+// Two fp32 values in a 64-bit register, operated on by one instruction (each half rounded as on its own).
+__device__ __forceinline__ uint64_t f32x2(float lo, float hi) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+    return r;
+}
+__device__ __forceinline__ void f32x2_split(uint64_t v, float& lo, float& hi) {
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v));
+}
+__device__ __forceinline__ uint64_t f32x2_add(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ uint64_t f32x2_mul(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ uint64_t f32x2_fma(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+
 // What the fast path below cannot decide; out of line, so that it costs the fast path no registers.
 __device__ __noinline__ inline uint32_t q4_scale_f64(float lo, float hi) {
     const double range = __dsub_rn(static_cast<double>(hi), static_cast<double>(lo));
     const float s32 = __double2float_rn(__ddiv_rn(range, 15.0));
     return pack_bf16x2(s32, 0.0f) & 0x7FFFu;               // a group of both zeros may give -0: the scale is +0
 }
-__device__ __noinline__ inline float q4_code_slow(float x, float lo, float s, float r) {
-    if (!(s > 0.0f)) return 0.0f;
+__device__ __noinline__ inline uint32_t q4_code_f64(float x, float lo, float s) {
+    const double q = __ddiv_rn(__dsub_rn(static_cast<double>(x), static_cast<double>(lo)), static_cast<double>(s));
+    return static_cast<uint32_t>(fminf(static_cast<float>(rint(q)), 15.0f));
+}
+__device__ __forceinline__ uint32_t q4_code_slow(float x, float lo, float s, float r) {
     const float t = __fsub_rn(x, lo), back = __fsub_rn(t, x);               // TwoSum: what t lost
     const float lost = __fadd_rn(__fsub_rn(x, __fsub_rn(t, back)), __fsub_rn(-lo, back));
-    if (s >= 0x1p-100f && lost == 0.0f) {                                   // (lost is NaN where t overflowed)
-        // c is off by one at most; d = t - c s is exact
-        float c = rintf(__fmul_rn(t, r));
-        const float d = __fmaf_rn(-c, s, t), half = 0.5f * s;
-        const bool odd = static_cast<int>(c) & 1;
-        if (fabsf(d) > half || (fabsf(d) == half && odd)) c += d > 0.0f ? 1.0f : -1.0f;
-        return c;
+    if (!(s >= 0x1p-100f && lost == 0.0f)) return q4_code_f64(x, lo, s);    // (lost is NaN where t overflowed)
+    // c is off by one at most; d = t - c s is exact
+    const float c = rintf(__fmul_rn(t, r));
+    const float d = __fmaf_rn(-c, s, t), half = 0.5f * s;
+    uint32_t code = static_cast<uint32_t>(c);
+    if (fabsf(d) > half || (fabsf(d) == half && (code & 1u))) code += d > 0.0f ? 1u : 0xffffffffu;
+    return code;
+}
+// Eight codes, side by side, of four words of two bf16 each.
+__device__ __noinline__ inline uint32_t q4_codes_slow(uint32_t x0, uint32_t x1, uint32_t x2, uint32_t x3, float lo, float s, float r) {
+    if (!(s > 0.0f)) return 0u;
+    uint32_t codes = 0u;
+#pragma unroll 1
+    for (int w = 0; w < 4; ++w) {
+        const uint32_t x = w == 0 ? x0 : w == 1 ? x1 : w == 2 ? x2 : x3;
+        codes |= (q4_code_slow(__uint_as_float(x << 16), lo, s, r) |
+                  (q4_code_slow(__uint_as_float(x & 0xFFFF0000u), lo, s, r) << 4)) << (8 * w);
     }
-    const double q = __ddiv_rn(__dsub_rn(static_cast<double>(x), static_cast<double>(lo)), static_cast<double>(s));
-    return fminf(static_cast<float>(rint(q)), 15.0f);
+    return codes;
 }
 
 // Quantises W words of two bf16 per lane.  A group is the elements of LANES consecutive, aligned lanes, all of
@@ -92,30 +129,28 @@ __device__ __forceinline__ uint32_t q4_quantise(const uint32_t (&x)[W], uint32_t
     float r;
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(s));
     constexpr float kMagic = 12582912.0f;                  // 1.5 * 2^23: adding it rounds to an integer
-    float c[2 * W];                                        // code + kMagic
+    // Codes side by side: the bits of code + kMagic are those of kMagic plus the code, whose multiples come off at the end.
+    constexpr uint32_t kEight = 0x11111111u, kBits = 0x4B400000u;
+    constexpr uint32_t kMagics = kBits * (W >= 4 ? kEight : kEight & ((1u << (8 * (W % 4))) - 1u));
 #pragma unroll
-    for (int e = 0; e < 2 * W; ++e) {
-        const float f = __uint_as_float((e & 1) ? (x[e >> 1] & 0xFFFF0000u) : (x[e >> 1] << 16));
-        const float t = __fsub_rn(f, lo), q = __fmul_rn(t, r);
-        c[e] = __fadd_rn(__fmaf_rn(__fmaf_rn(-q, s, t), r, q), kMagic);
+    for (int w = 0; w < W; ++w) {
+        const uint64_t t = f32x2_add(f32x2(__uint_as_float(x[w] << 16), __uint_as_float(x[w] & 0xFFFF0000u)), f32x2(-lo, -lo));
+        const uint64_t q = f32x2_mul(t, f32x2(r, r));
+        const uint64_t near = f32x2_fma(f32x2_fma(q, f32x2(-s, -s), t), f32x2(r, r), q);
+        float c0, c1;
+        f32x2_split(f32x2_add(near, f32x2(kMagic, kMagic)), c0, c1);
+        packed[w / 4] += (__float_as_uint(c0) << (8 * (w % 4))) + (__float_as_uint(c1) << (8 * (w % 4) + 4));
     }
+#pragma unroll
+    for (int w = 0; w < (W + 3) / 4; ++w) packed[w] -= kMagics;
     const float small = fminf(fabsf(__uint_as_float(least << 16)), fabsf(__uint_as_float(least & 0xFFFF0000u)));
     const bool plain = s >= 0x1p-100f && s32 < INFINITY;
     if (!(plain && fminf(small, lo == 0.0f ? INFINITY : fabsf(lo)) >= s * 0x1p-12f)) {
 #pragma unroll
-        for (int e = 0; e < 2 * W; ++e)
-            c[e] = kMagic + q4_code_slow(__uint_as_float((e & 1) ? (x[e >> 1] & 0xFFFF0000u) : (x[e >> 1] << 16)), lo, s, r);
-    }
-    // Codes side by side: the bits of c are those of kMagic plus the code, whose multiples come off at the end.
-#pragma unroll
-    for (int w = 0; w < (W + 3) / 4; ++w) {
-        uint32_t sum = 0u, magics = 0u;
-#pragma unroll
-        for (int e = 0; e < 8 && 8 * w + e < 2 * W; ++e) {
-            sum += __float_as_uint(c[8 * w + e]) << (4 * e);
-            magics += 0x4B400000u << (4 * e);
+        for (int w = 0; w < W; w += 4) {
+            packed[w / 4] = q4_codes_slow(x[w], x[w + 1 < W ? w + 1 : w], x[w + 2 < W ? w + 2 : w], x[w + 3 < W ? w + 3 : w], lo, s, r);
+            if (w + 4 > W) packed[w / 4] &= (1u << (8 * (W - w))) - 1u;
         }
-        packed[w] = sum - magics;
     }
     // -0 and +0 compare equal, so the minimum of a group that holds both is either; it is kept as +0
     const uint32_t m16 = lo == 0.0f ? 0u : __float_as_uint(lo) >> 16;
@@ -199,31 +234,6 @@ __device__ __forceinline__ void mma_f16_16816_zero(float (&d)[4], uint32_t a0, u
 __device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi) {
     uint32_t r;
     asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
-    return r;
-}
-
-// Two fp32 values in a 64-bit register, operated on by one instruction (each half rounded as on its own).
-__device__ __forceinline__ uint64_t f32x2(float lo, float hi) {
-    uint64_t r;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
-    return r;
-}
-__device__ __forceinline__ void f32x2_split(uint64_t v, float& lo, float& hi) {
-    asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v));
-}
-__device__ __forceinline__ uint64_t f32x2_add(uint64_t a, uint64_t b) {
-    uint64_t r;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-    return r;
-}
-__device__ __forceinline__ uint64_t f32x2_mul(uint64_t a, uint64_t b) {
-    uint64_t r;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-    return r;
-}
-__device__ __forceinline__ uint64_t f32x2_fma(uint64_t a, uint64_t b, uint64_t c) {
-    uint64_t r;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
     return r;
 }
 
