@@ -988,7 +988,7 @@ int ac_decode_plan_q4(const int32_t* token_counts_host, int B, int Hq, int Hkv, 
     if (sm_count <= 0) sm_count = g_last_sm_count > 0 ? g_last_sm_count : 148;
     // Every split count is priced by what the launch it gives (q4_attn.cu) was measured to do: the whole GPU moves
     // 5.6 TB/s of this cache (its arithmetic keeps it below HBM's rate), one CTA alone on its SM 43 GB/s with twelve warps
-    // and 32 with six, two sharing an SM 19 each, in a ragged batch 25; a wave costs 4 us of start and end, a further one
+    // and 32 with six, two sharing an SM 20 each, in a ragged batch 25; a wave costs 4 us of start and end, a further one
     // 3, the merge through the workspace 1.6 and the partial results' traffic.  (d/2 + 4 d/group bytes per token, side
     // and head; the plan does not know the group and takes 64.)
     const double bytes_per_token = 2.0 * (d / 2 + d / 16), gpu = 5.6e12 * sm_count / 148.0;
@@ -1025,7 +1025,7 @@ int ac_decode_plan_q4(const int32_t* token_counts_host, int B, int Hq, int Hkv, 
         }
         n *= Hkv;
         const bool fat = static_cast<long long>(B) * Hkv * cand <= sm_count;
-        const double rate = fat ? 43e9 : n <= sm_count ? 32e9 : n * longest * bytes_per_token > 1.25 * total ? 25e9 : 19e9;
+        const double rate = fat ? 43e9 : n <= sm_count ? 32e9 : n * longest * bytes_per_token > 1.25 * total ? 25e9 : 20e9;
         const double alone = longest * bytes_per_token / rate, together = total / gpu;
         double t = (alone > together ? alone : together) + 4e-6;
         if (n > 2.0 * sm_count) t += (ceil(n / (2.0 * sm_count)) - 1.0) * 3e-6;

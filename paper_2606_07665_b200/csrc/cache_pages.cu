@@ -1,10 +1,12 @@
 // Page bookkeeping and page copies: reserve, fork, release, compact, copy.
 //
-// The bookkeeping kernels hand out free pages lowest index first.  A single CTA walks the reference counts in
-// order, 16 pages per thread and step, and turns the free (or live) ones into ranks by a scan over the CTA; it
-// stops as soon as it has what the call needs.  Bound: latency (a few dependent passes over num_pages * 4 bytes
-// that sit in L2).  The copies are bound by HBM: a warp moves pieces of up to 4 KB, 16 bytes a lane, eight loads in
-// flight before the first store.
+// The bookkeeping kernels hand out free pages lowest index first.  For reserve and fork a single CTA walks the reference
+// counts in order, 16 pages per thread and step, and turns the free ones into ranks by a scan over the CTA; it stops as
+// soon as it has what the call needs.  Compaction needs every live page's rank: CTAs count and rank a chunk of the
+// counts each, in two launches.  Bound: latency (a few dependent passes over num_pages * 4 bytes that sit in L2): 8 forks
+// 7.9 us with their copies, the compaction of a pool of 512 pages 6.5.  The copies are bound by HBM, which reads and writes: a warp
+// moves pieces of up to 4 KB, 16 bytes a lane, eight loads in flight before the first store; a compaction that moves
+// 0.65 GB (1.3 GB read and written) takes 222 us = 5870 GB/s, 0.90 of the measured 6546.
 #include "ac_device.cuh"
 #include "ac_internal.h"
 
