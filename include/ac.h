@@ -506,7 +506,8 @@ int ac_kv_load_q4(void* k, void* v, const ac_q4_cache* cache, const int32_t* blo
 
 /* Split plan for ac_paged_decode_attn_q4: arguments and outputs as ac_decode_plan_for_lengths, except that
  * token_counts_host may be NULL (every row then counts max_context_len tokens) and the workspace is the
- * one of the fused merge (ac_fused_workspace_bytes).  Host only, pure; any plan gives the same results. */
+ * one of the fused merge (ac_fused_workspace_bytes).  Host only, pure; any plan is valid, results of different
+ * split counts differ in their low bits. */
 int ac_decode_plan_q4(const int32_t* token_counts_host, int B, int Hq, int Hkv, int d, int page_size,
                       int max_context_len, int sm_count, int* num_splits_out, int* split_tokens_out,
                       size_t* workspace_bytes_out);
