@@ -285,6 +285,14 @@ class _OnDevice:
             torch.cuda.current_stream().synchronize()      # zeroed whatever stream the calls run on
         self._flag = self.status_flag.data_ptr()
 
+    def _new(self, shape, stream, dtype=torch.bfloat16):
+        """A tensor that belongs to the stream that will write it, so that its memory is not handed to another one's work
+        while that stream still uses it."""
+        if stream is None:
+            return torch.empty(shape, dtype=dtype, device=self.device)
+        with torch.cuda.stream(torch.cuda.ExternalStream(stream, device=self.device) if isinstance(stream, int) else stream):
+            return torch.empty(shape, dtype=dtype, device=self.device)
+
     def _enqueue(self, name, args, stream, at):
         """Calls the library with the device current; args are marshalled but for the stream, which goes in at `at`."""
         if _current_device() != self._index:
@@ -388,7 +396,7 @@ class PagedAttention(_Rows):
         """q: rotated queries [B, Hq, d] bf16; returns out [B, Hq, d] bf16 (allocated unless given)."""
         _want(q, "q", self._q_shape, _BF16, self.device)
         if out is None:
-            out = torch.empty_like(q)
+            out = self._new(self._q_shape, stream, q.dtype)
         else:
             _want(out, "out", self._q_shape, _BF16, self.device)
         args = self._args.copy()
@@ -461,8 +469,8 @@ class Q4Cache(_OnDevice):
             if total_tokens is None:
                 raise ValueError("load needs total_tokens or both outputs")
             shape = (total_tokens, self.Hkv, self.d)
-            k_out = torch.empty(shape, dtype=torch.bfloat16, device=self.device) if k_out is None else k_out
-            v_out = torch.empty(shape, dtype=torch.bfloat16, device=self.device) if v_out is None else v_out
+            k_out = self._new(shape, stream) if k_out is None else k_out
+            v_out = self._new(shape, stream) if v_out is None else v_out
         self._bulk("ac_kv_load_q4", k_out, v_out, block_table, start_pos, row_offsets, stream)
         return k_out, v_out
 
@@ -514,7 +522,7 @@ class Q4DecodeStep(_Rows):
         _want(k_new, "k_new", self._kv_shape, _BF16, self.device)
         _want(v_new, "v_new", self._kv_shape, _BF16, self.device)
         if q_out is None:
-            q_out = torch.empty_like(q_in)
+            q_out = self._new(self._q_shape, stream, q_in.dtype)
         elif q_out is not q_in:
             _want(q_out, "q_out", self._q_shape, _BF16, self.device)
         args = self._append_args.copy()
@@ -526,7 +534,7 @@ class Q4DecodeStep(_Rows):
         """q: rotated queries [B, Hq, d] bf16; returns out [B, Hq, d] bf16 (allocated unless given)."""
         _want(q, "q", self._q_shape, _BF16, self.device)
         if out is None:
-            out = torch.empty_like(q)
+            out = self._new(self._q_shape, stream, q.dtype)
         else:
             _want(out, "out", self._q_shape, _BF16, self.device)
         args = self._attn_args.copy()

@@ -134,7 +134,8 @@ def with_specials(rng, x):
 
 @pytest.mark.parametrize("d,group", [(128, 128), (128, 64), (128, 32), (64, 64), (64, 32)])
 @pytest.mark.parametrize("layout", ["token_major", "head_major"])
-@pytest.mark.parametrize("total_heads,ps,lens", [(1, 16, [0]), (3, 32, [5, 0, 0, 33, 64]), (8, 48, [100, 1, 17])])
+@pytest.mark.parametrize("total_heads,ps,lens", [(1, 16, [0]), (3, 32, [5, 0, 0, 33, 64]), (8, 48, [100, 1, 17]),
+                                                  (40, 16, [3, 0, 18]), (1, 64, [700, 0, 331])])
 def test_store_and_load(rt, d, group, layout, total_heads, ps, lens):
     import torch
     rng = np.random.default_rng(5)
@@ -364,6 +365,34 @@ def test_attention_two_objects_on_two_streams(rt):
             h.attention(q, out=o[i], stream=st)
     torch.cuda.synchronize()
     assert all(torch.equal(o, want) for os in outs for o in os)
+
+
+@pytest.mark.parametrize("handle", [False, True])
+def test_results_belong_to_the_stream_that_writes_them(rt, handle):
+    """Memory of a result (and of the step's rotated queries, which nobody holds) that is dropped while another stream still
+    writes it must not go to the current stream's next tensor."""
+    import torch
+    c = Case(rt, 41, [700, 300], 8, 2, 64, 16, 64)
+    cache = c.upload(rt)
+    cos, sin = W.rope_table(1024, 64, 10000.0)
+    h = rt.Q4DecodeStep(cache, dev(c.table), dev(c.lens), 8, lens_host=c.lens, rope_cos=dev(cos), rope_sin=dev(sin))
+    q, k, v = (dev(bits(c.rng, 2, n, 64)).view(torch.bfloat16) for n in (8, 2, 2))
+    start, off = dev(np.zeros(2, dtype=np.int32)), dev(np.array([0, 4, 8], dtype=np.int32))
+    want = h.step(q, k, v)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    stream = side.cuda_stream if handle else side
+    made = []
+    own = h._new
+    h._new = cache._new = lambda *a: made.append(own(*a)) or made[-1]
+    got = h.step(q, k, v, stream=stream)
+    cache.load(dev(c.table), start, off, 8, stream=stream)
+    torch.cuda.synchronize()
+    assert torch.equal(got, want) and len(made) == 4
+    where = {t.data_ptr() for t in made}
+    shapes = [t.shape for t in made]
+    del made, got
+    assert not where & {t.data_ptr() for t in [torch.empty(s, dtype=torch.bfloat16, device="cuda") for s in shapes]}
 
 
 def test_append_in_place_rotates_the_queries_where_they_are(rt):
