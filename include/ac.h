@@ -99,9 +99,9 @@ int ac_sm_count(void);
  * small cost model (bandwidth of one CTA, waves of CTAs, partial-result traffic); splits are never
  * shorter than 256 tokens, or 128 where the grid is small enough for the merge inside a cluster.  max_context_len = the largest number of tokens any row attends over in this bucket
  * (cached + new).  Outputs: *num_splits_out >= 1, *split_tokens_out = tokens per split (a multiple
- * of 64; split s of row b covers tokens [s*split_tokens, min((s+1)*split_tokens, n_b)) ), and
- * *workspace_bytes_out = bytes of fp32 workspace the attention + merge calls need for that plan
- * (0 when num_splits == 1).  The paper's kernel merges across CTAs inside the attention kernel and
+ * of 64; split s of row b covers tokens [s*split_tokens, min((s+1)*split_tokens, n_b)), the last one
+ * all that are left), and *workspace_bytes_out = bytes of fp32 workspace the attention + merge calls
+ * need for that plan (0 when num_splits == 1).  The paper's kernel merges across CTAs inside the attention kernel and
  * does not state how it sizes the split; this heuristic is this library's own. */
 int ac_decode_plan(int B, int Hq, int Hkv, int d, int page_size, int max_context_len, int sm_count,
                    int* num_splits_out, int* split_tokens_out, size_t* workspace_bytes_out);
@@ -251,7 +251,9 @@ int ac_oproj_residual_rmsnorm(const void* attn_out, const void* w_o, int K, int 
  *   partial_lse = partial_o + B*Hq*num_splits*d          [B,Hq,num_splits]  natural-log
  * log-sum-exp of the scaled scores; a split with no tokens writes lse = -inf and leaves its
  * partial_o untouched.  workspace_bytes must be >= ac_workspace_bytes(B,Hq,d,num_splits).
- * max_context_len must be >= every n_b (tokens beyond num_splits*split_tokens are not visited).
+ * max_context_len sizes the splits (split_tokens = ac_split_tokens(max_context_len, num_splits)): it should be
+ * >= every n_b.  Where a row is longer all the same, its last split takes the rest: the result is that
+ * of the whole row, the call only takes longer.
  * Contents of cache slots at or past n_b, of unreferenced pages and of unused block-table entries
  * never influence the result.  A page id outside [0, num_pages) reads as zeros. */
 int ac_paged_decode_attn(const void* q_rot, const void* k_cache, const void* v_cache,

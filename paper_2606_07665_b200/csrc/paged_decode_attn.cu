@@ -226,8 +226,11 @@ __global__ void __launch_bounds__(NW * 32, NW == kFatWarps ? 1 : 2) paged_decode
 #pragma unroll
         for (int s = 0; s < STAGES; ++s) page_first[s] = load_page_id(s);     // the range moved
     }
-    const int tok_end = SINKS ? min((split + 1) * p.split_tokens, n_tokens - window_base)
-                              : min(window_base + (split + 1) * p.split_tokens, n_tokens);
+    // The last split goes on to the row's end, so that a row that has outgrown the plan is slower, not cut off.  (The fused
+    // step keeps to the grid: it cannot append a token beyond it, and says so in the status word.)
+    const int row_end = SINKS ? n_tokens - window_base : n_tokens;
+    const int grid_end = SINKS ? (split + 1) * p.split_tokens : window_base + (split + 1) * p.split_tokens;
+    const int tok_end = ROPE == ROPE_NONE && split == S - 1 ? row_end : min(grid_end, row_end);
 
     // Programmatic launch completion is signalled only AFTER this CTA has synchronised on the
     // preceding kernel (dependency_sync below).  The next kernel of the stream (launched with the
@@ -788,7 +791,7 @@ __global__ void __launch_bounds__(NW * 32, NW == kFatWarps ? 1 : 2) paged_decode
         // ---- fused merge inside a cluster: split 0 reads the other splits' staged results out of
         // their shared memory.  No global round trip, no ticket; CTAs whose split has no tokens pass
         // through the same two barriers and nothing else.
-        // splits with tokens, <= 16 (a row longer than the split grid covers still has S of them)
+        // splits with tokens, <= 16 (a row longer than the plan expected still has S of them)
         const int n_active = min(S, (n_tokens - window_base + p.split_tokens - 1) / p.split_tokens);
         cluster_sync_all();                              // every staged result is written and visible
         if (split == 0) {
@@ -839,7 +842,7 @@ __global__ void __launch_bounds__(NW * 32, NW == kFatWarps ? 1 : 2) paged_decode
     // Publish this CTA's partials, take a ticket, and let the holder of the last ticket do the merge.
     // Nobody waits for anybody: CTAs that are not last simply exit.
     __shared__ int s_is_last;
-    // splits with tokens (a row longer than the split grid covers still has S of them)
+    // splits with tokens (a row longer than the plan expected still has S of them)
     const int n_active = min(S, (n_tokens - window_base + p.split_tokens - 1) / p.split_tokens);
     // One acquire-release atomic by one thread, bracketed by CTA barriers: the release orders the
     // partials that every thread of this CTA stored before the first barrier ahead of the ticket, the

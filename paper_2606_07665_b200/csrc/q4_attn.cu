@@ -132,7 +132,8 @@ __global__ void __launch_bounds__(NW * 32, CTAS) paged_decode_attn_q4_kernel(con
     }
     const int range_tokens = n_tokens - window_base;
     const int tok_begin = split * p.split_tokens;
-    const int tok_end = min((split + 1) * p.split_tokens, range_tokens);
+    // The last split goes on to the row's end: a row that has outgrown the plan is slower, not cut off.
+    const int tok_end = split == S - 1 ? range_tokens : min((split + 1) * p.split_tokens, range_tokens);
 
     auto dependency_sync = [&]() {
         cudaGridDependencySynchronize();

@@ -328,7 +328,8 @@ class _Rows(_OnDevice):
     def plan(self, lens_host=None, max_context_len=None, num_splits=None, row_order="auto"):
         """Chooses the splits.  ``lens_host``: the rows' cached tokens on the host (< 0: inactive), as the scheduler
         that built context_lens has them; without them every row counts ``max_context_len`` tokens (default: what
-        the block table can hold).  Plan again when the lengths outgrow max_context_len."""
+        the block table can hold).  Plan again when the lengths outgrow max_context_len: the last split takes what lies
+        beyond it, which is right but slow."""
         if lens_host is not None and len(lens_host) != self.B:
             raise ValueError(f"{len(lens_host)} lengths for {self.B} rows")
         if max_context_len is None:
