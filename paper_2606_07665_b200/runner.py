@@ -255,6 +255,10 @@ class AttentionBlockStep:
 #
 # They validate once what stays (pools, tables, lengths) and per call what changes, keep the plan, the workspace
 # and the marshalled arguments, and enqueue on the current stream of their device (or on the one given).
+#
+# What an object allocates for itself stays allocated until every stream that it was used on is done with it, and for as long as the
+# object lives where a captured call uses it.  So plan() and the end of an object need no synchronisation; only a captured
+# graph must not be replayed beyond the object that it calls, and a stream given as a handle must outlive the object.
 
 _BF16 = (torch.bfloat16, torch.int16)          # bf16 values, or their bits
 
@@ -273,17 +277,36 @@ def _want(t, name, shape, dtypes, device):
 
 
 class _OnDevice:
-    """A device, ac_init on it, and its streams."""
+    """A device, ac_init on it, its streams, and what belongs to the calls on them."""
 
     def _bind(self, device):
         if device.type != "cuda":
             raise ValueError(f"tensors on {device}, expected a CUDA device")
         self.device, self._index, self._lib = device, device.index, ac.lib()
+        self._streams, self._captured, self._kept = set(), False, []
         with torch.cuda.device(device):
             ac.ac_init(device.index)
             self.status_flag = torch.zeros(1, dtype=torch.int32, device=device)
             torch.cuda.current_stream().synchronize()      # zeroed whatever stream the calls run on
         self._flag = self.status_flag.data_ptr()
+
+    def _buffers(self):
+        """The tensors that calls use and nobody else holds."""
+        return [self.status_flag]
+
+    def _used_on(self, stream):
+        """The buffers are in use on this stream (a handle) from now on; their memory must not go to anything else before
+        that stream is past the call (the allocator looks at this when it gets them back)."""
+        self._streams.add(stream)
+        used = torch.cuda.ExternalStream(stream, device=self.device)
+        for t in self._buffers():
+            t.record_stream(used)
+
+    def _replace_buffers(self):
+        """Before the buffers are replaced: captured calls go on using the present ones."""
+        if self._captured:
+            self._kept.append(self._buffers())
+        self._streams, self._captured = set(), False
 
     def _new(self, shape, stream, dtype=torch.bfloat16):
         """A tensor that belongs to the stream that will write it, so that its memory is not handed to another one's work
@@ -298,10 +321,16 @@ class _OnDevice:
         if _current_device() != self._index:
             with torch.cuda.device(self.device):
                 return self._enqueue(name, args, stream, at)
+        current = _raw_stream(self._index)
         if stream is None:
-            args[at] = _raw_stream(self._index)
-        else:
-            args[at] = stream if isinstance(stream, int) else stream.cuda_stream
+            stream = current
+        elif not isinstance(stream, int):
+            stream = stream.cuda_stream
+        args[at] = stream
+        if stream not in self._streams:
+            self._used_on(stream)
+        if not self._captured:
+            self._captured = _current_is_captured() if stream == current else _is_captured(stream)
         status = getattr(self._lib, name)(*args)
         if status != 0:
             raise ac.AcError(status, name)
@@ -310,10 +339,22 @@ class _OnDevice:
 # the current device and stream without the wrappers (a microsecond per call)
 _current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda i: torch.cuda.current_stream(i).cuda_stream)
+_current_is_captured = getattr(torch._C, "_cuda_isCurrentStreamCapturing", None) or torch.cuda.is_current_stream_capturing
+
+
+def _is_captured(stream):
+    """Whether this stream (a handle) is being captured into a graph."""
+    with torch.cuda.stream(torch.cuda.ExternalStream(stream)):
+        return torch.cuda.is_current_stream_capturing()
 
 
 class _Rows(_OnDevice):
     """A block table and context lengths, and the split plan of attention over them."""
+
+    workspace = row_order = None
+
+    def _buffers(self):
+        return [t for t in (self.status_flag, self.workspace, self.row_order) if t is not None]
 
     def _rows(self, block_table, context_lens, page_size, num_pages, Hq, Hkv, d):
         B = context_lens.shape[0]
@@ -329,7 +370,7 @@ class _Rows(_OnDevice):
         """Chooses the splits.  ``lens_host``: the rows' cached tokens on the host (< 0: inactive), as the scheduler
         that built context_lens has them; without them every row counts ``max_context_len`` tokens (default: what
         the block table can hold).  Plan again when the lengths outgrow max_context_len: the last split takes what lies
-        beyond it, which is right but slow."""
+        beyond it, which is right but slow.  Graphs captured before keep the plan that they were captured under."""
         if lens_host is not None and len(lens_host) != self.B:
             raise ValueError(f"{len(lens_host)} lengths for {self.B} rows")
         if max_context_len is None:
@@ -341,6 +382,7 @@ class _Rows(_OnDevice):
         with torch.cuda.device(self.device):
             if num_splits is None:
                 num_splits = self._choose(counts, span)
+            self._replace_buffers()
             self.num_splits = int(num_splits)
             self.workspace_bytes = ac.ac_fused_workspace_bytes(self.B, self.Hq, self.Hkv, self.d, self.num_splits)
             self.workspace = torch.zeros(max(self.workspace_bytes, 16) // 4, dtype=torch.float32, device=self.device)
@@ -362,7 +404,8 @@ class PagedAttention(_Rows):
     """Decode attention over a bf16 cache of the caller's, with an optional sliding window and sinks.
 
     ``k_cache``, ``v_cache``: [num_pages, page_size, Hkv, d] ("token_major") or [num_pages, Hkv, page_size, d].  The
-    object owns its workspace: its calls must not overlap on the GPU (one object per stream)."""
+    object owns its workspace: its calls, and replays of graphs captured from them, must not overlap on the GPU (one
+    object per stream)."""
 
     def __init__(self, k_cache, v_cache, block_table, context_lens, Hq, lens_host=None, window=0, sinks=0,
                  max_context_len=None, num_splits=None, row_order="auto", layout="token_major", softmax_scale=0.0,
@@ -437,7 +480,14 @@ class Q4Cache(_OnDevice):
         shape = (num_pages, page_size, Hkv, d // 2) if layout == "token_major" else (num_pages, Hkv, page_size, d // 2)
         k, v = (torch.zeros(shape, dtype=torch.uint8, device=device) for _ in range(2))
         params = torch.zeros((num_pages, Hkv, page_size, 2, d // group, 2), dtype=torch.bfloat16, device=device)
-        return cls(k, v, params, layout=layout)
+        cache = cls(k, v, params, layout=layout)
+        cache._allocated = (k, v, params)
+        return cache
+
+    _allocated = ()
+
+    def _buffers(self):
+        return [self.status_flag, *self._allocated]
 
     @property
     def pools(self):
@@ -481,7 +531,7 @@ class Q4DecodeStep(_Rows):
 
     ``rope_variants``: rotary_dim, interleaved, q_norm_weight, k_norm_weight, norm_eps as in
     ``ac_rope_kv_append_ex``; the rope tables are only needed for ``append`` and ``step``.  The object owns its
-    workspace: its calls must not overlap on the GPU (one object per stream)."""
+    workspace: its calls, and replays of graphs captured from them, must not overlap on the GPU (one object per stream)."""
 
     def __init__(self, cache, block_table, context_lens, Hq, lens_host=None, window=0, sinks=0, rope_cos=None,
                  rope_sin=None, max_context_len=None, num_splits=None, row_order="auto", rope_variants=None,
@@ -500,6 +550,9 @@ class Q4DecodeStep(_Rows):
             for t, what in ((rope_cos, "rope_cos"), (rope_sin, "rope_sin")):
                 _want(t, what, (rope_cos.shape[0], rotary // 2), (torch.float32,), self.device)
         self.plan(lens_host, max_context_len, num_splits, row_order)
+
+    def _buffers(self):
+        return super()._buffers() + self.cache._buffers()
 
     def _choose(self, counts, span):
         return ac.ac_decode_plan_q4(counts, self.B, self.Hq, self.Hkv, self.d, self.page_size, span)[0]
@@ -576,6 +629,9 @@ class CachePages(_OnDevice):
         self.workspace = torch.empty(ac.ac_cache_workspace_bytes(self.rows, self.num_pages, self.rows),
                                      dtype=torch.uint8, device=self.device)
         self._room = (self.workspace.data_ptr(), self.workspace.numel())
+
+    def _buffers(self):
+        return [self.status_flag, self.workspace]
 
     def reserve(self, new_tokens, stream=None):
         """Pages for new_tokens more tokens of every active row, lowest free page first, rows in order."""
