@@ -1065,8 +1065,12 @@ int ac_paged_decode_attn_q4(const void* q_rot, const ac_q4_cache* cache, const i
     st = parse_q4_cache(cache, s, &view);
     if (st != AC_OK) return st;
     if (!aligned16(q_rot) || !aligned16(out)) return AC_ERR_ALIGN;
-    // the kernel keeps a granule's place as 32 bits: 16-byte units in the code pools, granules in the parameters
-    if (view.stride_page > (1ll << 36) / num_pages ||
+    // the kernel keeps a granule's place as 32 bits: 16-byte units in the code pools, granules in the parameters.  (No
+    // product below is formed before it is known to stay within the limit: strides are the caller's.)
+    constexpr int64_t kReach = (1ll << 36) - 16;           // the last place that 32 bits of 16-byte units reach
+    const int64_t pages = num_pages - 1, tokens = page_size - 16;
+    if ((pages > 0 && view.stride_page > kReach / pages) || (tokens > 0 && view.stride_token > kReach / tokens) ||
+        pages * (pages > 0 ? view.stride_page : 0) + tokens * (tokens > 0 ? view.stride_token : 0) > kReach ||
         static_cast<long long>(num_pages) * Hkv * (page_size / 16) > 0xffffffffll)
         return AC_ERR_UNSUPPORTED;
     float* partial_o = nullptr;

@@ -1,0 +1,39 @@
+"""Host-side guards, no GPU: sizes at which 32 bits end."""
+import pytest
+
+P = 0x10000            # fake, aligned, never dereferenced: every call below is refused before a launch
+UNSUPPORTED, WORKSPACE = 3, 5
+
+
+@pytest.fixture(scope="module")
+def ac():
+    from paper_2606_07665_b200 import binding, build
+    build.build()
+    binding.lib()
+    return binding
+
+
+def attention(ac, num_pages, ps, page, token, head):
+    c = ac.AcQ4Cache(P, P, P, page, token, head, 64)
+    return ac.lib().ac_paged_decode_attn_q4(P, c, P, 33, P, 1, 0.0, 4, None, 0, P, 1, 8, 2, 64, ps, num_pages, 513, None, None, None)
+
+
+@pytest.mark.parametrize("num_pages,ps,page,token,head", [
+    (64, 16, 1 << 31, 64, 32),                        # pages far apart
+    (1 << 20, 64, 64, 64 << 20, 32),                  # slot-major: 64 slots of a million pages' 64 bytes, 2^38 bytes
+    (2, 256, 1 << 10, 1 << 29, 32),                   # a token stride that no page stride explains
+    (2, 256, 1 << 62, 1 << 62, 32),                   # products past 64 bits
+    (1 << 30, 256, 1 << 40, 1 << 40, 32),
+    (2, 32, 64, (1 << 36) // 16 + 16, 32)])           # just past the border
+def test_code_pools_of_more_than_36_bits_are_refused(ac, num_pages, ps, page, token, head):
+    assert attention(ac, num_pages, ps, page, token, head) == UNSUPPORTED
+
+
+@pytest.mark.parametrize("num_pages,ps,page,token,head", [
+    (1, 16, 1 << 60, 64, 32),                         # one page: its stride is never used
+    (2, 16, 1 << 35, 1 << 60, 32),                    # one granule per page: the token stride stays in 64 bits
+    (1 << 18, 64, 64, 64 << 18, 32),                  # slot-major, 2^30 bytes
+    (2, 32, 64, (1 << 36) // 16 - 16, 32)])           # just within
+def test_code_pools_within_36_bits_pass_that_guard(ac, num_pages, ps, page, token, head):
+    # what stops them here is the workspace that four splits want, looked at after the pools
+    assert attention(ac, num_pages, ps, page, token, head) == WORKSPACE
