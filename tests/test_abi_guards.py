@@ -20,7 +20,7 @@ def attention(ac, num_pages, ps, page, token, head):
 
 @pytest.mark.parametrize("num_pages,ps,page,token,head", [
     (64, 16, 1 << 31, 64, 32),                        # pages far apart
-    (1 << 20, 64, 64, 64 << 20, 32),                  # slot-major: 64 slots of a million pages' 64 bytes, 2^38 bytes
+    (1 << 20, 64, 1 << 12, 1 << 32, 32),              # slot-major: 64 slots of a million pages' 4096 bytes, 2^38 bytes
     (2, 256, 1 << 10, 1 << 29, 32),                   # a token stride that no page stride explains
     (2, 256, 1 << 62, 1 << 62, 32),                   # products past 64 bits
     (1 << 30, 256, 1 << 40, 1 << 40, 32),
