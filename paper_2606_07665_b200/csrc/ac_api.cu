@@ -261,7 +261,7 @@ static int plan_splits(int B, int Hq, int Hkv, int d, int page_size, int max_con
     } else {
         // Splits are at least 256 tokens long -- 128 where the merge is the cheap one inside a cluster
         // (small grids, where nothing but latency is at stake).
-        int s_max = (max_context_len + 63) / 64;            // the chunk-length test below does the limiting
+        int s_max = (max_context_len - 1) / 64 + 1;         // the chunk-length test below does the limiting
         if (s_max > 4096) s_max = 4096;
         if (token_counts != nullptr && static_cast<long long>(s_max) * B > 4000000ll) {
             s_max = static_cast<int>(4000000ll / B);      // bound the host work of the scan
@@ -287,7 +287,7 @@ static int plan_splits(int B, int Hq, int Hkv, int d, int page_size, int max_con
                     int t = token_counts[b];
                     if (t <= 0) continue;
                     if (t > max_context_len) t = max_context_len;
-                    pieces += (t + chunk - 1) / chunk;
+                    pieces += (t - 1) / chunk + 1;
                     const int m = t < chunk ? t : chunk;
                     if (m > most) most = m;
                 }
@@ -1004,7 +1004,7 @@ int ac_decode_plan_q4(const int32_t* token_counts_host, int B, int Hq, int Hkv, 
     total *= Hkv * bytes_per_token;
     long long S = 1;
     double best = 0.0;
-    long long most = (max_context_len + 255) / 256;                  // splits of at least 256 tokens
+    long long most = (max_context_len - 1) / 256 + 1;                // splits of at least 256 tokens
     if (most > 4096) most = 4096;
     if (most > 1 + 8ll * sm_count / (static_cast<long long>(B) * Hkv)) most = 1 + 8ll * sm_count / (static_cast<long long>(B) * Hkv);
     for (int cand = 1; cand <= most; ++cand) {
@@ -1017,7 +1017,7 @@ int ac_decode_plan_q4(const int32_t* token_counts_host, int B, int Hq, int Hkv, 
             longest = 0;
             for (int b = 0; b < B; ++b) {
                 const int t = tokens_of(b);
-                pieces += (t + chunk - 1) / chunk;
+                pieces += t > 0 ? (t - 1) / chunk + 1 : 0;
                 const int piece = t < chunk ? t : chunk;
                 longest = piece > longest ? piece : longest;
             }

@@ -37,3 +37,17 @@ def test_code_pools_of_more_than_36_bits_are_refused(ac, num_pages, ps, page, to
 def test_code_pools_within_36_bits_pass_that_guard(ac, num_pages, ps, page, token, head):
     # what stops them here is the workspace that four splits want, looked at after the pools
     assert attention(ac, num_pages, ps, page, token, head) == WORKSPACE
+
+
+@pytest.mark.parametrize("Hkv", [1, 8])
+def test_plans_for_two_billion_tokens(ac, Hkv):
+    # the split count of a context at the end of 32 bits is that of one a little shorter, and known lengths of the whole
+    # context give the plan that unknown ones give
+    near, end = 2**30 - 64, 2**31 - 1
+    want = ac.ac_decode_plan_q4(None, 1, 8, Hkv, 64, 16, near, 148)[0]
+    assert want > 1
+    assert ac.ac_decode_plan_q4(None, 1, 8, Hkv, 64, 16, end, 148)[0] == want
+    assert ac.ac_decode_plan_q4([end], 1, 8, Hkv, 64, 16, end, 148)[0] == want
+    want = ac.ac_decode_plan(1, 8, Hkv, 64, 16, end, 148)
+    assert want[0] == ac.ac_decode_plan(1, 8, Hkv, 64, 16, near, 148)[0]
+    assert ac.ac_decode_plan_for_lengths([end], 8, Hkv, 64, 16, end, 148) == want
