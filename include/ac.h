@@ -575,8 +575,9 @@ int ac_cache_reserve(int32_t* block_table, int max_pages_per_seq, const int32_t*
  * too (reference counts go up) and, where the parent's last page is partly filled, a page of its own
  * with a copy of the filled slots in every pool; context_lens[child] = context_lens[parent].  What else the
  * page and the child's table row held stays as it was.  The child row must be unused before (its
- * old pages are not released); a child listed twice, or that is also a parent, is a caller error; one parent
- * may have many children.  A fork whose page the pool cannot supply makes its child unused and sets
+ * old pages are not released); a child listed twice, or that is also a parent, is a caller error (which rows
+ * hold which pages is then undefined; lengths are those before the call, and nothing outside the tables is written);
+ * one parent may have many children.  A fork whose page the pool cannot supply makes its child unused and sets
  * AC_FLAG_POOL_EXHAUSTED; an unused parent gives an unused child.  n_pools may be 0 (bookkeeping only). */
 int ac_cache_fork(const ac_page_pool* pools, int n_pools, int32_t* block_table, int max_pages_per_seq,
                   int32_t* context_lens, int32_t* ref_counts, const int32_t* pairs, int n, int rows,

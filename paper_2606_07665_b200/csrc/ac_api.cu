@@ -1135,7 +1135,7 @@ int ac_cache_copy_pages(const ac_page_pool* pools, int n_pools, const int32_t* p
 
 size_t ac_cache_workspace_bytes(int rows, int num_pages, int n) {
     if (rows <= 0 || num_pages <= 0 || n < 0) return 0;
-    // reserve: offsets [rows], pages [num_pages]; fork: jobs [n] of 8 bytes, used [n], pages [min(n, num_pages)];
+    // reserve: offsets [rows], pages [num_pages]; fork: jobs [n] of 8 bytes, lengths [n], pages [min(n, num_pages)];
     // compact: head, moves [num_pages / 2 + 1] of 8 bytes, place [num_pages], counts of 4096 pages each
     const size_t p = static_cast<size_t>(num_pages), r = static_cast<size_t>(rows), k = static_cast<size_t>(n);
     return (32 + 8 * p + (p / 4096 + 1) * 4 + 8 * r + 16 * k + 15) / 16 * 16;

@@ -165,12 +165,12 @@ __device__ __forceinline__ void copy_piece(char* dst, const char* src, int64_t l
     if (tail < bytes) dst[lo + tail] = src[lo + tail];
 }
 
-// Jobs (source, destination) with, where used != nullptr, the number of slots that count.  blockIdx.y is the pool;
-// the warps of its CTAs take (job, segment, piece) units in turn.
-__device__ __forceinline__ void run_copies(const ac_page_pool& pool, const int2* jobs, const int32_t* used, int n,
+// Jobs (source, destination) with, where lens != nullptr, the length of the sequence whose last page is copied: of that only
+// the filled slots.  blockIdx.y is the pool; the warps of its CTAs take (job, segment, piece) units in turn.
+__device__ __forceinline__ void run_copies(const ac_page_pool& pool, const int2* jobs, const int32_t* lens, int n,
                                            int page_size, int num_pages, int32_t* status_flag) {
     const int lane = threadIdx.x & 31;
-    const int segments = used != nullptr ? pool.segments : 1;
+    const int segments = lens != nullptr ? pool.segments : 1;
     const int64_t seg_bytes = pool.page_bytes / segments;
     const int pieces = static_cast<int>((seg_bytes + kPiece - 1) / kPiece);
     const long long per_job = static_cast<long long>(segments) * pieces;
@@ -183,11 +183,11 @@ __device__ __forceinline__ void run_copies(const ac_page_pool& pool, const int2*
         const int seg = rest / pieces, piece = rest - seg * pieces;
         const int2 j = jobs[job];
         if (j.x < 0 || j.y < 0 || j.x >= num_pages || j.y >= num_pages) {
-            if (used == nullptr && lane == 0) raise(status_flag, AC_FLAG_PAGE_OOB);
+            if (lens == nullptr && lane == 0) raise(status_flag, AC_FLAG_PAGE_OOB);
             continue;
         }
         if (j.x == j.y) continue;
-        const int64_t end = used != nullptr ? seg_bytes / page_size * used[job] : seg_bytes;
+        const int64_t end = lens != nullptr ? seg_bytes / page_size * (lens[job] % page_size) : seg_bytes;
         const int64_t lo = static_cast<int64_t>(piece) * kPiece;
         const int64_t hi = min(end, lo + kPiece);
         if (lo >= hi) continue;
@@ -205,12 +205,13 @@ __global__ void __launch_bounds__(kCopyThreads) copy_pages_kernel(const __grid_c
 
 // ---- fork ------------------------------------------------------------------------------------------------
 
-// Gives every fork that needs a page its page; jobs[i] = (parent's last page, child's page) or (-1, page or -1)
-// where nothing is copied, used[i] = filled slots, and -1 there for a fork that does not take place.
+// Gives every fork that needs a page its page; jobs[i] = (parent's last page, child's page), or (-1, -1) where nothing is
+// copied, and lens[i] = the parent's length, or -1 for a fork that does not take place.  What follows goes by this length, which was
+// checked against the table here: the parent's own may change meanwhile (a row that is a child of the same call too).
 __global__ void __launch_bounds__(kPlanThreads) fork_plan_kernel(const int32_t* block_table, int max_pages_per_seq,
                                                                  const int32_t* context_lens, const int32_t* refs,
                                                                  const int2* pairs, int n, int rows, int page_size,
-                                                                 int num_pages, int2* jobs, int32_t* used,
+                                                                 int num_pages, int2* jobs, int32_t* lens,
                                                                  int32_t* list, int32_t* status_flag) {
     cudaTriggerProgrammaticLaunchCompletion();             // the next kernel waits for this one before it reads
     int need = 0;
@@ -227,7 +228,7 @@ __global__ void __launch_bounds__(kPlanThreads) fork_plan_kernel(const int32_t* 
                     raise(status_flag, AC_FLAG_POSITION_OOB);
                 } else if (len >= 0) {
                     part = len % page_size;
-                    state = part;
+                    state = len;
                     if (part > 0) src = block_table[static_cast<size_t>(pc.x) * max_pages_per_seq + len / page_size];
                 }
             }
@@ -235,7 +236,7 @@ __global__ void __launch_bounds__(kPlanThreads) fork_plan_kernel(const int32_t* 
         int total;
         const int rank = need + block_scan(part > 0 ? 1 : 0, &total);
         if (i < n) {
-            used[i] = state;
+            lens[i] = state;
             jobs[i] = make_int2(src, part > 0 ? rank : -1);      // the rank, until the pages are known
         }
         need += total;
@@ -244,9 +245,9 @@ __global__ void __launch_bounds__(kPlanThreads) fork_plan_kernel(const int32_t* 
     if (need > found && threadIdx.x == 0) raise(status_flag, AC_FLAG_POOL_EXHAUSTED);
     for (int i = threadIdx.x; i < n; i += kPlanThreads) {
         const int2 j = jobs[i];
-        if (used[i] <= 0) continue;
+        if (j.y < 0) continue;                                   // no page needed
         if (j.y >= found) {
-            used[i] = -1;
+            lens[i] = -1;
             jobs[i] = make_int2(-1, -1);
         } else {
             jobs[i].y = list[j.y];
@@ -260,23 +261,22 @@ __global__ void __launch_bounds__(kCopyThreads) fork_apply_kernel(const __grid_c
                                                                   int32_t* block_table, int max_pages_per_seq,
                                                                   int32_t* context_lens, int32_t* refs,
                                                                   const int2* pairs, const int2* jobs,
-                                                                  const int32_t* used, int n, int rows, int page_size,
+                                                                  const int32_t* lens, int n, int rows, int page_size,
                                                                   int num_pages, int32_t* status_flag) {
     cudaGridDependencySynchronize();           // no early signal: what follows may read the tables before its own wait
     if (blockIdx.y > 0) {
-        run_copies(pools.pool[blockIdx.y - 1], jobs, used, n, page_size, num_pages, nullptr);
+        run_copies(pools.pool[blockIdx.y - 1], jobs, lens, n, page_size, num_pages, nullptr);
         return;
     }
     for (int i = blockIdx.x; i < n; i += gridDim.x) {
         const int2 pc = pairs[i];
         if (pc.x < 0 || pc.x >= rows || pc.y < 0 || pc.y >= rows) continue;
-        const int part = used[i];
-        if (part < 0) {
+        const int len = lens[i];
+        if (len < 0) {
             if (threadIdx.x == 0) context_lens[pc.y] = -1;
             continue;
         }
-        const int len = context_lens[pc.x];
-        const int full = len / page_size;
+        const int full = len / page_size, part = len - full * page_size;
         const int32_t* from = block_table + static_cast<size_t>(pc.x) * max_pages_per_seq;
         int32_t* to = block_table + static_cast<size_t>(pc.y) * max_pages_per_seq;
         for (int k = threadIdx.x; k < full; k += kCopyThreads) {
@@ -493,11 +493,11 @@ cudaError_t launch_fork(const ac_page_pool* pools, int n_pools, int32_t* block_t
                         int32_t* context_lens, int32_t* refs, const int32_t* pairs, int n, int rows, int page_size,
                         int num_pages, void* workspace, int32_t* status_flag, int sms, cudaStream_t stream) {
     int2* jobs = static_cast<int2*>(workspace);
-    int32_t* used = reinterpret_cast<int32_t*>(jobs + n);
-    int32_t* list = used + n;
+    int32_t* lens = reinterpret_cast<int32_t*>(jobs + n);
+    int32_t* list = lens + n;
     const int2* pc = reinterpret_cast<const int2*>(pairs);
     fork_plan_kernel<<<1, kPlanThreads, 0, stream>>>(block_table, max_pages_per_seq, context_lens, refs, pc, n, rows,
-                                                     page_size, num_pages, jobs, used, list, status_flag);
+                                                     page_size, num_pages, jobs, lens, list, status_flag);
     cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess) return e;
     unsigned x = copy_grid(pools, n_pools, n, sms);
@@ -514,7 +514,7 @@ cudaError_t launch_fork(const ac_page_pool* pools, int n_pools, int32_t* block_t
     cfg.numAttrs = 1;
 #define AC_FORK_APPLY(N_)                                                                                            \
     cudaLaunchKernelEx(&cfg, fork_apply_kernel<N_>, pool_args<N_>(pools, n_pools), block_table, max_pages_per_seq,   \
-                       context_lens, refs, pc, static_cast<const int2*>(jobs), static_cast<const int32_t*>(used), n, \
+                       context_lens, refs, pc, static_cast<const int2*>(jobs), static_cast<const int32_t*>(lens), n, \
                        rows, page_size, num_pages, status_flag)
     return n_pools <= kFewPools ? AC_FORK_APPLY(kFewPools) : AC_FORK_APPLY(AC_MAX_PAGE_POOLS);
 #undef AC_FORK_APPLY
