@@ -490,7 +490,7 @@ int ac_rope_kv_append_q4(const void* q_in, void* q_out, const void* k_new, const
 /* Quantises many tokens of each row at once (a prompt whose keys are already rotated).  k, v are dense
  * bf16 [total_tokens, Hkv, d]; row b owns the tokens row_offsets[b] .. row_offsets[b+1] - 1 and its i-th
  * one is written to position start_pos[b] + i, i.e. page block_table[b, position / page_size].  row_offsets
- * is device int32 [B + 1], non-decreasing from 0; tokens at or past row_offsets[B] are ignored, rows with
+ * is device int32 [B + 1], non-decreasing; tokens before row_offsets[0] or at and past row_offsets[B] are ignored, rows with
  * start_pos[b] < 0 are inactive and write nothing.  total_tokens may be 0.  A token whose position or page
  * is out of range writes nothing and sets the status bits of ac_rope_kv_append.  Two tokens of one call in
  * the same slot are a caller error. */
@@ -500,7 +500,7 @@ int ac_kv_store_q4(const void* k, const void* v, const ac_q4_cache* cache, const
                    int32_t* status_flag, void* stream);
 
 /* The reverse: reads the same tokens back as bf16(c * s + m), rounded once, into dense k, v [total_tokens, Hkv, d].
- * Tokens of inactive rows, at or past row_offsets[B], or out of range (status bits set) read as +0. */
+ * Tokens of inactive rows, of no row, or out of range (status bits set) read as +0. */
 int ac_kv_load_q4(void* k, void* v, const ac_q4_cache* cache, const int32_t* block_table,
                   int max_pages_per_seq, const int32_t* start_pos, const int32_t* row_offsets,
                   int total_tokens, int B, int Hkv, int d, int page_size, int num_pages,

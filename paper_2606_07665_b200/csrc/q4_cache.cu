@@ -115,7 +115,7 @@ __device__ __forceinline__ TokenSlot find_slot(long long token, const Q4View& ca
         if (row_offsets[mid] <= token) lo = mid; else hi = mid;
     }
     const int start = start_pos[lo];
-    if (start < 0) return r;
+    if (start < 0 || token < row_offsets[lo]) return r;    // tokens before row 0 belong to no row: no position below 0
     const long long pos = start + (token - row_offsets[lo]);
     const long long idx = pos / page_size;
     if (idx >= max_pages_per_seq) {

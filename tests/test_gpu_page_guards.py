@@ -42,3 +42,29 @@ def test_fork_goes_by_the_lengths_before_the_call(rt):
     assert (got[last] == 17).all() and (got[mid] == width * ps).all()
     assert bool((guarded[rows] == -9).all())
     assert int(h.status_flag) == 0
+
+
+@pytest.mark.parametrize("d,group,heads", [(128, 64, 8), (64, 32, 3)])
+@pytest.mark.parametrize("first", [1, 5, 40, 400])
+def test_bulk_tokens_before_the_first_row_belong_to_no_row(rt, d, group, heads, first):
+    import torch
+    rng = np.random.default_rng(81)
+    B, ps, each = 3, 16, 30
+    total = first + B * each
+    cache = rt.Q4Cache.empty(B * 2 + 1, ps, heads, d, group)
+    table = i32([[1, 2], [3, 4], [5, 6]])                  # page 0 belongs to nobody, and nothing lies in front of it
+    before = [x.clone() for x in (cache.k_codes, cache.v_codes, cache.params)]
+    k, v = dev(bits(rng, total, heads, d)), dev(bits(rng, total, heads, d))
+    off, start = i32([first + each * b for b in range(B + 1)]), i32([0, 2, 1])
+    cache.store(k, v, table, start, off)
+    kb, vb = cache.load(table, start, off, total)
+    torch.cuda.synchronize()
+    assert int(cache.status_flag) == 0
+    for x, y in zip(before, (cache.k_codes, cache.v_codes, cache.params)):
+        assert torch.equal(x[0], y[0])
+    for got, x in ((kb, k), (vb, v)):
+        assert not host(got[:first]).any()                 # +0, not what the memory held
+        alone = rt.Q4Cache.empty(B * 2 + 1, ps, heads, d, group)
+        alone.store(x[first:], x[first:], table, start, off - first)
+        want, _ = alone.load(table, start, off - first, total - first)
+        assert torch.equal(got[first:], want)
