@@ -534,8 +534,10 @@ int ac_paged_decode_attn_q4(const void* q_rot, const ac_q4_cache* cache, const i
  * Bookkeeping of a page pool on the device, so that sequences can be grown, forked and dropped between
  * steps without a copy to the host.  State, all int32 in device memory: block_table [rows,
  * max_pages_per_seq], context_lens [rows] (tokens held; < 0: the row is unused) and ref_counts [num_pages]
- * (rows that hold the page; 0: free).  A row holds its first ceil(context_lens / page_size) pages, after
- * ac_cache_reserve also those of the reserved tokens until context_lens grows to count them.
+ * (rows that hold the page; 0: free).  A row holds its first ceil(context_lens / page_size) pages.  What ac_cache_reserve
+ * takes for it beyond those is counted in ref_counts but belongs to the row only once context_lens has grown to
+ * count it: the other calls do not know of it (ac_cache_release does not return it, ac_cache_compact does not follow
+ * it in the table).  ac_cache_trim returns whatever was reserved and not used.
  *
  * Free pages are handed out lowest index first, in the order of the call's list, so every call's
  * result is determined by its inputs.  The pools themselves are opaque bytes: any number of them (K and V
@@ -563,7 +565,8 @@ size_t ac_cache_workspace_bytes(int rows, int num_pages, int n);
 
 /* Gives every active row room for new_tokens more tokens: pages ceil(n/page_size) .. ceil((n + new_tokens) /
  * page_size) - 1 of the row are taken from the free pages (reference count 1), rows in order.  Pages are
- * taken again at each call: reserve, then let context_lens grow by new_tokens before reserving anew.
+ * taken again at each call: reserve, then let context_lens grow by new_tokens before reserving anew, or,
+ * where rows grow by less (prompts of different lengths, tokens that were not accepted), call ac_cache_trim first.
  * When the free pages run out, the row that does not get all of its pages and every later row that needs
  * any get none, and AC_FLAG_POOL_EXHAUSTED is set; a row whose pages would exceed max_pages_per_seq gets
  * none and sets AC_FLAG_POSITION_OOB. */
@@ -585,11 +588,19 @@ int ac_cache_fork(const ac_page_pool* pools, int n_pools, int32_t* block_table, 
                   int32_t* status_flag, void* stream);
 
 /* Drops the rows listed in row_list (device int32 [n]): the reference counts of their pages go down and
- * context_lens[row] becomes -1; the table entries stay.  A row that is unused, or listed again, is a
+ * context_lens[row] becomes -1; the table entries stay, and so do pages reserved for them (see ac_cache_trim).  A row that is unused, or listed again, is a
  * no-op.  A count that is already 0 stays 0 and sets AC_FLAG_REF_COUNT. */
 int ac_cache_release(const int32_t* block_table, int max_pages_per_seq, int32_t* context_lens,
                      int32_t* ref_counts, const int32_t* row_list, int n, int rows, int page_size,
                      int num_pages, int32_t* status_flag, void* stream);
+
+/* Returns what was reserved and not used: every count becomes the number of active rows that hold the page by their
+ * lengths, so pages reserved for tokens that did not come, or for rows released since, are free again.  Counts are
+ * rebuilt from the table alone: a page that the caller has counted up by itself is free too unless a row holds it.
+ * A row longer than its table row counts as far as that goes and sets AC_FLAG_POSITION_OOB, a page outside the pool
+ * is skipped and sets AC_FLAG_PAGE_OOB.  Two launches. */
+int ac_cache_trim(const int32_t* block_table, int max_pages_per_seq, const int32_t* context_lens,
+                  int32_t* ref_counts, int rows, int page_size, int num_pages, int32_t* status_flag, void* stream);
 
 /* Moves the live pages (reference count > 0) to the lowest ids: with L of them, the live pages at ids >= L
  * move, in order, to the free ids < L, in every pool, and the block table entries of the active rows and the
@@ -597,7 +608,8 @@ int ac_cache_release(const int32_t* block_table, int max_pages_per_seq, int32_t*
  * that still reads the old table reads the same bytes until those pages are handed out again.  The new
  * table and counts go to block_table_out and ref_counts_out, which may be the inputs themselves or other
  * buffers of the same shape (both or neither aliased); context_lens does not change.  Table entries past a
- * row's pages and rows that are not active are copied as they are: call it with nothing reserved. */
+ * row's pages and rows that are not active are copied as they are: call it with nothing reserved (after
+ * ac_cache_trim). */
 int ac_cache_compact(const ac_page_pool* pools, int n_pools, const int32_t* block_table,
                      int32_t* block_table_out, int max_pages_per_seq, const int32_t* context_lens,
                      const int32_t* ref_counts, int32_t* ref_counts_out, int rows, int page_size,

@@ -35,7 +35,7 @@ EXPORTS = ("ac_init", "ac_status_string", "ac_last_cuda_error", "ac_sm_count", "
            "ac_hbm_read_probe", "ac_qkv_rope_kv_append_ex", "ac_rope_kv_append_q4", "ac_kv_store_q4",
            "ac_kv_load_q4", "ac_decode_plan_q4", "ac_paged_decode_attn_q4", "ac_cache_copy_pages",
            "ac_cache_workspace_bytes", "ac_cache_reserve", "ac_cache_fork", "ac_cache_release",
-           "ac_cache_compact")
+           "ac_cache_trim", "ac_cache_compact")
 AC_STATIC_SCRATCH_BYTES = 8 << 20
 
 
@@ -173,6 +173,8 @@ def lib():
         L.ac_cache_release.argtypes = [c_void_p, c_int, c_void_p, c_void_p, c_void_p, c_int, c_int, c_int, c_int,
                                        c_void_p, c_void_p]
         L.ac_cache_release.restype = c_int
+        L.ac_cache_trim.argtypes = [c_void_p, c_int, c_void_p, c_void_p, c_int, c_int, c_int, c_void_p, c_void_p]
+        L.ac_cache_trim.restype = c_int
         L.ac_cache_compact.argtypes = [POINTER(AcPagePool), c_int, c_void_p, c_void_p, c_int, c_void_p, c_void_p,
                                        c_void_p, c_int, c_int, c_int, c_void_p, c_void_p, c_size_t, c_void_p,
                                        c_void_p]
@@ -531,6 +533,12 @@ def ac_cache_release(block_table, max_pages_per_seq, context_lens, ref_counts, r
     _check(lib().ac_cache_release(_ptr(block_table), max_pages_per_seq, _ptr(context_lens), _ptr(ref_counts),
                                   _ptr(row_list), n, rows, page_size, num_pages, _ptr(status_flag),
                                   _stream(stream)), "ac_cache_release")
+
+
+def ac_cache_trim(block_table, max_pages_per_seq, context_lens, ref_counts, rows, page_size, num_pages,
+                  status_flag=None, stream=None):
+    _check(lib().ac_cache_trim(_ptr(block_table), max_pages_per_seq, _ptr(context_lens), _ptr(ref_counts), rows,
+                               page_size, num_pages, _ptr(status_flag), _stream(stream)), "ac_cache_trim")
 
 
 def ac_cache_compact(pools, n_pools, block_table, block_table_out, max_pages_per_seq, context_lens, ref_counts,

@@ -1197,6 +1197,19 @@ int ac_cache_release(const int32_t* block_table, int max_pages_per_seq, int32_t*
     return e == cudaSuccess ? AC_OK : fail_cuda(static_cast<int>(e));
 }
 
+int ac_cache_trim(const int32_t* block_table, int max_pages_per_seq, const int32_t* context_lens,
+                  int32_t* ref_counts, int rows, int page_size, int num_pages, int32_t* status_flag, void* stream) {
+    if (!block_table || !context_lens || !ref_counts) return AC_ERR_NULL;
+    int st = check_pages(max_pages_per_seq, rows, page_size, num_pages);
+    if (st != AC_OK) return st;
+    int dev;
+    st = current_ready_device(&dev);
+    if (st != AC_OK) return st;
+    cudaError_t e = launch_trim(block_table, max_pages_per_seq, context_lens, ref_counts, rows, page_size, num_pages,
+                                status_flag, static_cast<cudaStream_t>(stream));
+    return e == cudaSuccess ? AC_OK : fail_cuda(static_cast<int>(e));
+}
+
 int ac_cache_compact(const ac_page_pool* pools, int n_pools, const int32_t* block_table,
                      int32_t* block_table_out, int max_pages_per_seq, const int32_t* context_lens,
                      const int32_t* ref_counts, int32_t* ref_counts_out, int rows, int page_size,

@@ -145,6 +145,8 @@ cudaError_t launch_fork(const ac_page_pool* pools, int n_pools, int32_t* block_t
 cudaError_t launch_release(const int32_t* block_table, int max_pages_per_seq, int32_t* context_lens, int32_t* refs,
                            const int32_t* row_list, int n, int rows, int page_size, int num_pages,
                            int32_t* status_flag, cudaStream_t stream);
+cudaError_t launch_trim(const int32_t* block_table, int max_pages_per_seq, const int32_t* context_lens, int32_t* refs,
+                        int rows, int page_size, int num_pages, int32_t* status_flag, cudaStream_t stream);
 cudaError_t launch_compact(const ac_page_pool* pools, int n_pools, const int32_t* block_table, int32_t* table_out,
                            int max_pages_per_seq, const int32_t* context_lens, const int32_t* refs, int32_t* refs_out,
                            int rows, int page_size, int num_pages, int32_t* live_out, void* workspace,

@@ -1,4 +1,4 @@
-// Page bookkeeping and page copies: reserve, fork, release, compact, copy.
+// Page bookkeeping and page copies: reserve, fork, release, trim, compact, copy.
 //
 // The bookkeeping kernels hand out free pages lowest index first.  For reserve and fork a single CTA walks the reference
 // counts in order, 16 pages per thread and step, and turns the free ones into ranks by a scan over the CTA; it stops as
@@ -329,6 +329,26 @@ __global__ void __launch_bounds__(kCopyThreads) release_kernel(const int32_t* bl
     }
 }
 
+// ---- trim ------------------------------------------------------------------------------------------------
+
+// One CTA per row adds the row's pages to counts that were cleared before.
+__global__ void __launch_bounds__(kCopyThreads) count_held_kernel(const int32_t* block_table, int max_pages_per_seq,
+                                                                  const int32_t* context_lens, int32_t* refs,
+                                                                  int page_size, int num_pages, int32_t* status_flag) {
+    const int len = context_lens[blockIdx.x];
+    if (len <= 0) return;
+    int pages = pages_for(len, page_size);
+    if (pages > max_pages_per_seq) {
+        if (threadIdx.x == 0) raise(status_flag, AC_FLAG_POSITION_OOB);
+        pages = max_pages_per_seq;
+    }
+    for (int k = threadIdx.x; k < pages; k += kCopyThreads) {
+        const int page = block_table[static_cast<size_t>(blockIdx.x) * max_pages_per_seq + k];
+        if (page < 0 || page >= num_pages) raise(status_flag, AC_FLAG_PAGE_OOB);
+        else atomicAdd(refs + page, 1);
+    }
+}
+
 // ---- compact ---------------------------------------------------------------------------------------------
 
 // Ranks without a scan over the whole pool in one CTA: chunks of kChunk pages are counted, and each chunk's CTA then adds up
@@ -525,6 +545,15 @@ cudaError_t launch_release(const int32_t* block_table, int max_pages_per_seq, in
                            int32_t* status_flag, cudaStream_t stream) {
     release_kernel<<<n, kCopyThreads, 0, stream>>>(block_table, max_pages_per_seq, context_lens, refs, row_list, rows,
                                                    page_size, num_pages, status_flag);
+    return cudaGetLastError();
+}
+
+cudaError_t launch_trim(const int32_t* block_table, int max_pages_per_seq, const int32_t* context_lens, int32_t* refs,
+                        int rows, int page_size, int num_pages, int32_t* status_flag, cudaStream_t stream) {
+    const cudaError_t e = cudaMemsetAsync(refs, 0, static_cast<size_t>(num_pages) * sizeof(int32_t), stream);
+    if (e != cudaSuccess) return e;
+    count_held_kernel<<<rows, kCopyThreads, 0, stream>>>(block_table, max_pages_per_seq, context_lens, refs, page_size,
+                                                         num_pages, status_flag);
     return cudaGetLastError();
 }
 

@@ -4,7 +4,7 @@ Only plumbing: torch tensors for device memory, the split plan from the library,
 C-ABI calls in order.  Every arithmetic step runs inside libac's kernels.
 
 ``DecodeStep`` stages a synthetic workload; ``PagedAttention`` (bf16 cache), ``Q4Cache`` with ``Q4DecodeStep``
-(4-bit cache) and ``CachePages`` (reserve, fork, release, compact, copy) work on tensors that the caller owns.
+(4-bit cache) and ``CachePages`` (reserve, fork, release, trim, compact, copy) work on tensors that the caller owns.
 """
 from __future__ import annotations
 
@@ -602,7 +602,7 @@ class Q4DecodeStep(_Rows):
 
 
 class CachePages(_OnDevice):
-    """Pages of any number of pools under one block table: reserve, fork, release, compact, copy.
+    """Pages of any number of pools under one block table: reserve, fork, release, trim, compact, copy.
 
     ``pools``: contiguous tensors [num_pages, ...], each alone or with the number of segments of its page ([page,
     slot, ...]: 1; [page, head, slot, ...]: the heads).  ``block_table`` int32 [rows, max_pages_per_seq],
@@ -634,7 +634,8 @@ class CachePages(_OnDevice):
         return [self.status_flag, self.workspace]
 
     def reserve(self, new_tokens, stream=None):
-        """Pages for new_tokens more tokens of every active row, lowest free page first, rows in order."""
+        """Pages for new_tokens more tokens of every active row, lowest free page first, rows in order.  Let the rows
+        grow by that many tokens before the next call, or call trim() first."""
         self._enqueue("ac_cache_reserve",
                       [self.block_table.data_ptr(), self.max_pages_per_seq, self.context_lens.data_ptr(),
                        self.ref_counts.data_ptr(), int(new_tokens), self.rows, self.page_size, self.num_pages,
@@ -654,7 +655,7 @@ class CachePages(_OnDevice):
                        self.page_size, self.num_pages, *self._room, self._flag, None], stream, -1)
 
     def release(self, row_list, stream=None):
-        """row_list: int32 [n]; unused and repeated rows are no-ops."""
+        """row_list: int32 [n]; unused and repeated rows are no-ops.  Pages reserved for the rows stay taken until trim()."""
         n = row_list.shape[0]
         _want(row_list, "row_list", (n,), (torch.int32,), self.device)
         if n == 0:
@@ -663,6 +664,12 @@ class CachePages(_OnDevice):
                       [self.block_table.data_ptr(), self.max_pages_per_seq, self.context_lens.data_ptr(),
                        self.ref_counts.data_ptr(), row_list.data_ptr(), n, self.rows, self.page_size, self.num_pages,
                        self._flag, None], stream, -1)
+
+    def trim(self, stream=None):
+        """Frees what was reserved and not used, for released rows too: counts the pages that the rows hold anew."""
+        self._enqueue("ac_cache_trim",
+                      [self.block_table.data_ptr(), self.max_pages_per_seq, self.context_lens.data_ptr(),
+                       self.ref_counts.data_ptr(), self.rows, self.page_size, self.num_pages, self._flag, None], stream, -1)
 
     def copy(self, pairs, stream=None):
         """Copies whole pages: pairs int32 [n, 2] (source, destination)."""
@@ -674,7 +681,7 @@ class CachePages(_OnDevice):
                                               self._flag, None], stream, -1)
 
     def compact(self, table_out=None, refs_out=None, live_out=None, stream=None):
-        """Moves the live pages to the lowest ids.  In place, or (both given) into another table and counts, so that
+        """Moves the live pages to the lowest ids; nothing may be reserved (trim() before it).  In place, or (both given) into another table and counts, so that
         a step in flight can still read the old ones.  ``live_out`` int32 [1] receives the number of live pages."""
         if (table_out is None) != (refs_out is None):
             raise ValueError("table_out and refs_out go together")

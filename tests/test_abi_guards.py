@@ -51,3 +51,12 @@ def test_plans_for_two_billion_tokens(ac, Hkv):
     want = ac.ac_decode_plan(1, 8, Hkv, 64, 16, end, 148)
     assert want[0] == ac.ac_decode_plan(1, 8, Hkv, 64, 16, near, 148)[0]
     assert ac.ac_decode_plan_for_lengths([end], 8, Hkv, 64, 16, end, 148) == want
+
+
+def test_trim_refusals(ac):
+    def trim(table=P, mp=8, lens=P, refs=P, rows=4, ps=16, pages=64):
+        return ac.lib().ac_cache_trim(table, mp, lens, refs, rows, ps, pages, None, None)
+
+    assert trim(table=None) == trim(lens=None) == trim(refs=None) == 1
+    assert trim(mp=0) == trim(rows=0) == trim(ps=0) == trim(pages=0) == trim(pages=-5) == 2
+    assert trim(pages=2**30 + 1) == UNSUPPORTED
