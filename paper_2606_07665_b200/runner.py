@@ -264,7 +264,10 @@ _BF16 = (torch.bfloat16, torch.int16)          # bf16 values, or their bits
 
 
 def _want(t, name, shape, dtypes, device):
-    """t is a contiguous tensor of this shape (a torch.Size), type and device; raises ValueError otherwise."""
+    """t is a contiguous tensor of this shape (a torch.Size), type and device; raises ValueError otherwise (TypeError for
+    what is no tensor)."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name}: {type(t).__name__}, expected a tensor")
     if t.shape == shape and t.dtype in dtypes and t.is_contiguous() and t.device == device:
         return
     if t.dtype not in dtypes:
@@ -544,6 +547,9 @@ class Q4DecodeStep(_Rows):
         self.rope_cos, self.rope_sin = rope_cos, rope_sin
         variants = dict(rope_variants or {})
         self._norms = (variants.get("q_norm_weight"), variants.get("k_norm_weight"))      # kept alive
+        for t, what in zip(self._norms, ("q_norm_weight", "k_norm_weight")):
+            if t is not None:
+                _want(t, what, (self.d,), _BF16, self.device)
         self._rope = ac._rope_options(**variants)
         if rope_cos is not None:
             rotary = int(variants.get("rotary_dim", 0)) or self.d

@@ -1,0 +1,44 @@
+"""What the objects over the caller's tensors refuse before anything is launched."""
+import numpy as np
+import pytest
+
+from paper_2606_07665_b200 import workloads as W
+from tests.test_gpu_q4 import Case, bits, dev
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def rt():
+    import torch
+    from paper_2606_07665_b200 import build, runner
+    build.build()
+    torch.cuda.set_device(0)
+    return runner
+
+
+@pytest.fixture(scope="module")
+def case(rt):
+    c = Case(rt, 100, [10, 20], 4, 2, 64, 16, 32)
+    cache = c.upload(rt)
+    cos, sin = (dev(x) for x in W.rope_table(64, 64, 10000.0))
+    return c, cache, cos, sin
+
+
+@pytest.mark.parametrize("which", ["q_norm_weight", "k_norm_weight"])
+def test_norm_weights(rt, case, which):
+    import torch
+    c, cache, cos, sin = case
+    good = torch.ones(64, dtype=torch.bfloat16, device="cuda")
+
+    def make(weight):
+        return rt.Q4DecodeStep(cache, dev(c.table), dev(c.lens), 4, lens_host=c.lens, rope_cos=cos, rope_sin=sin,
+                               rope_variants={which: weight, "norm_eps": 1e-5})
+
+    for bad in (good.cpu(), good.float(), good[:32], torch.ones(128, dtype=torch.bfloat16, device="cuda")[::2], good.reshape(1, 64)):
+        with pytest.raises(ValueError, match=which):
+            make(bad)
+    with pytest.raises(TypeError, match=which):
+        make(good.data_ptr())
+    make(good)
+    make(good.view(torch.int16))
