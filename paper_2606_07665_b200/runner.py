@@ -551,6 +551,8 @@ class Q4DecodeStep(_Rows):
             if t is not None:
                 _want(t, what, (self.d,), _BF16, self.device)
         self._rope = ac._rope_options(**variants)
+        if (rope_cos is None) != (rope_sin is None):
+            raise ValueError("rope_cos and rope_sin go together")
         if rope_cos is not None:
             rotary = int(variants.get("rotary_dim", 0)) or self.d
             for t, what in ((rope_cos, "rope_cos"), (rope_sin, "rope_sin")):

@@ -42,3 +42,18 @@ def test_norm_weights(rt, case, which):
         make(good.data_ptr())
     make(good)
     make(good.view(torch.int16))
+
+
+def test_rope_tables_come_in_pairs(rt, case):
+    c, cache, cos, sin = case
+
+    def make(a, b, **variants):
+        return rt.Q4DecodeStep(cache, dev(c.table), dev(c.lens), 4, lens_host=c.lens, rope_cos=a, rope_sin=b, rope_variants=variants)
+
+    for a, b in ((cos, None), (None, sin), (cos, sin[:32]), (cos, sin.cpu()), (cos, sin.double()), (cos[0], sin[0])):
+        with pytest.raises(ValueError, match="rope"):
+            make(a, b)
+    with pytest.raises(ValueError, match="rope"):
+        make(cos, sin, rotary_dim=32)                      # tables of another width
+    make(cos, sin)
+    make(None, None)
