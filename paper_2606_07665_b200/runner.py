@@ -480,6 +480,8 @@ class Q4Cache(_OnDevice):
 
     @classmethod
     def empty(cls, num_pages, page_size, Hkv, d, group=64, layout="token_major", device="cuda:0"):
+        if group not in (32, 64, 128) or group > d:
+            raise ValueError(f"group {group}: expected 32, 64 or 128, and at most {d}")
         shape = (num_pages, page_size, Hkv, d // 2) if layout == "token_major" else (num_pages, Hkv, page_size, d // 2)
         k, v = (torch.zeros(shape, dtype=torch.uint8, device=device) for _ in range(2))
         params = torch.zeros((num_pages, Hkv, page_size, 2, d // group, 2), dtype=torch.bfloat16, device=device)

@@ -60,3 +60,10 @@ def test_trim_refusals(ac):
     assert trim(table=None) == trim(lens=None) == trim(refs=None) == 1
     assert trim(mp=0) == trim(rows=0) == trim(ps=0) == trim(pages=0) == trim(pages=-5) == 2
     assert trim(pages=2**30 + 1) == UNSUPPORTED
+
+
+@pytest.mark.parametrize("d,group", [(128, 48), (128, 100), (64, 128), (64, 0), (128, -64), (128, 16), (64, 65)])
+def test_an_empty_cache_has_the_group_that_was_asked_for_or_none(d, group):
+    from paper_2606_07665_b200 import runner
+    with pytest.raises(ValueError, match="group"):
+        runner.Q4Cache.empty(4, 16, 2, d, group=group)
