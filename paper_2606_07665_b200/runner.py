@@ -373,9 +373,15 @@ class _Rows(_OnDevice):
         """Chooses the splits.  ``lens_host``: the rows' cached tokens on the host (< 0: inactive), as the scheduler
         that built context_lens has them; without them every row counts ``max_context_len`` tokens (default: what
         the block table can hold).  Plan again when the lengths outgrow max_context_len: the last split takes what lies
-        beyond it, which is right but slow.  Graphs captured before keep the plan that they were captured under."""
+        beyond it, which is right but slow.  Graphs captured before keep the plan that they were captured under.
+        ``row_order``: the order in which the grid serves the rows, a permutation on the host, None for the kernel's own, or "auto"
+        (longest first where lens_host is known and the grid is more than one wave deep)."""
         if lens_host is not None and len(lens_host) != self.B:
             raise ValueError(f"{len(lens_host)} lengths for {self.B} rows")
+        if row_order is not None and not (isinstance(row_order, str) and row_order == "auto"):
+            row_order = np.asarray(row_order)              # the kernels index the rows with it
+            if not np.array_equal(np.sort(row_order, axis=None), np.arange(self.B)) or row_order.ndim != 1:
+                raise ValueError(f"row_order: expected 'auto' or a permutation of 0 .. {self.B - 1}")
         if max_context_len is None:
             max_context_len = (max(1, max(int(n) + 1 for n in lens_host)) if lens_host is not None
                                else self.max_pages_per_seq * self.page_size)
@@ -393,7 +399,7 @@ class _Rows(_OnDevice):
             self.row_order = None
             if isinstance(row_order, str):
                 deep = self.B > 1 and self.B * self.Hkv * self.num_splits > 2 * (ac.ac_sm_count() or 148)
-                if row_order == "auto" and lens_host is not None and deep:
+                if lens_host is not None and deep:
                     row_order = np.argsort(-np.asarray(lens_host, dtype=np.int64), kind="stable")
                 else:
                     row_order = None

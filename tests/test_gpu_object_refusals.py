@@ -57,3 +57,20 @@ def test_rope_tables_come_in_pairs(rt, case):
         make(cos, sin, rotary_dim=32)                      # tables of another width
     make(cos, sin)
     make(None, None)
+
+
+def test_row_orders_are_permutations(rt, case):
+    import torch
+    c, cache, cos, sin = case
+    h = rt.Q4DecodeStep(cache, dev(c.table), dev(c.lens), 4, lens_host=c.lens, num_splits=2, row_order=[1, 0])
+    q = dev(bits(np.random.default_rng(1), 2, 4, 64))
+    want = h.attention(q)
+    for bad in ([0], [0, 0], [0, 1, 2], [0, 2], [-1, 0], [[0, 1]], [0.5, 1.0], [], "longest"):
+        with pytest.raises(ValueError, match="row_order"):
+            h.plan(lens_host=c.lens, num_splits=2, row_order=bad)
+        with pytest.raises(ValueError, match="row_order"):
+            rt.Q4DecodeStep(cache, dev(c.table), dev(c.lens), 4, lens_host=c.lens, row_order=bad)
+    assert torch.equal(h.attention(q), want)                # the plan from before still stands
+    for good in ("auto", None, [0, 1], np.array([1, 0]), torch.tensor([1, 0])):
+        h.plan(lens_host=c.lens, num_splits=2, row_order=good)
+        assert torch.equal(h.attention(q), want)
