@@ -279,6 +279,13 @@ def _want(t, name, shape, dtypes, device):
     raise ValueError(f"{name}: not contiguous")
 
 
+def _new_tokens(n):
+    """1: attention over context_lens[b] + 1 tokens, the one just appended among them; 0: over the cached ones alone."""
+    if n not in (0, 1):
+        raise ValueError(f"new_tokens {n}, expected 0 or 1")
+    return int(n)
+
+
 class _OnDevice:
     """A device, ac_init on it, its streams, and what belongs to the calls on them."""
 
@@ -426,7 +433,7 @@ class PagedAttention(_Rows):
         _want(v_cache, "v_cache", k_cache.shape, _BF16, self.device)
         token, head = {"token_major": (1, 2), "head_major": (2, 1)}[layout]
         self.k_cache, self.v_cache, self.window, self.sinks = k_cache, v_cache, int(window), int(sinks)
-        self.softmax_scale, self.new_tokens = float(softmax_scale), int(new_tokens)
+        self.softmax_scale, self.new_tokens = float(softmax_scale), _new_tokens(new_tokens)
         self._strides = (k_cache.stride(0), k_cache.stride(token), k_cache.stride(head))
         self._rows(block_table, context_lens, k_cache.shape[token], k_cache.shape[0], Hq, k_cache.shape[head],
                    k_cache.shape[3])
@@ -549,7 +556,7 @@ class Q4DecodeStep(_Rows):
                  softmax_scale=0.0, new_tokens=1):
         self._bind(cache.device)
         self.cache, self.window, self.sinks = cache, int(window), int(sinks)
-        self.softmax_scale, self.new_tokens = float(softmax_scale), int(new_tokens)
+        self.softmax_scale, self.new_tokens = float(softmax_scale), _new_tokens(new_tokens)
         self._rows(block_table, context_lens, cache.page_size, cache.num_pages, Hq, cache.Hkv, cache.d)
         self._q_shape, self._kv_shape = (torch.Size((self.B, h, self.d)) for h in (self.Hq, self.Hkv))
         self.rope_cos, self.rope_sin = rope_cos, rope_sin
@@ -614,6 +621,8 @@ class Q4DecodeStep(_Rows):
 
     def step(self, q_in, k_new, v_new, q_rot=None, out=None, stream=None):
         """append, then attention over context_lens[b] + 1 tokens."""
+        if self.new_tokens != 1:
+            raise ValueError(f"step attends over the token that it appends: new_tokens is {self.new_tokens}, not 1")
         return self.attention(self.append(q_in, k_new, v_new, q_rot, stream), out, stream)
 
 

@@ -74,3 +74,22 @@ def test_row_orders_are_permutations(rt, case):
     for good in ("auto", None, [0, 1], np.array([1, 0]), torch.tensor([1, 0])):
         h.plan(lens_host=c.lens, num_splits=2, row_order=good)
         assert torch.equal(h.attention(q), want)
+
+
+def test_step_attends_over_the_token_that_it_appends(rt, case):
+    # an object for attention over the cached tokens alone has no step: it would leave out the token just written
+    c, cache, cos, sin = case
+    rng = np.random.default_rng(2)
+    q, k, v = (dev(bits(rng, 2, n, 64)) for n in (4, 2, 2))
+    kw = dict(lens_host=c.lens, rope_cos=cos, rope_sin=sin)
+    before = rt.Q4DecodeStep(cache, dev(c.table), dev(c.lens), 4, new_tokens=0, **kw)
+    with pytest.raises(ValueError, match="new_tokens"):
+        before.step(q, k, v)
+    for n in (2, -1):
+        with pytest.raises(ValueError, match="new_tokens"):
+            rt.Q4DecodeStep(cache, dev(c.table), dev(c.lens), 4, new_tokens=n, **kw)
+        with pytest.raises(ValueError, match="new_tokens"):
+            kv = dev(bits(rng, 4, 16, 2, 64))
+            rt.PagedAttention(kv, kv, dev(c.table.clip(0)), dev(c.lens), 4, lens_host=c.lens, new_tokens=n)
+    before.attention(q)
+    rt.Q4DecodeStep(cache, dev(c.table), dev(c.lens), 4, **kw).step(q, k, v)
