@@ -279,6 +279,13 @@ def _want(t, name, shape, dtypes, device):
     raise ValueError(f"{name}: not contiguous")
 
 
+def _axes(layout):
+    """(slot axis, head axis) of a pool [num_pages, ., ., .]."""
+    if layout not in ("token_major", "head_major"):
+        raise ValueError(f"layout {layout!r}, expected 'token_major' or 'head_major'")
+    return (1, 2) if layout == "token_major" else (2, 1)
+
+
 def _new_tokens(n):
     """1: attention over context_lens[b] + 1 tokens, the one just appended among them; 0: over the cached ones alone."""
     if n not in (0, 1):
@@ -431,7 +438,7 @@ class PagedAttention(_Rows):
             raise ValueError(f"k_cache: {k_cache.dim()} dimensions, expected 4")
         _want(k_cache, "k_cache", k_cache.shape, _BF16, self.device)
         _want(v_cache, "v_cache", k_cache.shape, _BF16, self.device)
-        token, head = {"token_major": (1, 2), "head_major": (2, 1)}[layout]
+        token, head = _axes(layout)
         self.k_cache, self.v_cache, self.window, self.sinks = k_cache, v_cache, int(window), int(sinks)
         self.softmax_scale, self.new_tokens = float(softmax_scale), _new_tokens(new_tokens)
         self._strides = (k_cache.stride(0), k_cache.stride(token), k_cache.stride(head))
@@ -475,7 +482,7 @@ class Q4Cache(_OnDevice):
         self._bind(k_codes.device)
         if k_codes.dim() != 4 or params.dim() != 6:
             raise ValueError("codes have 4 dimensions, params 6")
-        token, head = {"token_major": (1, 2), "head_major": (2, 1)}[layout]
+        token, head = _axes(layout)
         self.num_pages, self.page_size, self.Hkv = k_codes.shape[0], k_codes.shape[token], k_codes.shape[head]
         self.d, self.layout = 2 * k_codes.shape[3], layout
         if page_size is not None and page_size != self.page_size:
@@ -493,6 +500,7 @@ class Q4Cache(_OnDevice):
 
     @classmethod
     def empty(cls, num_pages, page_size, Hkv, d, group=64, layout="token_major", device="cuda:0"):
+        _axes(layout)
         if group not in (32, 64, 128) or group > d:
             raise ValueError(f"group {group}: expected 32, 64 or 128, and at most {d}")
         shape = (num_pages, page_size, Hkv, d // 2) if layout == "token_major" else (num_pages, Hkv, page_size, d // 2)

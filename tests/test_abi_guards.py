@@ -67,3 +67,9 @@ def test_an_empty_cache_has_the_group_that_was_asked_for_or_none(d, group):
     from paper_2606_07665_b200 import runner
     with pytest.raises(ValueError, match="group"):
         runner.Q4Cache.empty(4, 16, 2, d, group=group)
+
+
+def test_unknown_layouts_are_refused():
+    from paper_2606_07665_b200 import runner
+    with pytest.raises(ValueError, match="layout"):
+        runner.Q4Cache.empty(4, 16, 2, 64, layout="headmajor")

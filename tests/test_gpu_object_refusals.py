@@ -93,3 +93,12 @@ def test_step_attends_over_the_token_that_it_appends(rt, case):
             rt.PagedAttention(kv, kv, dev(c.table.clip(0)), dev(c.lens), 4, lens_host=c.lens, new_tokens=n)
     before.attention(q)
     rt.Q4DecodeStep(cache, dev(c.table), dev(c.lens), 4, **kw).step(q, k, v)
+
+
+def test_layouts(rt, case):
+    c, cache, cos, sin = case
+    with pytest.raises(ValueError, match="layout"):
+        rt.Q4Cache(cache.k_codes, cache.v_codes, cache.params, layout="tokens")
+    kv = dev(bits(np.random.default_rng(3), 4, 16, 2, 64))
+    with pytest.raises(ValueError, match="layout"):
+        rt.PagedAttention(kv, kv, dev(c.table), dev(c.lens), 4, layout="")
