@@ -8,6 +8,8 @@ C-ABI calls in order.  Every arithmetic step runs inside libac's kernels.
 """
 from __future__ import annotations
 
+import ctypes
+
 import numpy as np
 import torch
 
@@ -266,10 +268,13 @@ _BF16 = (torch.bfloat16, torch.int16)          # bf16 values, or their bits
 def _want(t, name, shape, dtypes, device):
     """t is a contiguous tensor of this shape (a torch.Size), type and device; raises ValueError otherwise (TypeError for
     what is no tensor)."""
+    try:
+        if t.shape == shape and t.dtype in dtypes and t.is_contiguous() and t.device == device:
+            return
+    except AttributeError:
+        pass
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name}: {type(t).__name__}, expected a tensor")
-    if t.shape == shape and t.dtype in dtypes and t.is_contiguous() and t.device == device:
-        return
     if t.dtype not in dtypes:
         raise ValueError(f"{name}: type {t.dtype}, expected {' or '.join(map(str, dtypes))}")
     if tuple(t.shape) != tuple(shape):
@@ -338,16 +343,16 @@ class _OnDevice:
         if _current_device() != self._index:
             with torch.cuda.device(self.device):
                 return self._enqueue(name, args, stream, at)
-        current = _raw_stream(self._index)
         if stream is None:
-            stream = current
-        elif not isinstance(stream, int):
-            stream = stream.cuda_stream
+            stream = _raw_stream(self._index)
+            self._captured = self._captured or _current_is_captured()
+        else:
+            if not isinstance(stream, int):
+                stream = stream.cuda_stream
+            self._captured = self._captured or _is_captured(stream)
         args[at] = stream
         if stream not in self._streams:
             self._used_on(stream)
-        if not self._captured:
-            self._captured = _current_is_captured() if stream == current else _is_captured(stream)
         status = getattr(self._lib, name)(*args)
         if status != 0:
             raise ac.AcError(status, name)
@@ -359,10 +364,14 @@ _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda i:
 _current_is_captured = getattr(torch._C, "_cuda_isCurrentStreamCapturing", None) or torch.cuda.is_current_stream_capturing
 
 
-def _is_captured(stream):
-    """Whether this stream (a handle) is being captured into a graph."""
-    with torch.cuda.stream(torch.cuda.ExternalStream(stream)):
-        return torch.cuda.is_current_stream_capturing()
+def _is_captured(stream, _driver=[]):
+    """Whether this stream (a handle) is being captured into a graph.  Asked of the driver: making the stream the current one to
+    ask torch costs as much as the call that follows."""
+    if not _driver:
+        _driver.append(ctypes.CDLL("libcuda.so.1").cuStreamIsCapturing)
+        _driver[0].argtypes = [ctypes.c_void_p, ctypes.POINTER(ctypes.c_int)]
+    status = ctypes.c_int(0)
+    return _driver[0](stream, status) == 0 and status.value != 0
 
 
 class _Rows(_OnDevice):

@@ -142,6 +142,28 @@ def test_a_captured_graph_keeps_the_plan_that_it_was_captured_under(rt, kind, wa
         assert bool(((out.view(torch.bfloat16).double() - want.view(torch.bfloat16).double()).abs() < 0.05).all())
 
 
+def test_a_capture_is_noticed_on_a_stream_that_is_not_the_current_one(rt):
+    import torch
+    h, call, out = attention(rt, "q4")
+    a, b = torch.cuda.Stream(), torch.cuda.Stream()
+    call(b)
+    torch.cuda.synchronize()
+    want = out.clone()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=a):
+        b.wait_stream(a)
+        call(b.cuda_stream)             # the fork of the capture, by its handle
+        a.wait_stream(b)
+    old = place(h.workspace, h.row_order)
+    h.plan(lens_host=LENS, num_splits=7, row_order=[2, 0, 1])
+    torch.cuda.synchronize()
+    assert not overlap(old, place(h.workspace, h.row_order)) and not handed_out(old)
+    out.zero_()
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(out, want)
+
+
 def test_plans_in_a_loop_do_not_pile_up(rt):
     # without captured graphs nothing old is kept
     import torch
