@@ -520,8 +520,10 @@ int ac_decode_plan_q4(const int32_t* token_counts_host, int B, int Hq, int Hkv, 
  * fp32, and the softmax weights times a V group's scale are rounded to fp16 (2^-11 relative, or 2^-31 of the
  * largest V scale seen, whichever is more) for the second product.  Slots at or past n_b, unreferenced pages and
  * unused block-table entries never influence the result; a page id outside [0, num_pages) reads as zeros.
- * Outside the supported range: queries of magnitude 2^116 and more, and (AC_ERR_UNSUPPORTED) code pools in which 16 tokens
- * of a page start 2^36 bytes or more behind the base, whatever the order of the strides.  The workspace belongs to one call at a time: calls that may overlap need one each. */
+ * Outside the supported range: queries of magnitude 2^116 and more; rows whose tokens times the largest magnitude of V
+ * reach 2^118 (the running sums are fp32, and a weight may be up to 2^8 before the final division); and
+ * (AC_ERR_UNSUPPORTED) code pools in which 16 tokens of a page start 2^36 bytes or more behind the base, whatever the
+ * order of the strides.  The workspace belongs to one call at a time: calls that may overlap need one each. */
 int ac_paged_decode_attn_q4(const void* q_rot, const ac_q4_cache* cache, const int32_t* block_table,
                             int max_pages_per_seq, const int32_t* context_lens, int new_tokens,
                             float softmax_scale, int num_splits, void* workspace, size_t workspace_bytes,
