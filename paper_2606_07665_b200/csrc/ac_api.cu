@@ -986,7 +986,8 @@ int ac_decode_plan_q4(const int32_t* token_counts_host, int B, int Hq, int Hkv, 
     if (st != AC_OK) return st;
     if (max_context_len <= 0) return AC_ERR_SHAPE;
     if (sm_count <= 0) sm_count = g_last_sm_count > 0 ? g_last_sm_count : 148;
-    // Every split count is priced by what the launch it gives (q4_attn.cu) was measured to do: the whole GPU moves
+    // Every split count is priced by what launches with one and with two CTAs per SM (q4_attn.cu) were measured to do (short
+    // splits in more than two waves run three CTAs of four warps, which has no price of its own): the whole GPU moves
     // 5.6 TB/s of this cache (its arithmetic keeps it below HBM's rate), one CTA alone on its SM 43 GB/s with twelve warps
     // and 32 with six, two sharing an SM 20 each, in a ragged batch 25; a wave costs 4 us of start and end, a further one
     // 3, the merge through the workspace 1.6 and the partial results' traffic.  (d/2 + 4 d/group bytes per token, side

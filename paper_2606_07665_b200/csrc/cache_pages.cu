@@ -4,9 +4,11 @@
 // counts in order, 16 pages per thread and step, and turns the free ones into ranks by a scan over the CTA; it stops as
 // soon as it has what the call needs.  Compaction needs every live page's rank: CTAs count and rank a chunk of the
 // counts each, in two launches.  Bound: latency (a few dependent passes over num_pages * 4 bytes that sit in L2): 8 forks
-// 7.9 us with their copies, the compaction of a pool of 512 pages 6.5.  The copies are bound by HBM, which reads and writes: a warp
-// moves pieces of up to 4 KB, 16 bytes a lane, eight loads in flight before the first store; a compaction that moves
-// 0.65 GB (1.3 GB read and written) takes 222 us = 5870 GB/s, 0.90 of the measured 6546.
+// with their copies and the release of the children 7.9 us, one page for each of 64 rows 8.0, trim 3.2, the compaction of
+// a pool of 512 pages 6.5.  The one CTA's walk grows with what lies in front of the free pages: 36000 live ones make that reserve
+// 11.7 us and those forks 13.4.  The copies are bound by HBM, which reads and writes: a warp moves pieces of up to 4 KB, 16
+// bytes a lane, eight loads in flight before the first store; a compaction that moves 0.65 GB (1.3 GB read and written) takes
+// 222 us = 5870 GB/s, 0.90 of the measured 6546, one of 96 pools (0.79 GB read and written, 300 rows) 127 us.
 #include "ac_device.cuh"
 #include "ac_internal.h"
 
@@ -206,8 +208,8 @@ __global__ void __launch_bounds__(kCopyThreads) copy_pages_kernel(const __grid_c
 // ---- fork ------------------------------------------------------------------------------------------------
 
 // Gives every fork that needs a page its page; jobs[i] = (parent's last page, child's page), or (-1, -1) where nothing is
-// copied, and lens[i] = the parent's length, or -1 for a fork that does not take place.  What follows goes by this length, which was
-// checked against the table here: the parent's own may change meanwhile (a row that is a child of the same call too).
+// copied, and lens[i] = the parent's length, or -1 for a fork that does not take place.  What follows goes by this length,
+// which was checked against the table here: the parent's own may change meanwhile (a row that is a child of the call too).
 __global__ void __launch_bounds__(kPlanThreads) fork_plan_kernel(const int32_t* block_table, int max_pages_per_seq,
                                                                  const int32_t* context_lens, const int32_t* refs,
                                                                  const int2* pairs, int n, int rows, int page_size,
@@ -472,8 +474,8 @@ PoolArgs<N> pool_args(const ac_page_pool* pools, int n_pools) {
     return a;
 }
 
-// CTAs per pool: enough warps for every piece of `jobs` pages (jobs < 0: not known), at most four waves of 8 CTAs
-// per SM over all pools.
+// CTAs per pool: enough warps for every piece of `jobs` pages, at most 8 CTAs per SM over all pools (two waves of the four
+// that are resident with 62 or 64 registers a thread).  Fork and compaction raise it to what their tables take.
 unsigned copy_grid(const ac_page_pool* pools, int n_pools, long long jobs, int sms) {
     long long most = 1;
     for (int i = 0; i < n_pools; ++i) {

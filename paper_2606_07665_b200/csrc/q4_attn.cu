@@ -29,8 +29,8 @@
 //
 // Bound: HBM in principle, with the arithmetic right behind it.  4 rows of 131072 tokens, 64:8 heads of 128, group 64 (604
 // MB): the loads alone take 92 to 97 us, the arithmetic alone 93 (each measured with the other taken out), both
-// together 111 us = 5440 GB/s, 0.83 of the measured read rate of 6546; back to back for a second or more the board's power limit
-// makes it 135.  64 rows of 128 to 8192 tokens, 32:8 heads (285 MB): 58 us = 4900 GB/s.  The instructions per tile are those of
+// together 111 us = 5440 GB/s, 0.83 of the measured copy rate of 6546 (a stream that only reads reaches 7400: 0.74);
+// back to back for a second or more the board's power limit makes it 135.  64 rows of 128 to 8192 tokens, 32:8 heads (285 MB): 58 us = 4900 GB/s.  The instructions per tile are those of
 // unpacking (ALU) and of the per-token scales; the fp32 arithmetic is done on pairs of heads (add, mul and fma on f32x2:
 // 120.6 -> 116.0 us at 4 splits).
 #include <limits.h>
@@ -682,7 +682,8 @@ __global__ void __launch_bounds__(NW * 32, CTAS) paged_decode_attn_q4_kernel(con
 //   BASE   two CTAs per SM: the second one's stream covers the first one's start and end (the same long rows in 9 splits: 111);
 //   SLIM   three CTAs of four warps for grids of more than two waves' worth of short splits, where starts and ends are much
 //          of a CTA's life (256 rows of 512 to 2048 tokens: 42.1 against 47.1 us in BASE; 64 rows of up to 8192, unsplit: 83
-//          against 58, a long row's CTA is alone at the end).
+//          against 58, a long row's CTA is alone at the end).  The border between them, kSlimMaxSplitTokens, lies between these
+//          two; it was not swept.
 // With more than eight heads per KV head the accumulators double: four or eight warps, 255 registers.
 enum class Fit { FAT, BASE, SLIM };
 constexpr int kSlimMaxSplitTokens = 2560;
