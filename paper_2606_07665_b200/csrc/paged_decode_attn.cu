@@ -21,7 +21,8 @@
 // registers.  There it is rounded to bf16, the type of V (2^-8 relative a weight): the only rounding below
 // fp32 before the result's own, and the sum of the weights is that of the unrounded ones.  (32 rows of 4196
 // attended tokens: error 2.2e-3 of the result's norm, where rounding the exact result to bf16 alone is
-// 1.7e-3.)  Softmax is the online form (running max and sum per row, in the exp2 domain) with warp-shuffle reductions across the four lanes that share a row.  At the end the warps' partial
+// 1.7e-3.)  Softmax is the online form (running max and sum per row, in the exp2 domain) with
+// warp-shuffle reductions across the four lanes that share a row.  At the end the warps' partial
 // (max, sum, O) are combined through shared memory and the CTA writes either the final bf16 row
 // (one split) or its normalised fp32 partial plus the natural-log log-sum-exp (several splits).
 // With the fused merge the splits of a (request, KV head) are combined inside this kernel: by the CTA

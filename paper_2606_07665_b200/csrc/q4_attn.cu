@@ -30,9 +30,9 @@
 // Bound: HBM in principle, with the arithmetic right behind it.  4 rows of 131072 tokens, 64:8 heads of 128, group 64 (604
 // MB): the loads alone take 92 to 97 us, the arithmetic alone 93 (each measured with the other taken out), both
 // together 111 us = 5440 GB/s, 0.83 of the measured copy rate of 6546 (a stream that only reads reaches 7400: 0.74);
-// back to back for a second or more the board's power limit makes it 135.  64 rows of 128 to 8192 tokens, 32:8 heads (285 MB): 58 us = 4900 GB/s.  The instructions per tile are those of
-// unpacking (ALU) and of the per-token scales; the fp32 arithmetic is done on pairs of heads (add, mul and fma on f32x2:
-// 120.6 -> 116.0 us at 4 splits).
+// back to back for a second or more the board's power limit makes it 135.  64 rows of 128 to 8192 tokens, 32:8 heads
+// (285 MB): 58 us = 4900 GB/s.  The instructions per tile are those of unpacking (ALU) and of the per-token scales;
+// the fp32 arithmetic is done on pairs of heads (add, mul and fma on f32x2: 120.6 -> 116.0 us at 4 splits).
 #include <limits.h>
 #include <math.h>
 

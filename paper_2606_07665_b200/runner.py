@@ -305,7 +305,8 @@ class _OnDevice:
         if device.type != "cuda":
             raise ValueError(f"tensors on {device}, expected a CUDA device")
         self.device, self._index, self._lib = device, device.index, ac.lib()
-        self._streams, self._captured, self._kept = set(), False, []
+        self._streams = set()
+        self._captured = True                              # nobody asks, unless the buffers can be replaced
         with torch.cuda.device(device):
             ac.ac_init(device.index)
             self.status_flag = torch.zeros(1, dtype=torch.int32, device=device)
@@ -323,12 +324,6 @@ class _OnDevice:
         used = torch.cuda.ExternalStream(stream, device=self.device)
         for t in self._buffers():
             t.record_stream(used)
-
-    def _replace_buffers(self):
-        """Before the buffers are replaced: captured calls go on using the present ones."""
-        if self._captured:
-            self._kept.append(self._buffers())
-        self._streams, self._captured = set(), False
 
     def _new(self, shape, stream, dtype=torch.bfloat16):
         """A tensor that belongs to the stream that will write it, so that its memory is not handed to another one's work
@@ -378,6 +373,13 @@ class _Rows(_OnDevice):
     """A block table and context lengths, and the split plan of attention over them."""
 
     workspace = row_order = None
+    _kept = ()
+
+    def _replace_buffers(self):
+        """Before plan() replaces the buffers: captured calls go on using the present ones."""
+        if self._captured and self.workspace is not None:
+            self._kept += (self._buffers(),)
+        self._streams, self._captured = set(), False
 
     def _buffers(self):
         return [t for t in (self.status_flag, self.workspace, self.row_order) if t is not None]

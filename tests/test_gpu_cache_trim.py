@@ -32,7 +32,7 @@ def trimmed(b, flags=0):
 
 
 CASES = [([40, 16, 0, 33, 1, 15], 16, 64, 8, 12, [(0, 6)]), ([100], 48, 20, 4, 3, []), ([], 16, 37, 4, 3, []), ([5, 700, -1, 64], 32, 1001, 30, 9, [(1, 4), (1, 5)]),
-         ([300] * 20, 16, 20000, 25, 60, [(3, 22)]), ([15] * 1500, 16, 3000, 2, 1500, [])]
+         ([300] * 20, 16, 2000, 25, 60, [(3, 22)]), ([15] * 1500, 16, 3000, 2, 1500, [])]
 
 
 @pytest.mark.parametrize("lens,ps,num_pages,width,rows,shared", CASES)
