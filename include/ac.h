@@ -590,8 +590,9 @@ int ac_cache_fork(const ac_page_pool* pools, int n_pools, int32_t* block_table, 
                   int32_t* status_flag, void* stream);
 
 /* Drops the rows listed in row_list (device int32 [n]): the reference counts of their pages go down and
- * context_lens[row] becomes -1; the table entries stay, and so do pages reserved for them (see ac_cache_trim).  A row that is unused, or listed again, is a
- * no-op.  A count that is already 0 stays 0 and sets AC_FLAG_REF_COUNT. */
+ * context_lens[row] becomes -1; the table entries stay, and pages reserved for the rows stay taken (see
+ * ac_cache_trim).  A row that is unused, or listed again, is a no-op.  A count that is already 0 stays 0 and sets
+ * AC_FLAG_REF_COUNT. */
 int ac_cache_release(const int32_t* block_table, int max_pages_per_seq, int32_t* context_lens,
                      int32_t* ref_counts, const int32_t* row_list, int n, int rows, int page_size,
                      int num_pages, int32_t* status_flag, void* stream);

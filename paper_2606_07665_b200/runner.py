@@ -258,9 +258,10 @@ class AttentionBlockStep:
 # They validate once what stays (pools, tables, lengths) and per call what changes, keep the plan, the workspace
 # and the marshalled arguments, and enqueue on the current stream of their device (or on the one given).
 #
-# What an object allocates for itself stays allocated until every stream that it was used on is done with it, and for as long as the
-# object lives where a captured call uses it.  So plan() and the end of an object need no synchronisation; only a captured
-# graph must not be replayed beyond the object that it calls, and a stream given as a handle must outlive the object.
+# What an object allocates for itself stays allocated until every stream that it was used on is done with it, and for as
+# long as the object lives where a captured call uses it.  So plan() and the end of an object need no synchronisation;
+# only a captured graph must not be replayed beyond the objects that it calls, and a stream given as a handle must
+# outlive them.
 
 _BF16 = (torch.bfloat16, torch.int16)          # bf16 values, or their bits
 
@@ -725,8 +726,8 @@ class CachePages(_OnDevice):
                                               self._flag, None], stream, -1)
 
     def compact(self, table_out=None, refs_out=None, live_out=None, stream=None):
-        """Moves the live pages to the lowest ids; nothing may be reserved (trim() before it).  In place, or (both given) into another table and counts, so that
-        a step in flight can still read the old ones.  ``live_out`` int32 [1] receives the number of live pages."""
+        """Moves the live pages to the lowest ids; nothing may be reserved (trim() before it).  In place, or (both given)
+        into another table and counts, so that a step in flight can still read the old ones.  ``live_out`` int32 [1] receives the number of live pages."""
         if (table_out is None) != (refs_out is None):
             raise ValueError("table_out and refs_out go together")
         if table_out is None:

@@ -9,7 +9,7 @@ from tests.test_gpu_q4 import Case, bits, dev
 pytestmark = pytest.mark.gpu
 
 LENS = [5000, 100, 3000]
-WAIT = 400_000_000                    # cycles that the side stream is busy before the call: a fifth of a second
+WAIT = 1_000_000_000                  # cycles that the side stream is busy before the call: half a second
 
 
 @pytest.fixture(scope="module")
@@ -78,9 +78,10 @@ def test_buffers_outlive_the_calls_that_use_them(rt, kind, how, end):
     early = handed_out(old)
     busy = not side.query()
     torch.cuda.synchronize()
-    assert busy, "the side stream was done too early for this test to say anything"
-    assert not early
     assert torch.equal(out, want)
+    if not busy:
+        pytest.skip("the side stream was done too early for this test to say anything")
+    assert not early
     if end == "plan":
         call(None)                     # another split count, so other low bits
         torch.cuda.synchronize()
@@ -111,7 +112,9 @@ def test_pages_and_cache_buffers_outlive_the_calls_that_use_them(rt):
     early = handed_out(old)
     busy = not side.query()
     torch.cuda.synchronize()
-    assert busy and not early
+    if not busy:
+        pytest.skip("the side stream was done too early for this test to say anything")
+    assert not early
 
 
 @pytest.mark.parametrize("kind", ["q4", "bf16"])
