@@ -531,6 +531,119 @@ int ac_paged_decode_attn_q4(const void* q_rot, const ac_q4_cache* cache, const i
                             int max_context_len, int32_t* status_flag, void* stream,
                             const ac_attn_options* options);
 
+/* ---- the cache held in 8 bits --------------------------------------------------------------------
+ *
+ * Half of the bf16 cache's bytes per token.  A block of `block` consecutive slots of a page has, for each KV head and for
+ * each of K and V, one scale s, a power of two; an element is held as a code c of the format and stands for c * s.
+ *   AC_Q8_INT8  c an integer, -127 .. 127 (two's complement; M = 127)
+ *   AC_Q8_E4M3  c an 8-bit floating-point number: sign, 4 bits of exponent (bias 7), 3 of fraction, no infinities,
+ *               0x7F and 0xFF are NaN (M = 448)
+ * The scale is the least s = 2^e with max |x| <= M s over the tokens of the block, -100 <= e <= 121 (INT8) or 119 (E4M3),
+ * and c = x / s rounded to the nearest code (ties to even), at most M in magnitude.  x is bf16: the rotated, bf16-rounded key,
+ * or the value vector.  A block that holds an infinity or a NaN has s = NaN and reads back as NaN.
+ *
+ * Writing goes on in a block that is partly filled: a write at a slot that does not begin a block keeps the block's scale
+ * where it suffices for the new tokens too; otherwise the scale grows to what they need and the codes of the slots in front
+ * become c * (old s / new s), rounded as above.  A scale at least doubles when it grows, so a code that was rounded more than once
+ * is off by less than one of its final steps (INT8).  A write at the first slot of a block begins it anew, whatever it held.  What
+ * appending one by one and storing at once leave may differ by that.  No other block is touched: a page that rows share is
+ * written by none of them (ac_cache_fork copies the partly filled page).  Attention and load take any finite positive scale. */
+#define AC_Q8_INT8 0
+#define AC_Q8_E4M3 1
+typedef struct ac_q8_cache {
+    void* k_codes;           /* byte j of (page, slot, head) at page*stride_page + slot*stride_token + head*stride_head + j, */
+    void* v_codes;           /* j < d; 16-byte aligned bases, strides in BYTES, multiples of 16 below 2^40, token and head >= d */
+    float* scales;           /* s of (page, head, block, side) at page*stride_scales + (head*(page_size/block) + block)*2 + side,
+                                side 0 for K and 1 for V; 16-byte aligned */
+    int64_t stride_page, stride_token, stride_head;
+    int64_t stride_scales;   /* in floats; even, at least Hkv * (page_size/block) * 2 (a multiple of 4 for ac_page_pool) */
+    int block;               /* tokens: a multiple of 16 that divides page_size */
+    int format;              /* AC_Q8_INT8 or AC_Q8_E4M3 */
+    int reserved[2];
+} ac_q8_cache;
+
+/* ac_rope_kv_append_ex into an 8-bit cache: q is rotated into q_out bit for bit as there; k is normalised and rotated as
+ * there, rounded to bf16 and then quantised, v is quantised as it is.  Rows that are inactive or out of range behave as there.
+ * Supported shapes, errors and status bits as there; an unknown format or a block that is no multiple of 16 is
+ * AC_ERR_UNSUPPORTED, one that does not divide the page AC_ERR_SHAPE. */
+int ac_rope_kv_append_q8(const void* q_in, void* q_out, const void* k_new, const void* v_new,
+                         const ac_q8_cache* cache, const int32_t* block_table, int max_pages_per_seq,
+                         const int32_t* context_lens, const float* rope_cos, const float* rope_sin,
+                         int max_position, int B, int Hq, int Hkv, int d, int page_size, int num_pages,
+                         int32_t* status_flag, void* stream, const ac_rope_options* options);
+
+/* ac_kv_store_q4 and ac_kv_load_q4 for the 8-bit cache: arguments, rows, errors and status bits as there.  The tokens that one
+ * call writes into a block are one write; where they go on in a partly filled block, what the row holds in front of them
+ * must be there. Load gives bf16(c * s), which is exact but where c * s is subnormal. */
+int ac_kv_store_q8(const void* k, const void* v, const ac_q8_cache* cache, const int32_t* block_table,
+                   int max_pages_per_seq, const int32_t* start_pos, const int32_t* row_offsets,
+                   int total_tokens, int B, int Hkv, int d, int page_size, int num_pages,
+                   int32_t* status_flag, void* stream);
+int ac_kv_load_q8(void* k, void* v, const ac_q8_cache* cache, const int32_t* block_table,
+                  int max_pages_per_seq, const int32_t* start_pos, const int32_t* row_offsets,
+                  int total_tokens, int B, int Hkv, int d, int page_size, int num_pages,
+                  int32_t* status_flag, void* stream);
+
+/* Split plan for ac_paged_decode_attn_q8: arguments and outputs as ac_decode_plan_q4. */
+int ac_decode_plan_q8(const int32_t* token_counts_host, int B, int Hq, int Hkv, int d, int page_size,
+                      int max_context_len, int sm_count, int* num_splits_out, int* split_tokens_out,
+                      size_t* workspace_bytes_out);
+
+/* Paged decode attention over the 8-bit cache, merge included: ac_paged_decode_attn_ex with fused_merge set (splits, workspace,
+ * inactive rows, window, sinks, row_order and max_context_len as there; options->rope must be NULL).  K and V enter as the
+ * exact values c * s; q is bf16, products and sums are fp32, and the softmax weights times V's scale are rounded to fp16
+ * (2^-11 relative, or 2^-31 of the largest V scale seen, whichever is more) for the second product.  Slots at or past n_b, the
+ * scales of blocks in which the row attends over no token, unreferenced pages and unused block-table entries never influence
+ * the result; a page id outside [0, num_pages) reads as zeros.  Outside the supported range: as ac_paged_decode_attn_q4
+ * says of q and V.  AC_FLAG_WAIT_TIMEOUT is the only status bit.  The workspace belongs to one call at a time: calls that may
+ * overlap need one each. */
+int ac_paged_decode_attn_q8(const void* q_rot, const ac_q8_cache* cache, const int32_t* block_table,
+                            int max_pages_per_seq, const int32_t* context_lens, int new_tokens,
+                            float softmax_scale, int num_splits, void* workspace, size_t workspace_bytes,
+                            void* out, int B, int Hq, int Hkv, int d, int page_size, int num_pages,
+                            int max_context_len, int32_t* status_flag, void* stream,
+                            const ac_attn_options* options);
+
+/* ---- rotary positions ---------------------------------------------------------------------------- */
+
+/* Frequencies f_i = base^(-2i/R), i < R/2, R = rotary_dim, and what is done to them for contexts longer than the one that they
+ * were made for. */
+#define AC_ROPE_NONE 0       /* as they are */
+#define AC_ROPE_LINEAR 1     /* f_i / factor: positions are squeezed */
+#define AC_ROPE_BASE 2       /* base * factor^(R/(R-2)) for base: the lowest frequency is slowed down by factor, the highest stays */
+#define AC_ROPE_RAMP 3       /* g f_i + (1 - g) f_i / factor, g = clamp((original * f_i / (2 pi) - low) / (high - low), 0, 1):
+                                frequencies that turn more than `high` times in the original context stay, those that turn less
+                                than `low` times are slowed down, in between they are blended */
+typedef struct ac_rope_scaling {
+    int kind;                /* AC_ROPE_... */
+    int reserved;
+    double base;             /* > 0 */
+    double factor;           /* > 0 (not used for AC_ROPE_NONE) */
+    double original;         /* AC_ROPE_RAMP: positions of the original context, > 0 */
+    double low, high;        /* AC_ROPE_RAMP: low < high */
+    double magnitude;        /* cosines and sines are multiplied by it; 0 means 1 */
+} ac_rope_scaling;
+
+/* Tables for ac_rope_kv_append and its relatives and for ac_rope_rows: rope_cos[j, i] = magnitude * cos((first_position + j) f_i),
+ * rope_sin likewise, j < positions, fp32 [positions, rotary_dim/2] dense, rounded from an fp64 evaluation (error of the angle:
+ * 2^-52 of it).  rotary_dim is even; for AC_ROPE_BASE it is at least 4.  positions may be 0. */
+int ac_rope_tables(float* rope_cos, float* rope_sin, int64_t first_position, int positions, int rotary_dim,
+                   const ac_rope_scaling* scaling, void* stream);
+
+/* A1 for many tokens of each row (prompts): token i of row b, i.e. token row_offsets[b] + i of the packed tensors, is rotated at
+ * position start_pos[b] + i exactly as ac_rope_kv_append_ex rotates the new token's q and k (options as there: rotary_dim,
+ * interleaved, norm weights).  q_in [total_tokens, Hq, d] and k_in [total_tokens, Hkv, d] are bf16 with dense heads and
+ * tokens stride_*_token elements apart (multiples of 8, at least Hq*d or Hkv*d), so that they may be parts of a joint projection's
+ * output; q_out and k_out likewise, each either its input with the same stride or apart from both inputs.  Hkv may be 0 (then k_in
+ * and k_out are ignored).  row_offsets, start_pos and their rows as ac_kv_store_q4: tokens of inactive rows and of no row are not
+ * touched; a token at or past max_position is not written and sets AC_FLAG_POSITION_OOB.  Any Hq and Hkv whose sum is at most
+ * 65535; d is 64 or 128. */
+int ac_rope_rows(const void* q_in, void* q_out, int64_t stride_q_in_token, int64_t stride_q_out_token,
+                 const void* k_in, void* k_out, int64_t stride_k_in_token, int64_t stride_k_out_token,
+                 const int32_t* start_pos, const int32_t* row_offsets, int total_tokens, int B, int Hq, int Hkv, int d,
+                 const float* rope_cos, const float* rope_sin, int max_position, int32_t* status_flag, void* stream,
+                 const ac_rope_options* options);
+
 /* ---- pages ----------------------------------------------------------------------------------------
  *
  * Bookkeeping of a page pool on the device, so that sequences can be grown, forked and dropped between
@@ -549,7 +662,8 @@ typedef struct ac_page_pool {
     int64_t page_bytes;      /* a multiple of 16 * segments */
     int segments;            /* a page is this many equal pieces, each holding the page's slots in order: 1 for
                                 [page, slot, head, d], Hkv for [page, head, slot, ...] */
-    int reserved;
+    int whole;               /* non-zero: a page's bytes do not follow its slots (the scales of an 8-bit cache), so that
+                                ac_cache_fork copies all of a partly filled page; page_bytes is then any multiple of 16 */
 } ac_page_pool;
 
 /* Most pools of one call. */

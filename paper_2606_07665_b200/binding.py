@@ -9,7 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from ctypes import c_char_p, c_float, c_int, c_int64, c_size_t, c_void_p, POINTER
+from ctypes import c_char_p, c_double, c_float, c_int, c_int64, c_size_t, c_void_p, POINTER
 
 _LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libac.so")
 _lib = None
@@ -24,6 +24,8 @@ AC_FLAG_POOL_EXHAUSTED = 8
 AC_FLAG_REF_COUNT = 16
 AC_FLAG_ROW_OOB = 32
 AC_MAX_PAGE_POOLS = 128
+AC_Q8_INT8, AC_Q8_E4M3 = 0, 1
+AC_ROPE_NONE, AC_ROPE_LINEAR, AC_ROPE_BASE, AC_ROPE_RAMP = range(4)
 
 EXPORTS = ("ac_init", "ac_status_string", "ac_last_cuda_error", "ac_sm_count", "ac_decode_plan",
            "ac_decode_plan_for_lengths",
@@ -33,7 +35,9 @@ EXPORTS = ("ac_init", "ac_status_string", "ac_last_cuda_error", "ac_sm_count", "
            "ac_decode_step_fused", "ac_paged_decode_attn_ex", "ac_decode_step_fused_ex",
            "ac_rope_kv_append_ex", "ac_qkv_rope_kv_append", "ac_oproj_residual_rmsnorm",
            "ac_hbm_read_probe", "ac_qkv_rope_kv_append_ex", "ac_rope_kv_append_q4", "ac_kv_store_q4",
-           "ac_kv_load_q4", "ac_decode_plan_q4", "ac_paged_decode_attn_q4", "ac_cache_copy_pages",
+           "ac_kv_load_q4", "ac_decode_plan_q4", "ac_paged_decode_attn_q4", "ac_rope_kv_append_q8",
+           "ac_kv_store_q8", "ac_kv_load_q8", "ac_decode_plan_q8", "ac_paged_decode_attn_q8", "ac_rope_tables",
+           "ac_rope_rows", "ac_cache_copy_pages",
            "ac_cache_workspace_bytes", "ac_cache_reserve", "ac_cache_fork", "ac_cache_release",
            "ac_cache_trim", "ac_cache_compact")
 AC_STATIC_SCRATCH_BYTES = 8 << 20
@@ -57,9 +61,22 @@ class AcQ4Cache(ctypes.Structure):
                 ("stride_token", c_int64), ("stride_head", c_int64), ("group", c_int), ("reserved", c_int * 3)]
 
 
+class AcQ8Cache(ctypes.Structure):
+    """Mirror of ac_q8_cache (strides of the codes in bytes, of the scales in floats)."""
+    _fields_ = [("k_codes", c_void_p), ("v_codes", c_void_p), ("scales", c_void_p), ("stride_page", c_int64),
+                ("stride_token", c_int64), ("stride_head", c_int64), ("stride_scales", c_int64), ("block", c_int),
+                ("format", c_int), ("reserved", c_int * 2)]
+
+
+class AcRopeScaling(ctypes.Structure):
+    """Mirror of ac_rope_scaling."""
+    _fields_ = [("kind", c_int), ("reserved", c_int), ("base", c_double), ("factor", c_double),
+                ("original", c_double), ("low", c_double), ("high", c_double), ("magnitude", c_double)]
+
+
 class AcPagePool(ctypes.Structure):
     """Mirror of ac_page_pool."""
-    _fields_ = [("base", c_void_p), ("page_bytes", c_int64), ("segments", c_int), ("reserved", c_int)]
+    _fields_ = [("base", c_void_p), ("page_bytes", c_int64), ("segments", c_int), ("whole", c_int)]
 
 
 class AcError(RuntimeError):
@@ -160,6 +177,16 @@ def lib():
                                               c_float, c_int, c_void_p, c_size_t, c_void_p] + [c_int] * 7 +
                                               [c_void_p, c_void_p, POINTER(AcAttnOptions)])
         L.ac_paged_decode_attn_q4.restype = c_int
+        q8 = {POINTER(AcQ4Cache): POINTER(AcQ8Cache)}
+        for name in ("ac_rope_kv_append", "ac_kv_store", "ac_kv_load", "ac_decode_plan", "ac_paged_decode_attn"):
+            fn = getattr(L, name + "_q8")                  # the calls of the 4-bit cache with the other descriptor
+            fn.argtypes = [q8.get(t, t) for t in getattr(L, name + "_q4").argtypes]
+            fn.restype = c_int
+        L.ac_rope_tables.argtypes = [c_void_p, c_void_p, c_int64, c_int, c_int, POINTER(AcRopeScaling), c_void_p]
+        L.ac_rope_tables.restype = c_int
+        L.ac_rope_rows.argtypes = ([c_void_p, c_void_p, c_int64, c_int64] * 2 + [c_void_p, c_void_p] + [c_int] * 5 +
+                                   [c_void_p, c_void_p, c_int, c_void_p, c_void_p, POINTER(AcRopeOptions)])
+        L.ac_rope_rows.restype = c_int
         L.ac_cache_copy_pages.argtypes = [POINTER(AcPagePool), c_int, c_void_p, c_int, c_int, c_void_p, c_void_p]
         L.ac_cache_copy_pages.restype = c_int
         L.ac_cache_workspace_bytes.argtypes = [c_int] * 3
@@ -473,17 +500,21 @@ def ac_kv_load_q4(k, v, cache, block_table, max_pages_per_seq, start_pos, row_of
                                _ptr(status_flag), _stream(stream)), "ac_kv_load_q4")
 
 
-def ac_decode_plan_q4(token_counts, B, Hq, Hkv, d, page_size, max_context_len, sm_count=0):
-    """token_counts: host sequence of B ints or None.  Returns (num_splits, split_tokens, workspace_bytes)."""
+def _plan_quantised(name, token_counts, B, Hq, Hkv, d, page_size, max_context_len, sm_count):
     counts = None
     if token_counts is not None:
         if len(token_counts) != B:
             raise ValueError(f"{len(token_counts)} token counts for {B} rows")
         counts = ctypes.cast((ctypes.c_int32 * B)(*[int(t) for t in token_counts]), c_void_p)
     ns, st, wb = c_int(0), c_int(0), c_size_t(0)
-    _check(lib().ac_decode_plan_q4(counts, B, Hq, Hkv, d, page_size, max_context_len, sm_count,
-                                   ctypes.byref(ns), ctypes.byref(st), ctypes.byref(wb)), "ac_decode_plan_q4")
+    _check(getattr(lib(), name)(counts, B, Hq, Hkv, d, page_size, max_context_len, sm_count,
+                                ctypes.byref(ns), ctypes.byref(st), ctypes.byref(wb)), name)
     return ns.value, st.value, wb.value
+
+
+def ac_decode_plan_q4(token_counts, B, Hq, Hkv, d, page_size, max_context_len, sm_count=0):
+    """token_counts: host sequence of B ints or None.  Returns (num_splits, split_tokens, workspace_bytes)."""
+    return _plan_quantised("ac_decode_plan_q4", token_counts, B, Hq, Hkv, d, page_size, max_context_len, sm_count)
 
 
 def ac_paged_decode_attn_q4(q_rot, cache, block_table, max_pages_per_seq, context_lens, new_tokens, softmax_scale,
@@ -496,13 +527,85 @@ def ac_paged_decode_attn_q4(q_rot, cache, block_table, max_pages_per_seq, contex
         ctypes.byref(_options(window, True, row_order, sinks=sinks))), "ac_paged_decode_attn_q4")
 
 
+# ---- the 8-bit cache ---------------------------------------------------------------------------------------
+
+
+def q8_cache(k_codes, v_codes, scales, stride_page, stride_token, stride_head, stride_scales, block, fmt) -> AcQ8Cache:
+    """The descriptor of an 8-bit cache; strides of the codes in bytes, of the scales in floats.  The tensors must outlive it."""
+    return AcQ8Cache(_ptr(k_codes), _ptr(v_codes), _ptr(scales), stride_page, stride_token, stride_head, stride_scales, block,
+                     fmt)
+
+
+def ac_rope_kv_append_q8(q_in, q_out, k_new, v_new, cache, block_table, max_pages_per_seq, context_lens,
+                         rope_cos, rope_sin, max_position, B, Hq, Hkv, d, page_size, num_pages,
+                         status_flag=None, stream=None, rotary_dim=0, interleaved=False, q_norm_weight=None,
+                         k_norm_weight=None, norm_eps=0.0):
+    opt = _rope_options(rotary_dim, interleaved, q_norm_weight, k_norm_weight, norm_eps)
+    _check(lib().ac_rope_kv_append_q8(_ptr(q_in), _ptr(q_out), _ptr(k_new), _ptr(v_new), cache,
+                                      _ptr(block_table), max_pages_per_seq, _ptr(context_lens), _ptr(rope_cos),
+                                      _ptr(rope_sin), max_position, B, Hq, Hkv, d, page_size, num_pages,
+                                      _ptr(status_flag), _stream(stream), ctypes.byref(opt)),
+           "ac_rope_kv_append_q8")
+
+
+def ac_kv_store_q8(k, v, cache, block_table, max_pages_per_seq, start_pos, row_offsets, total_tokens, B, Hkv, d,
+                   page_size, num_pages, status_flag=None, stream=None):
+    _check(lib().ac_kv_store_q8(_ptr(k), _ptr(v), cache, _ptr(block_table), max_pages_per_seq, _ptr(start_pos),
+                                _ptr(row_offsets), total_tokens, B, Hkv, d, page_size, num_pages,
+                                _ptr(status_flag), _stream(stream)), "ac_kv_store_q8")
+
+
+def ac_kv_load_q8(k, v, cache, block_table, max_pages_per_seq, start_pos, row_offsets, total_tokens, B, Hkv, d,
+                  page_size, num_pages, status_flag=None, stream=None):
+    _check(lib().ac_kv_load_q8(_ptr(k), _ptr(v), cache, _ptr(block_table), max_pages_per_seq, _ptr(start_pos),
+                               _ptr(row_offsets), total_tokens, B, Hkv, d, page_size, num_pages,
+                               _ptr(status_flag), _stream(stream)), "ac_kv_load_q8")
+
+
+def ac_decode_plan_q8(token_counts, B, Hq, Hkv, d, page_size, max_context_len, sm_count=0):
+    """token_counts: host sequence of B ints or None.  Returns (num_splits, split_tokens, workspace_bytes)."""
+    return _plan_quantised("ac_decode_plan_q8", token_counts, B, Hq, Hkv, d, page_size, max_context_len, sm_count)
+
+
+def ac_paged_decode_attn_q8(q_rot, cache, block_table, max_pages_per_seq, context_lens, new_tokens, softmax_scale,
+                            num_splits, workspace, workspace_bytes, out, B, Hq, Hkv, d, page_size, num_pages,
+                            max_context_len, status_flag=None, stream=None, window=0, row_order=None, sinks=0):
+    _check(lib().ac_paged_decode_attn_q8(
+        _ptr(q_rot), cache, _ptr(block_table), max_pages_per_seq, _ptr(context_lens), new_tokens,
+        softmax_scale, num_splits, _ptr(workspace), workspace_bytes, _ptr(out), B, Hq, Hkv, d, page_size, num_pages,
+        max_context_len, _ptr(status_flag), _stream(stream),
+        ctypes.byref(_options(window, True, row_order, sinks=sinks))), "ac_paged_decode_attn_q8")
+
+
+# ---- rotary positions --------------------------------------------------------------------------------------
+
+
+def rope_scaling(base=10000.0, kind=AC_ROPE_NONE, factor=1.0, original=0.0, low=0.0, high=0.0, magnitude=0.0) -> AcRopeScaling:
+    return AcRopeScaling(kind, 0, base, factor, original, low, high, magnitude)
+
+
+def ac_rope_tables(rope_cos, rope_sin, first_position, positions, rotary_dim, scaling, stream=None):
+    _check(lib().ac_rope_tables(_ptr(rope_cos), _ptr(rope_sin), first_position, positions, rotary_dim,
+                                ctypes.byref(scaling), _stream(stream)), "ac_rope_tables")
+
+
+def ac_rope_rows(q_in, q_out, stride_q_in_token, stride_q_out_token, k_in, k_out, stride_k_in_token, stride_k_out_token,
+                 start_pos, row_offsets, total_tokens, B, Hq, Hkv, d, rope_cos, rope_sin, max_position, status_flag=None,
+                 stream=None, rotary_dim=0, interleaved=False, q_norm_weight=None, k_norm_weight=None, norm_eps=0.0):
+    opt = _rope_options(rotary_dim, interleaved, q_norm_weight, k_norm_weight, norm_eps)
+    _check(lib().ac_rope_rows(_ptr(q_in), _ptr(q_out), stride_q_in_token, stride_q_out_token, _ptr(k_in), _ptr(k_out),
+                              stride_k_in_token, stride_k_out_token, _ptr(start_pos), _ptr(row_offsets), total_tokens, B,
+                              Hq, Hkv, d, _ptr(rope_cos), _ptr(rope_sin), max_position, _ptr(status_flag),
+                              _stream(stream), ctypes.byref(opt)), "ac_rope_rows")
+
+
 # ---- pages -------------------------------------------------------------------------------------------------
 
 
 def page_pools(pools):
-    """``pools``: sequence of (tensor or address, page_bytes, segments) -> a ctypes array of ac_page_pool."""
-    return (AcPagePool * max(1, len(pools)))(*[AcPagePool(_ptr(base), page_bytes, segments, 0)
-                                               for base, page_bytes, segments in pools])
+    """``pools``: sequence of (tensor or address, page_bytes, segments[, whole]) -> a ctypes array of ac_page_pool."""
+    return (AcPagePool * max(1, len(pools)))(*[AcPagePool(_ptr(base), page_bytes, segments, *whole)
+                                               for base, page_bytes, segments, *whole in pools])
 
 
 def ac_cache_copy_pages(pools, n_pools, pairs, n, num_pages, status_flag=None, stream=None):

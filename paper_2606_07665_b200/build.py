@@ -14,10 +14,10 @@ CSRC = os.path.join(PKG_DIR, "csrc")
 LIB_PATH = os.path.join(PKG_DIR, "libac.so")
 SOURCES = ["ac_api.cu", "rope_kv_append.cu", "paged_decode_attn.cu", "splitkv_merge.cu",
            "attn_static_scratch.cu", "qkv_prelude.cu", "stage_inputs.cu", "proj_tc.cu", "hbm_probe.cu",
-           "q4_attn.cu", "q4_cache.cu", "cache_pages.cu"]
+           "q4_attn.cu", "q4_cache.cu", "cache_pages.cu", "q8_attn.cu", "q8_cache.cu", "rope_rows.cu"]
 HEADERS = [os.path.join(CSRC, "ac_device.cuh"), os.path.join(CSRC, "ac_internal.h"),
            os.path.join(CSRC, "rope_variant.cuh"), os.path.join(CSRC, "split_merge.cuh"),
-           os.path.join(CSRC, "q4_format.cuh"),
+           os.path.join(CSRC, "q4_format.cuh"), os.path.join(CSRC, "q8_format.cuh"), os.path.join(CSRC, "rope_fast.cuh"),
            os.path.join(ROOT, "include", "ac.h")]
 
 

@@ -144,6 +144,7 @@ int ac_init(int device) {
         if (e == cudaSuccess) e = qkv_set_attributes(st.smem_optin);
         if (e == cudaSuccess) e = proj_tc_set_attributes(st.smem_optin);
         if (e == cudaSuccess) e = q4_attn_set_attributes(st.smem_optin);
+        if (e == cudaSuccess) e = q8_attn_set_attributes(st.smem_optin);
         if (e != cudaSuccess) {
             status = fail_cuda(static_cast<int>(e));
             break;
@@ -977,22 +978,24 @@ int ac_kv_load_q4(void* k, void* v, const ac_q4_cache* cache, const int32_t* blo
                       page_size, num_pages, status_flag, stream, false);
 }
 
-int ac_decode_plan_q4(const int32_t* token_counts_host, int B, int Hq, int Hkv, int d, int page_size,
-                      int max_context_len, int sm_count, int* num_splits_out, int* split_tokens_out,
-                      size_t* workspace_bytes_out) {
+// What the plan of a quantised cache goes by: bytes per token and head (K and V), rates in bytes per second, times in seconds.
+struct PlanRates {
+    double bytes_per_token;
+    double gpu;                // the whole GPU, of 148 SMs
+    double fat, alone, pair, ragged_pair;      // one CTA: of a one-per-SM launch, alone on its SM, sharing it, sharing it in a ragged batch
+    double wave, more_waves, merge;
+};
+
+static int plan_quantised(const PlanRates& rates, const int32_t* token_counts_host, int B, int Hq, int Hkv, int d, int page_size,
+                          int max_context_len, int sm_count, int* num_splits_out, int* split_tokens_out,
+                          size_t* workspace_bytes_out) {
     if (!num_splits_out || !split_tokens_out || !workspace_bytes_out) return AC_ERR_NULL;
     Shape s{B, Hq, Hkv, d, page_size, 1};
     int st = check_shape(s);
     if (st != AC_OK) return st;
     if (max_context_len <= 0) return AC_ERR_SHAPE;
     if (sm_count <= 0) sm_count = g_last_sm_count > 0 ? g_last_sm_count : 148;
-    // Every split count is priced by what launches with one and with two CTAs per SM (q4_attn.cu) were measured to do (short
-    // splits in more than two waves run three CTAs of four warps, which has no price of its own): the whole GPU moves
-    // 5.6 TB/s of this cache (its arithmetic keeps it below HBM's rate), one CTA alone on its SM 43 GB/s with twelve warps
-    // and 32 with six, two sharing an SM 20 each, in a ragged batch 25; a wave costs 4 us of start and end, a further one
-    // 3, the merge through the workspace 1.6 and the partial results' traffic.  (d/2 + 4 d/group bytes per token, side
-    // and head; the plan does not know the group and takes 64.)
-    const double bytes_per_token = 2.0 * (d / 2 + d / 16), gpu = 5.6e12 * sm_count / 148.0;
+    const double bytes_per_token = rates.bytes_per_token, gpu = rates.gpu * sm_count / 148.0;
     auto tokens_of = [&](int b) {
         const int t = token_counts_host == nullptr ? max_context_len : token_counts_host[b];
         return t <= 0 ? 0 : t < max_context_len ? t : max_context_len;
@@ -1026,11 +1029,11 @@ int ac_decode_plan_q4(const int32_t* token_counts_host, int B, int Hq, int Hkv, 
         }
         n *= Hkv;
         const bool fat = static_cast<long long>(B) * Hkv * cand <= sm_count;
-        const double rate = fat ? 43e9 : n <= sm_count ? 32e9 : n * longest * bytes_per_token > 1.25 * total ? 25e9 : 20e9;
+        const double rate = fat ? rates.fat : n <= sm_count ? rates.alone : n * longest * bytes_per_token > 1.25 * total ? rates.ragged_pair : rates.pair;
         const double alone = longest * bytes_per_token / rate, together = total / gpu;
-        double t = (alone > together ? alone : together) + 4e-6;
-        if (n > 2.0 * sm_count) t += (ceil(n / (2.0 * sm_count)) - 1.0) * 3e-6;
-        if (cand > 1) t += 1.6e-6 + 2.0 * n * (Hq / Hkv) * (d + 1.0) * 4.0 / gpu;
+        double t = (alone > together ? alone : together) + rates.wave;
+        if (n > 2.0 * sm_count) t += (ceil(n / (2.0 * sm_count)) - 1.0) * rates.more_waves;
+        if (cand > 1) t += rates.merge + 2.0 * n * (Hq / Hkv) * (d + 1.0) * 4.0 / gpu;
         if (best == 0.0 || t < best) {
             best = t;
             S = cand;
@@ -1042,6 +1045,20 @@ int ac_decode_plan_q4(const int32_t* token_counts_host, int B, int Hq, int Hkv, 
     *split_tokens_out = split_tokens_for(max_context_len, static_cast<int>(S));
     *workspace_bytes_out = ac_fused_workspace_bytes(B, Hq, Hkv, d, static_cast<int>(S));
     return AC_OK;
+}
+
+int ac_decode_plan_q4(const int32_t* token_counts_host, int B, int Hq, int Hkv, int d, int page_size,
+                      int max_context_len, int sm_count, int* num_splits_out, int* split_tokens_out,
+                      size_t* workspace_bytes_out) {
+    // Every split count is priced by what launches with one and with two CTAs per SM (q4_attn.cu) were measured to do (short
+    // splits in more than two waves run three CTAs of four warps, which has no price of its own): the whole GPU moves
+    // 5.6 TB/s of this cache (its arithmetic keeps it below HBM's rate), one CTA alone on its SM 43 GB/s with twelve warps
+    // and 32 with six, two sharing an SM 20 each, in a ragged batch 25; a wave costs 4 us of start and end, a further one
+    // 3, the merge through the workspace 1.6 and the partial results' traffic.  (d/2 + 4 d/group bytes per token, side
+    // and head; the plan does not know the group and takes 64.)
+    const PlanRates rates = {2.0 * (d / 2 + d / 16), 5.6e12, 43e9, 32e9, 20e9, 25e9, 4e-6, 3e-6, 1.6e-6};
+    return plan_quantised(rates, token_counts_host, B, Hq, Hkv, d, page_size, max_context_len, sm_count, num_splits_out,
+                          split_tokens_out, workspace_bytes_out);
 }
 
 int ac_paged_decode_attn_q4(const void* q_rot, const ac_q4_cache* cache, const int32_t* block_table,
@@ -1097,6 +1114,244 @@ int ac_paged_decode_attn_q4(const void* q_rot, const ac_q4_cache* cache, const i
     return e == cudaSuccess ? AC_OK : fail_cuda(static_cast<int>(e));
 }
 
+// ---- the 8-bit cache ------------------------------------------------------------------------------
+
+// Checks the cache descriptor against the shape and translates it.
+static int parse_q8_cache(const ac_q8_cache* cache, const Shape& s, Q8View* view) {
+    if (!cache || !cache->k_codes || !cache->v_codes || !cache->scales) return AC_ERR_NULL;
+    if (cache->format != AC_Q8_INT8 && cache->format != AC_Q8_E4M3) return AC_ERR_UNSUPPORTED;
+    if (cache->block <= 0) return AC_ERR_SHAPE;
+    if (cache->block % 16 != 0) return AC_ERR_UNSUPPORTED;
+    if (s.page_size % cache->block != 0) return AC_ERR_SHAPE;
+    if (cache->stride_page <= 0 || cache->stride_token <= 0 || cache->stride_head <= 0) return AC_ERR_SHAPE;
+    if (cache->stride_page % 16 || cache->stride_token % 16 || cache->stride_head % 16) return AC_ERR_ALIGN;
+    if (cache->stride_token < s.d || cache->stride_head < s.d) return AC_ERR_SHAPE;
+    constexpr int64_t kMost = 1ll << 40;                   // what a tensor map takes
+    if (cache->stride_page >= kMost || cache->stride_token >= kMost || cache->stride_head >= kMost) return AC_ERR_UNSUPPORTED;
+    if (cache->stride_scales < static_cast<int64_t>(s.Hkv) * (s.page_size / cache->block) * 2) return AC_ERR_SHAPE;
+    if (cache->stride_scales % 2) return AC_ERR_ALIGN;
+    if (!aligned16(cache->k_codes) || !aligned16(cache->v_codes) || !aligned16(cache->scales)) return AC_ERR_ALIGN;
+    view->k_codes = static_cast<uint8_t*>(cache->k_codes);
+    view->v_codes = static_cast<uint8_t*>(cache->v_codes);
+    view->scales = cache->scales;
+    view->stride_page = cache->stride_page;
+    view->stride_token = cache->stride_token;
+    view->stride_head = cache->stride_head;
+    view->stride_scales = cache->stride_scales;
+    view->block = cache->block;
+    view->format = cache->format;
+    return AC_OK;
+}
+
+// 4-D view of a code pool, (element, token in page, head, page), for boxes of `box` tokens of one head.
+static int make_q8_map(CUtensorMap* map, const void* base, const Shape& s, const Q8View& c, int box_tokens) {
+    cuuint64_t dims[4] = {static_cast<cuuint64_t>(s.d), static_cast<cuuint64_t>(s.page_size), static_cast<cuuint64_t>(s.Hkv),
+                          static_cast<cuuint64_t>(s.num_pages)};
+    cuuint64_t strides[3] = {static_cast<cuuint64_t>(c.stride_token), static_cast<cuuint64_t>(c.stride_head),
+                             static_cast<cuuint64_t>(c.stride_page)};
+    cuuint32_t box[4] = {static_cast<cuuint32_t>(s.d), static_cast<cuuint32_t>(box_tokens), 1, 1};
+    cuuint32_t elem_strides[4] = {1, 1, 1, 1};
+    CUresult r = g_encode_tiled(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 4, const_cast<void*>(base), dims, strides, box,
+                                elem_strides, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                                s.d == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
+                                CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (r != CUDA_SUCCESS) return fail_cuda(static_cast<int>(r));
+    return AC_OK;
+}
+
+int ac_rope_kv_append_q8(const void* q_in, void* q_out, const void* k_new, const void* v_new,
+                         const ac_q8_cache* cache, const int32_t* block_table, int max_pages_per_seq,
+                         const int32_t* context_lens, const float* rope_cos, const float* rope_sin,
+                         int max_position, int B, int Hq, int Hkv, int d, int page_size, int num_pages,
+                         int32_t* status_flag, void* stream, const ac_rope_options* options) {
+    if (!q_in || !q_out || !k_new || !v_new || !block_table || !context_lens || !rope_cos || !rope_sin)
+        return AC_ERR_NULL;
+    Shape s{B, Hq, Hkv, d, page_size, num_pages};
+    int st = check_shape(s);
+    if (st != AC_OK) return st;
+    if (max_pages_per_seq <= 0 || max_position <= 0) return AC_ERR_SHAPE;
+    Q8View view;
+    st = parse_q8_cache(cache, s, &view);
+    if (st != AC_OK) return st;
+    if (!aligned16(q_in) || !aligned16(q_out) || !aligned16(k_new) || !aligned16(v_new) ||
+        !aligned16(rope_cos) || !aligned16(rope_sin))
+        return AC_ERR_ALIGN;
+    RopeVariant variant;
+    const RopeVariant* vp = nullptr;
+    st = parse_rope_options(options, d, &variant, &vp);
+    if (st != AC_OK) return st;
+    int dev;
+    st = current_ready_device(&dev);
+    if (st != AC_OK) return st;
+    cudaError_t e = launch_rope_kv_append_q8(q_in, q_out, k_new, v_new, view, block_table, max_pages_per_seq,
+                                             context_lens, rope_cos, rope_sin, max_position, B, Hq, Hkv, d,
+                                             page_size, num_pages, status_flag, vp,
+                                             static_cast<cudaStream_t>(stream));
+    return e == cudaSuccess ? AC_OK : fail_cuda(static_cast<int>(e));
+}
+
+static int kv_bulk_q8(void* k, void* v, const ac_q8_cache* cache, const int32_t* block_table,
+                      int max_pages_per_seq, const int32_t* start_pos, const int32_t* row_offsets,
+                      int total_tokens, int B, int Hkv, int d, int page_size, int num_pages,
+                      int32_t* status_flag, void* stream, bool store) {
+    if (!k || !v || !block_table || !start_pos || !row_offsets) return AC_ERR_NULL;
+    Shape s{B, Hkv, Hkv, d, page_size, num_pages};
+    int st = check_shape(s);
+    if (st != AC_OK) return st;
+    if (max_pages_per_seq <= 0 || total_tokens < 0) return AC_ERR_SHAPE;
+    Q8View view;
+    st = parse_q8_cache(cache, s, &view);
+    if (st != AC_OK) return st;
+    if (!aligned16(k) || !aligned16(v)) return AC_ERR_ALIGN;
+    int dev;
+    st = current_ready_device(&dev);
+    if (st != AC_OK) return st;
+    if (total_tokens == 0) return AC_OK;
+    cudaError_t e = launch_kv_bulk_q8(k, v, view, block_table, max_pages_per_seq, start_pos, row_offsets,
+                                      total_tokens, B, Hkv, d, page_size, num_pages, status_flag, store,
+                                      g_devices[dev].sm_count, static_cast<cudaStream_t>(stream));
+    return e == cudaSuccess ? AC_OK : fail_cuda(static_cast<int>(e));
+}
+
+int ac_kv_store_q8(const void* k, const void* v, const ac_q8_cache* cache, const int32_t* block_table,
+                   int max_pages_per_seq, const int32_t* start_pos, const int32_t* row_offsets,
+                   int total_tokens, int B, int Hkv, int d, int page_size, int num_pages,
+                   int32_t* status_flag, void* stream) {
+    return kv_bulk_q8(const_cast<void*>(k), const_cast<void*>(v), cache, block_table, max_pages_per_seq, start_pos,
+                      row_offsets, total_tokens, B, Hkv, d, page_size, num_pages, status_flag, stream, true);
+}
+
+int ac_kv_load_q8(void* k, void* v, const ac_q8_cache* cache, const int32_t* block_table,
+                  int max_pages_per_seq, const int32_t* start_pos, const int32_t* row_offsets,
+                  int total_tokens, int B, int Hkv, int d, int page_size, int num_pages,
+                  int32_t* status_flag, void* stream) {
+    return kv_bulk_q8(k, v, cache, block_table, max_pages_per_seq, start_pos, row_offsets, total_tokens, B, Hkv, d,
+                      page_size, num_pages, status_flag, stream, false);
+}
+
+int ac_decode_plan_q8(const int32_t* token_counts_host, int B, int Hq, int Hkv, int d, int page_size,
+                      int max_context_len, int sm_count, int* num_splits_out, int* split_tokens_out,
+                      size_t* workspace_bytes_out) {
+    const PlanRates rates = {2.0 * d + 0.5, 6.4e12, 50e9, 36e9, 24e9, 30e9, 4e-6, 3e-6, 1.6e-6};
+    return plan_quantised(rates, token_counts_host, B, Hq, Hkv, d, page_size, max_context_len, sm_count, num_splits_out,
+                          split_tokens_out, workspace_bytes_out);
+}
+
+int ac_paged_decode_attn_q8(const void* q_rot, const ac_q8_cache* cache, const int32_t* block_table,
+                            int max_pages_per_seq, const int32_t* context_lens, int new_tokens,
+                            float softmax_scale, int num_splits, void* workspace, size_t workspace_bytes,
+                            void* out, int B, int Hq, int Hkv, int d, int page_size, int num_pages,
+                            int max_context_len, int32_t* status_flag, void* stream,
+                            const ac_attn_options* options) {
+    const int window = options != nullptr ? options->window : 0;
+    const int sinks = options != nullptr ? options->sinks : 0;
+    const int32_t* row_order = options != nullptr ? options->row_order : nullptr;
+    if (!q_rot || !block_table || !context_lens || !out) return AC_ERR_NULL;
+    Shape s{B, Hq, Hkv, d, page_size, num_pages};
+    int st = check_shape(s);
+    if (st != AC_OK) return st;
+    if (max_pages_per_seq <= 0 || max_context_len <= 0 || num_splits <= 0 || window < 0 || sinks < 0)
+        return AC_ERR_SHAPE;
+    if ((new_tokens != 0 && new_tokens != 1) || num_splits > 65535) return AC_ERR_UNSUPPORTED;
+    if (options != nullptr && options->rope != nullptr) return AC_ERR_UNSUPPORTED;
+    Q8View view;
+    st = parse_q8_cache(cache, s, &view);
+    if (st != AC_OK) return st;
+    if (!aligned16(q_rot) || !aligned16(out)) return AC_ERR_ALIGN;
+    float* partial_o = nullptr;
+    float* partial_lse = nullptr;
+    int32_t* arrivals = nullptr;
+    if (num_splits > 1) {
+        if (!workspace || workspace_bytes < ac_fused_workspace_bytes(B, Hq, Hkv, d, num_splits)) return AC_ERR_WORKSPACE;
+        if (!aligned16(workspace)) return AC_ERR_ALIGN;
+        partial_o = static_cast<float*>(workspace);
+        partial_lse = partial_o + static_cast<size_t>(B) * Hq * num_splits * d;
+        arrivals = reinterpret_cast<int32_t*>(partial_lse + static_cast<size_t>(B) * Hq * num_splits);
+    }
+    int dev;
+    st = current_ready_device(&dev);
+    if (st != AC_OK) return st;
+    CUtensorMap k_map, v_map;
+    const int box = q8_attn_box(page_size);
+    st = make_q8_map(&k_map, view.k_codes, s, view, box);
+    if (st == AC_OK) st = make_q8_map(&v_map, view.v_codes, s, view, box);
+    if (st != AC_OK) return st;
+    const float scale = softmax_scale > 0.0f ? softmax_scale : 1.0f / sqrtf(static_cast<float>(d));
+    const int limit = ac_window_span(window, sinks);
+    const int split_tokens = split_tokens_for(limit < max_context_len ? limit : max_context_len, num_splits);
+    cudaError_t e = launch_paged_decode_attn_q8(k_map, v_map, q_rot, view, block_table, max_pages_per_seq, context_lens,
+                                                new_tokens, scale, num_splits, split_tokens, partial_o, partial_lse,
+                                                arrivals, out, B, Hq, Hkv, d, page_size, num_pages, window, sinks,
+                                                row_order, status_flag, static_cast<cudaStream_t>(stream));
+    return e == cudaSuccess ? AC_OK : fail_cuda(static_cast<int>(e));
+}
+
+// ---- rotary positions -----------------------------------------------------------------------------
+
+int ac_rope_tables(float* rope_cos, float* rope_sin, int64_t first_position, int positions, int rotary_dim,
+                   const ac_rope_scaling* scaling, void* stream) {
+    if (!rope_cos || !rope_sin || !scaling) return AC_ERR_NULL;
+    if (positions < 0 || first_position < 0 || rotary_dim <= 0 || rotary_dim % 2 != 0) return AC_ERR_SHAPE;
+    if (scaling->kind < AC_ROPE_NONE || scaling->kind > AC_ROPE_RAMP) return AC_ERR_UNSUPPORTED;
+    auto positive = [](double x) { return x > 0.0 && x <= 1e300; };        // false for NaN
+    if (!positive(scaling->base)) return AC_ERR_SHAPE;
+    if (scaling->kind != AC_ROPE_NONE && !positive(scaling->factor)) return AC_ERR_SHAPE;
+    if (scaling->kind == AC_ROPE_BASE && rotary_dim < 4) return AC_ERR_SHAPE;
+    if (scaling->kind == AC_ROPE_RAMP && (!positive(scaling->original) || !(scaling->low < scaling->high))) return AC_ERR_SHAPE;
+    if (!(scaling->magnitude >= 0.0)) return AC_ERR_SHAPE;
+    if (!aligned16(rope_cos) || !aligned16(rope_sin)) return AC_ERR_ALIGN;
+    int dev;
+    int st = current_ready_device(&dev);
+    if (st != AC_OK) return st;
+    if (positions == 0) return AC_OK;
+    RopeScaling sc;
+    sc.kind = scaling->kind;
+    sc.base = scaling->base;
+    if (sc.kind == AC_ROPE_BASE) sc.base *= pow(scaling->factor, rotary_dim / (rotary_dim - 2.0));
+    sc.factor = scaling->factor;
+    sc.original = scaling->original;
+    sc.low = scaling->low;
+    sc.high = scaling->high;
+    sc.magnitude = scaling->magnitude == 0.0 ? 1.0 : scaling->magnitude;
+    cudaError_t e = launch_rope_tables(rope_cos, rope_sin, first_position, positions, rotary_dim, sc,
+                                       g_devices[dev].sm_count, static_cast<cudaStream_t>(stream));
+    return e == cudaSuccess ? AC_OK : fail_cuda(static_cast<int>(e));
+}
+
+int ac_rope_rows(const void* q_in, void* q_out, int64_t stride_q_in_token, int64_t stride_q_out_token,
+                 const void* k_in, void* k_out, int64_t stride_k_in_token, int64_t stride_k_out_token,
+                 const int32_t* start_pos, const int32_t* row_offsets, int total_tokens, int B, int Hq, int Hkv, int d,
+                 const float* rope_cos, const float* rope_sin, int max_position, int32_t* status_flag, void* stream,
+                 const ac_rope_options* options) {
+    if (!q_in || !q_out || (Hkv > 0 && (!k_in || !k_out)) || !start_pos || !row_offsets || !rope_cos || !rope_sin)
+        return AC_ERR_NULL;
+    if (total_tokens < 0 || B <= 0 || Hq <= 0 || Hkv < 0 || d <= 0 || max_position <= 0) return AC_ERR_SHAPE;
+    if ((d != 64 && d != 128) || static_cast<long long>(Hq) + Hkv > 65535 || B > 65535) return AC_ERR_UNSUPPORTED;
+    if (stride_q_in_token < static_cast<int64_t>(Hq) * d || stride_q_out_token < static_cast<int64_t>(Hq) * d) return AC_ERR_SHAPE;
+    if (stride_q_in_token % 8 || stride_q_out_token % 8) return AC_ERR_ALIGN;
+    if (Hkv > 0) {
+        if (stride_k_in_token < static_cast<int64_t>(Hkv) * d || stride_k_out_token < static_cast<int64_t>(Hkv) * d) return AC_ERR_SHAPE;
+        if (stride_k_in_token % 8 || stride_k_out_token % 8) return AC_ERR_ALIGN;
+        if (!aligned16(k_in) || !aligned16(k_out)) return AC_ERR_ALIGN;
+        if (k_in == k_out && stride_k_in_token != stride_k_out_token) return AC_ERR_SHAPE;
+    }
+    if (!aligned16(q_in) || !aligned16(q_out) || !aligned16(rope_cos) || !aligned16(rope_sin)) return AC_ERR_ALIGN;
+    if (q_in == q_out && stride_q_in_token != stride_q_out_token) return AC_ERR_SHAPE;
+    RopeVariant variant;
+    const RopeVariant* vp = nullptr;
+    int st = parse_rope_options(options, d, &variant, &vp);
+    if (st != AC_OK) return st;
+    int dev;
+    st = current_ready_device(&dev);
+    if (st != AC_OK) return st;
+    if (total_tokens == 0) return AC_OK;
+    cudaError_t e = launch_rope_rows(q_in, q_out, stride_q_in_token, stride_q_out_token, k_in, k_out, stride_k_in_token,
+                                     stride_k_out_token, start_pos, row_offsets, total_tokens, B, Hq, Hkv, d, rope_cos,
+                                     rope_sin, max_position, status_flag, vp, g_devices[dev].sm_count,
+                                     static_cast<cudaStream_t>(stream));
+    return e == cudaSuccess ? AC_OK : fail_cuda(static_cast<int>(e));
+}
+
 // ---- pages ----------------------------------------------------------------------------------------
 
 static int check_pools(const ac_page_pool* pools, int n_pools, int page_size) {
@@ -1107,7 +1362,7 @@ static int check_pools(const ac_page_pool* pools, int n_pools, int page_size) {
         if (pools[i].base == nullptr) return AC_ERR_NULL;
         if (pools[i].page_bytes <= 0 || pools[i].segments <= 0) return AC_ERR_SHAPE;
         if (!aligned16(pools[i].base) || pools[i].page_bytes % (16ll * pools[i].segments) != 0) return AC_ERR_ALIGN;
-        if (page_size > 0 && pools[i].page_bytes / pools[i].segments % page_size != 0) return AC_ERR_SHAPE;
+        if (page_size > 0 && pools[i].whole == 0 && pools[i].page_bytes / pools[i].segments % page_size != 0) return AC_ERR_SHAPE;
     }
     return AC_OK;
 }

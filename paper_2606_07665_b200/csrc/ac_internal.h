@@ -70,6 +70,23 @@ struct Q4View {
     int group;
 };
 
+// The 8-bit cache as the kernels see it (validated by the ABI layer).
+struct Q8View {
+    uint8_t* k_codes;
+    uint8_t* v_codes;
+    float* scales;                                    // [page] [head][block][K, V], pages stride_scales floats apart
+    int64_t stride_page, stride_token, stride_head;   // bytes
+    int64_t stride_scales;                            // floats
+    int block;                                        // tokens of a block
+    int format;                                       // AC_Q8_INT8 or AC_Q8_E4M3
+};
+
+// Frequencies of the rotary tables (validated by the ABI layer; AC_ROPE_BASE is already in base).
+struct RopeScaling {
+    int kind;
+    double base, factor, original, low, high, magnitude;
+};
+
 // Per-kernel launchers; each validates nothing (the ABI layer did) and returns a cudaError_t.
 cudaError_t attn_set_attributes(int smem_optin);
 cudaError_t launch_rope_kv_append(const void* q_in, void* q_out, const void* k_new, const void* v_new,
@@ -134,6 +151,31 @@ cudaError_t launch_paged_decode_attn_q4(const void* q_rot, const Q4View& cache, 
                                         float* partial_lse, int32_t* arrivals, void* out, int B, int Hq, int Hkv,
                                         int d, int page_size, int num_pages, int window, int sinks,
                                         const int32_t* row_order, cudaStream_t stream);
+cudaError_t launch_rope_kv_append_q8(const void* q_in, void* q_out, const void* k_new, const void* v_new,
+                                     const Q8View& cache, const int32_t* block_table, int max_pages_per_seq,
+                                     const int32_t* context_lens, const float* rope_cos, const float* rope_sin,
+                                     int max_position, int B, int Hq, int Hkv, int d, int page_size, int num_pages,
+                                     int32_t* status_flag, const RopeVariant* variant, cudaStream_t stream);
+cudaError_t launch_kv_bulk_q8(void* k, void* v, const Q8View& cache, const int32_t* block_table,
+                              int max_pages_per_seq, const int32_t* start_pos, const int32_t* row_offsets,
+                              int total_tokens, int B, int Hkv, int d, int page_size, int num_pages,
+                              int32_t* status_flag, bool store, int sms, cudaStream_t stream);
+cudaError_t q8_attn_set_attributes(int smem_optin);
+int q8_attn_box(int page_size);         // tokens of the boxes that the attention kernel's tensor maps must have
+cudaError_t launch_paged_decode_attn_q8(const CUtensorMap& k_map, const CUtensorMap& v_map, const void* q_rot,
+                                        const Q8View& cache, const int32_t* block_table, int max_pages_per_seq,
+                                        const int32_t* context_lens, int new_tokens, float scale, int num_splits,
+                                        int split_tokens, float* partial_o, float* partial_lse, int32_t* arrivals,
+                                        void* out, int B, int Hq, int Hkv, int d, int page_size, int num_pages,
+                                        int window, int sinks, const int32_t* row_order, int32_t* status_flag,
+                                        cudaStream_t stream);
+cudaError_t launch_rope_rows(const void* q_in, void* q_out, int64_t q_in_token, int64_t q_out_token, const void* k_in,
+                             void* k_out, int64_t k_in_token, int64_t k_out_token, const int32_t* start_pos,
+                             const int32_t* row_offsets, int total_tokens, int B, int Hq, int Hkv, int d,
+                             const float* rope_cos, const float* rope_sin, int max_position, int32_t* status_flag,
+                             const RopeVariant* variant, int sms, cudaStream_t stream);
+cudaError_t launch_rope_tables(float* rope_cos, float* rope_sin, long long first_position, int positions,
+                               int rotary_dim, const RopeScaling& scaling, int sms, cudaStream_t stream);
 cudaError_t launch_copy_pages(const ac_page_pool* pools, int n_pools, const int32_t* pairs, int n, int num_pages,
                               int32_t* status_flag, int sms, cudaStream_t stream);
 cudaError_t launch_reserve(int32_t* block_table, int max_pages_per_seq, const int32_t* context_lens, int32_t* refs,

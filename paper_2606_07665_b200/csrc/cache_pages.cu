@@ -172,7 +172,8 @@ __device__ __forceinline__ void copy_piece(char* dst, const char* src, int64_t l
 __device__ __forceinline__ void run_copies(const ac_page_pool& pool, const int2* jobs, const int32_t* lens, int n,
                                            int page_size, int num_pages, int32_t* status_flag) {
     const int lane = threadIdx.x & 31;
-    const int segments = lens != nullptr ? pool.segments : 1;
+    const bool slots = lens != nullptr && pool.whole == 0;
+    const int segments = slots ? pool.segments : 1;
     const int64_t seg_bytes = pool.page_bytes / segments;
     const int pieces = static_cast<int>((seg_bytes + kPiece - 1) / kPiece);
     const long long per_job = static_cast<long long>(segments) * pieces;
@@ -189,7 +190,7 @@ __device__ __forceinline__ void run_copies(const ac_page_pool& pool, const int2*
             continue;
         }
         if (j.x == j.y) continue;
-        const int64_t end = lens != nullptr ? seg_bytes / page_size * (lens[job] % page_size) : seg_bytes;
+        const int64_t end = slots ? seg_bytes / page_size * (lens[job] % page_size) : seg_bytes;
         const int64_t lo = static_cast<int64_t>(piece) * kPiece;
         const int64_t hi = min(end, lo + kPiece);
         if (lo >= hi) continue;

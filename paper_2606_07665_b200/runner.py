@@ -4,7 +4,8 @@ Only plumbing: torch tensors for device memory, the split plan from the library,
 C-ABI calls in order.  Every arithmetic step runs inside libac's kernels.
 
 ``DecodeStep`` stages a synthetic workload; ``PagedAttention`` (bf16 cache), ``Q4Cache`` with ``Q4DecodeStep``
-(4-bit cache) and ``CachePages`` (reserve, fork, release, trim, compact, copy) work on tensors that the caller owns.
+(4-bit cache), ``Q8Cache`` with ``Q8DecodeStep`` (8-bit cache), ``Rope`` (rotary tables, prompts rotated) and ``CachePages``
+(reserve, fork, release, trim, compact, copy) work on tensors that the caller owns.
 """
 from __future__ import annotations
 
@@ -484,54 +485,25 @@ class PagedAttention(_Rows):
         return out
 
 
-class Q4Cache(_OnDevice):
-    """A 4-bit paged cache over the caller's tensors (``empty`` allocates them).
-
-    ``k_codes``, ``v_codes``: uint8 [num_pages, page_size, Hkv, d/2] ("token_major") or [num_pages, Hkv, page_size,
-    d/2] ("head_major"); ``params``: bf16 [num_pages, Hkv, page_size, 2, d/group, 2] (K and V; scale, minimum)."""
-
-    def __init__(self, k_codes, v_codes, params, page_size=None, layout="token_major"):
-        self._bind(k_codes.device)
-        if k_codes.dim() != 4 or params.dim() != 6:
-            raise ValueError("codes have 4 dimensions, params 6")
-        token, head = _axes(layout)
-        self.num_pages, self.page_size, self.Hkv = k_codes.shape[0], k_codes.shape[token], k_codes.shape[head]
-        self.d, self.layout = 2 * k_codes.shape[3], layout
-        if page_size is not None and page_size != self.page_size:
-            raise ValueError(f"codes have pages of {self.page_size} tokens, not {page_size}")
-        groups = params.shape[4]
-        if groups <= 0 or self.d % groups:
-            raise ValueError(f"{groups} groups over {self.d} elements")
-        self.group = self.d // groups
-        _want(k_codes, "k_codes", k_codes.shape, (torch.uint8,), self.device)
-        _want(v_codes, "v_codes", k_codes.shape, (torch.uint8,), self.device)
-        _want(params, "params", (self.num_pages, self.Hkv, self.page_size, 2, groups, 2), _BF16, self.device)
-        self.k_codes, self.v_codes, self.params = k_codes, v_codes, params
-        self.struct = ac.q4_cache(k_codes, v_codes, params, k_codes.stride(0), k_codes.stride(token),
-                                  k_codes.stride(head), self.group)
-
-    @classmethod
-    def empty(cls, num_pages, page_size, Hkv, d, group=64, layout="token_major", device="cuda:0"):
-        _axes(layout)
-        if group not in (32, 64, 128) or group > d:
-            raise ValueError(f"group {group}: expected 32, 64 or 128, and at most {d}")
-        shape = (num_pages, page_size, Hkv, d // 2) if layout == "token_major" else (num_pages, Hkv, page_size, d // 2)
-        k, v = (torch.zeros(shape, dtype=torch.uint8, device=device) for _ in range(2))
-        params = torch.zeros((num_pages, Hkv, page_size, 2, d // group, 2), dtype=torch.bfloat16, device=device)
-        cache = cls(k, v, params, layout=layout)
-        cache._allocated = (k, v, params)
-        return cache
+class _QuantisedCache(_OnDevice):
+    """Bulk writes and reads of a quantised cache, whatever its format (``_format`` ends the names of its calls)."""
 
     _allocated = ()
 
     def _buffers(self):
         return [self.status_flag, *self._allocated]
 
-    @property
-    def pools(self):
-        """(tensor, segments of a page) of the three pools, for CachePages."""
-        codes = 1 if self.layout == "token_major" else self.Hkv
-        return [(self.k_codes, codes), (self.v_codes, codes), (self.params, self.Hkv)]
+    def _codes(self, k_codes, v_codes, page_size, layout, dtypes):
+        """Checks the code pools and takes over what they say; returns the strides of page, token and head."""
+        token, head = _axes(layout)
+        self.num_pages, self.page_size, self.Hkv = k_codes.shape[0], k_codes.shape[token], k_codes.shape[head]
+        self.layout = layout
+        if page_size is not None and page_size != self.page_size:
+            raise ValueError(f"codes have pages of {self.page_size} tokens, not {page_size}")
+        _want(k_codes, "k_codes", k_codes.shape, dtypes, self.device)
+        _want(v_codes, "v_codes", k_codes.shape, (k_codes.dtype,), self.device)
+        self.k_codes, self.v_codes = k_codes, v_codes
+        return k_codes.stride(0), k_codes.stride(token), k_codes.stride(head)
 
     def _bulk(self, name, k, v, block_table, start_pos, row_offsets, stream):
         B = start_pos.shape[0]
@@ -550,7 +522,7 @@ class Q4Cache(_OnDevice):
     def store(self, k, v, block_table, start_pos, row_offsets, stream=None):
         """Quantises k, v (bf16 [tokens, Hkv, d], keys rotated): row b's tokens row_offsets[b] .. row_offsets[b+1] - 1
         go to positions start_pos[b], start_pos[b] + 1, ..."""
-        self._bulk("ac_kv_store_q4", k, v, block_table, start_pos, row_offsets, stream)
+        self._bulk("ac_kv_store_" + self._format, k, v, block_table, start_pos, row_offsets, stream)
 
     def load(self, block_table, start_pos, row_offsets, total_tokens=None, k_out=None, v_out=None, stream=None):
         """The same tokens as bf16 [tokens, Hkv, d]; outputs are allocated unless given."""
@@ -560,12 +532,109 @@ class Q4Cache(_OnDevice):
             shape = (total_tokens, self.Hkv, self.d)
             k_out = self._new(shape, stream) if k_out is None else k_out
             v_out = self._new(shape, stream) if v_out is None else v_out
-        self._bulk("ac_kv_load_q4", k_out, v_out, block_table, start_pos, row_offsets, stream)
+        self._bulk("ac_kv_load_" + self._format, k_out, v_out, block_table, start_pos, row_offsets, stream)
         return k_out, v_out
 
 
-class Q4DecodeStep(_Rows):
-    """One decode step over a 4-bit cache: RoPE + quantised append, then attention (two launches).
+class Q4Cache(_QuantisedCache):
+    """A 4-bit paged cache over the caller's tensors (``empty`` allocates them).
+
+    ``k_codes``, ``v_codes``: uint8 [num_pages, page_size, Hkv, d/2] ("token_major") or [num_pages, Hkv, page_size,
+    d/2] ("head_major"); ``params``: bf16 [num_pages, Hkv, page_size, 2, d/group, 2] (K and V; scale, minimum)."""
+
+    _format = "q4"
+
+    def __init__(self, k_codes, v_codes, params, page_size=None, layout="token_major"):
+        self._bind(k_codes.device)
+        if k_codes.dim() != 4 or params.dim() != 6:
+            raise ValueError("codes have 4 dimensions, params 6")
+        strides = self._codes(k_codes, v_codes, page_size, layout, (torch.uint8,))
+        self.d = 2 * k_codes.shape[3]
+        groups = params.shape[4]
+        if groups <= 0 or self.d % groups:
+            raise ValueError(f"{groups} groups over {self.d} elements")
+        self.group = self.d // groups
+        _want(params, "params", (self.num_pages, self.Hkv, self.page_size, 2, groups, 2), _BF16, self.device)
+        self.params = params
+        self.struct = ac.q4_cache(k_codes, v_codes, params, *strides, self.group)
+
+    @classmethod
+    def empty(cls, num_pages, page_size, Hkv, d, group=64, layout="token_major", device="cuda:0"):
+        _axes(layout)
+        if group not in (32, 64, 128) or group > d:
+            raise ValueError(f"group {group}: expected 32, 64 or 128, and at most {d}")
+        shape = (num_pages, page_size, Hkv, d // 2) if layout == "token_major" else (num_pages, Hkv, page_size, d // 2)
+        k, v = (torch.zeros(shape, dtype=torch.uint8, device=device) for _ in range(2))
+        params = torch.zeros((num_pages, Hkv, page_size, 2, d // group, 2), dtype=torch.bfloat16, device=device)
+        cache = cls(k, v, params, layout=layout)
+        cache._allocated = (k, v, params)
+        return cache
+
+    @property
+    def pools(self):
+        """(tensor, segments of a page) of the three pools, for CachePages."""
+        codes = 1 if self.layout == "token_major" else self.Hkv
+        return [(self.k_codes, codes), (self.v_codes, codes), (self.params, self.Hkv)]
+
+
+class Q8Cache(_QuantisedCache):
+    """An 8-bit paged cache over the caller's tensors (``empty`` allocates them).
+
+    ``k_codes``, ``v_codes``: int8 or float8_e4m3fn [num_pages, page_size, Hkv, d] ("token_major") or [num_pages, Hkv,
+    page_size, d] ("head_major"); ``scales``: fp32 [num_pages, Hkv, page_size/block, 2] (K and V), powers of two, one for every
+    ``block`` consecutive slots.  Pages of the scales may lie further apart than they are long; for ``pools`` they have
+    to be a multiple of 16 bytes apart, as ``empty`` makes them."""
+
+    _format = "q8"
+
+    def __init__(self, k_codes, v_codes, scales, page_size=None, layout="token_major"):
+        self._bind(k_codes.device)
+        if k_codes.dim() != 4 or scales.dim() != 4:
+            raise ValueError("codes and scales have 4 dimensions")
+        strides = self._codes(k_codes, v_codes, page_size, layout, (torch.int8, torch.float8_e4m3fn))
+        self.d, blocks = k_codes.shape[3], scales.shape[2]
+        if blocks <= 0 or self.page_size % blocks:
+            raise ValueError(f"{blocks} blocks in pages of {self.page_size} tokens")
+        self.block = self.page_size // blocks
+        page = self.Hkv * blocks * 2
+        apart = scales.stride(0) if self.num_pages > 1 else max(scales.stride(0), page)
+        _want(scales[0], "scales", (self.Hkv, blocks, 2), (torch.float32,), self.device)
+        if scales.shape[0] != self.num_pages:
+            raise ValueError(f"scales of {scales.shape[0]} pages, codes of {self.num_pages}")
+        if apart < page:
+            raise ValueError("scales: pages overlap")
+        self.scales, self._apart = scales, apart
+        fmt = ac.AC_Q8_INT8 if k_codes.dtype == torch.int8 else ac.AC_Q8_E4M3
+        self.struct = ac.q8_cache(k_codes, v_codes, scales, *strides, apart, self.block, fmt)
+
+    @classmethod
+    def empty(cls, num_pages, page_size, Hkv, d, block=16, dtype=torch.float8_e4m3fn, layout="token_major", device="cuda:0"):
+        _axes(layout)
+        if block <= 0 or block % 16 or page_size % block:
+            raise ValueError(f"block {block}: expected a multiple of 16 that divides {page_size}")
+        if dtype not in (torch.int8, torch.float8_e4m3fn):
+            raise ValueError(f"type {dtype}, expected {torch.int8} or {torch.float8_e4m3fn}")
+        shape = (num_pages, page_size, Hkv, d) if layout == "token_major" else (num_pages, Hkv, page_size, d)
+        k, v = (torch.zeros(shape, dtype=torch.uint8, device=device).view(dtype) for _ in range(2))
+        blocks = page_size // block
+        width = Hkv * blocks * 2
+        held = torch.zeros((num_pages, -(-width // 4) * 4), dtype=torch.float32, device=device)
+        cache = cls(k, v, held[:, :width].view(num_pages, Hkv, blocks, 2), layout=layout)
+        cache._allocated = (k, v, held)
+        return cache
+
+    @property
+    def pools(self):
+        """(tensor, segments of a page, whether a fork copies the whole page) of the three pools, for CachePages."""
+        if self._apart % 4:
+            raise ValueError("scales: pages have to be a multiple of 16 bytes apart (empty makes them so)")
+        codes = 1 if self.layout == "token_major" else self.Hkv
+        held = self.scales.as_strided((self.num_pages, self._apart), (self._apart, 1))
+        return [(self.k_codes, codes), (self.v_codes, codes), (held, 1, True)]
+
+
+class _QuantisedStep(_Rows):
+    """One decode step over a quantised cache: RoPE + quantised append, then attention (two launches).
 
     ``rope_variants``: rotary_dim, interleaved, q_norm_weight, k_norm_weight, norm_eps as in
     ``ac_rope_kv_append_ex``; the rope tables are only needed for ``append`` and ``step``.  The object owns its
@@ -574,6 +643,8 @@ class Q4DecodeStep(_Rows):
     def __init__(self, cache, block_table, context_lens, Hq, lens_host=None, window=0, sinks=0, rope_cos=None,
                  rope_sin=None, max_context_len=None, num_splits=None, row_order="auto", rope_variants=None,
                  softmax_scale=0.0, new_tokens=1):
+        if not isinstance(cache, self._cache_type):
+            raise TypeError(f"cache: {type(cache).__name__}, expected a {self._cache_type.__name__}")
         self._bind(cache.device)
         self.cache, self.window, self.sinks = cache, int(window), int(sinks)
         self.softmax_scale, self.new_tokens = float(softmax_scale), _new_tokens(new_tokens)
@@ -598,7 +669,8 @@ class Q4DecodeStep(_Rows):
         return super()._buffers() + self.cache._buffers()
 
     def _choose(self, counts, span):
-        return ac.ac_decode_plan_q4(counts, self.B, self.Hq, self.Hkv, self.d, self.page_size, span)[0]
+        plan = getattr(ac, "ac_decode_plan_" + self.cache._format)
+        return plan(counts, self.B, self.Hq, self.Hkv, self.d, self.page_size, span)[0]
 
     def _marshal(self):
         shape = [self.B, self.Hq, self.Hkv, self.d, self.page_size, self.num_pages]
@@ -624,7 +696,7 @@ class Q4DecodeStep(_Rows):
             _want(q_out, "q_out", self._q_shape, _BF16, self.device)
         args = self._append_args.copy()
         args[:4] = q_in.data_ptr(), q_out.data_ptr(), k_new.data_ptr(), v_new.data_ptr()
-        self._enqueue("ac_rope_kv_append_q4", args, stream, -2)
+        self._enqueue("ac_rope_kv_append_" + self.cache._format, args, stream, -2)
         return q_out
 
     def attention(self, q, out=None, stream=None):
@@ -636,7 +708,7 @@ class Q4DecodeStep(_Rows):
             _want(out, "out", self._q_shape, _BF16, self.device)
         args = self._attn_args.copy()
         args[0], args[10] = q.data_ptr(), out.data_ptr()
-        self._enqueue("ac_paged_decode_attn_q4", args, stream, -2)
+        self._enqueue("ac_paged_decode_attn_" + self.cache._format, args, stream, -2)
         return out
 
     def step(self, q_in, k_new, v_new, q_rot=None, out=None, stream=None):
@@ -646,11 +718,117 @@ class Q4DecodeStep(_Rows):
         return self.attention(self.append(q_in, k_new, v_new, q_rot, stream), out, stream)
 
 
+class Q4DecodeStep(_QuantisedStep):
+    """One decode step over a 4-bit cache: RoPE + quantised append, then attention (two launches).  See _QuantisedStep."""
+
+    _cache_type = Q4Cache
+
+
+class Q8DecodeStep(_QuantisedStep):
+    """One decode step over an 8-bit cache: RoPE + quantised append, then attention (two launches).  See _QuantisedStep."""
+
+    _cache_type = Q8Cache
+
+
+class Rope(_OnDevice):
+    """Rotary positions: tables over the caller's tensors (``scaled`` allocates them), and prompts rotated by them.
+
+    ``cos``, ``sin``: fp32 [max_position, rotary_dim/2], as the decode steps take them.  interleaved, q_norm_weight,
+    k_norm_weight and norm_eps as in ``ac_rope_kv_append_ex``."""
+
+    _allocated = ()
+    _KINDS = {"none": ac.AC_ROPE_NONE, "linear": ac.AC_ROPE_LINEAR, "base": ac.AC_ROPE_BASE, "ramp": ac.AC_ROPE_RAMP}
+
+    def __init__(self, cos, sin, rotary_dim=0, interleaved=False, q_norm_weight=None, k_norm_weight=None, norm_eps=0.0):
+        self._bind(cos.device)
+        if cos.dim() != 2 or cos.shape[0] < 1 or cos.shape[1] < 1:
+            raise ValueError(f"cos: shape {tuple(cos.shape)}, expected [max_position, rotary_dim/2]")
+        for t, what in ((cos, "cos"), (sin, "sin")):
+            _want(t, what, cos.shape, (torch.float32,), self.device)
+        if rotary_dim and rotary_dim != 2 * cos.shape[1]:
+            raise ValueError(f"tables of {cos.shape[1]} frequencies, rotary_dim {rotary_dim}")
+        self.cos, self.sin, self.max_position, self.rotary_dim = cos, sin, cos.shape[0], 2 * cos.shape[1]
+        self._norms = (q_norm_weight, k_norm_weight)       # kept alive
+        for t, what in zip(self._norms, ("q_norm_weight", "k_norm_weight")):
+            if t is not None:
+                _want(t, what, (t.shape[-1],), _BF16, self.device)
+        self._options = ac._rope_options(self.rotary_dim, interleaved, q_norm_weight, k_norm_weight, norm_eps)
+
+    @classmethod
+    def scaled(cls, max_position, rotary_dim, base=10000.0, scaling="none", factor=1.0, original=0.0, low=0.0, high=0.0,
+               magnitude=1.0, device="cuda:0", **variants):
+        """Tables of max_position positions, filled as ``fill`` says; ``variants``: interleaved and the norms."""
+        if max_position < 1 or rotary_dim < 2 or rotary_dim % 2:
+            raise ValueError(f"{max_position} positions of rotary_dim {rotary_dim}")
+        cos, sin = (torch.empty((max_position, rotary_dim // 2), dtype=torch.float32, device=device) for _ in range(2))
+        rope = cls(cos, sin, **variants)
+        rope._allocated = (cos, sin)
+        rope.fill(0, base, scaling, factor, original, low, high, magnitude)
+        return rope
+
+    def _buffers(self):
+        return [self.status_flag, *self._allocated]
+
+    def fill(self, first_position=0, base=10000.0, scaling="none", factor=1.0, original=0.0, low=0.0, high=0.0,
+             magnitude=1.0, stream=None):
+        """Row j of the tables becomes magnitude times cosine and sine of position first_position + j.  ``scaling``: "none",
+        "linear" (angles / factor), "base" (a larger base: the lowest frequency / factor) or "ramp" (frequencies that
+        turn less than ``low`` times in ``original`` positions / factor, more than ``high`` times as they are, blended between)."""
+        if scaling not in self._KINDS:
+            raise ValueError(f"scaling {scaling!r}, expected one of {', '.join(self._KINDS)}")
+        how = ac.rope_scaling(float(base), self._KINDS[scaling], float(factor), float(original), float(low), float(high),
+                              float(magnitude))
+        self._enqueue("ac_rope_tables", [self.cos.data_ptr(), self.sin.data_ptr(), int(first_position), self.max_position,
+                                         self.rotary_dim, how, None], stream, -1)
+
+    def _tokens(self, t, name, total, d):
+        """t is [total, heads, d] bf16 with dense heads; returns the elements from one token to the next."""
+        if t.dim() != 3 or t.shape[0] != total or t.shape[2] != d or t.dtype not in _BF16 or t.device != self.device:
+            raise ValueError(f"{name}: {t.dtype} {tuple(t.shape)} on {t.device}, expected bf16 [{total}, heads, {d}] on {self.device}")
+        heads = t.shape[1]
+        if t.stride(2) != 1 or (heads > 1 and t.stride(1) != d):
+            raise ValueError(f"{name}: heads of a token are not contiguous")
+        return t.stride(0) if total > 1 else max(heads * d, 8)
+
+    def rows(self, q, k, start_pos, row_offsets, q_out=None, k_out=None, stream=None):
+        """Rotates q [tokens, Hq, d] and k [tokens, Hkv, d] (bf16, d 64 or 128; k may be None): row b's tokens row_offsets[b] ..
+        row_offsets[b+1] - 1 stand at positions start_pos[b], start_pos[b] + 1, ...  The heads of a token are contiguous, tokens
+        may be any multiple of 8 elements apart (parts of a joint projection).  Outputs are allocated unless given and may be the
+        inputs; tokens of no row stay as they are.  Returns q_out, k_out."""
+        if not isinstance(q, torch.Tensor) or q.dim() != 3:
+            raise ValueError("q: expected a tensor [tokens, heads, d]")
+        total, Hq, d = q.shape
+        B = start_pos.shape[0]
+        _want(start_pos, "start_pos", (B,), (torch.int32,), self.device)
+        _want(row_offsets, "row_offsets", (B + 1,), (torch.int32,), self.device)
+        for t, what in zip(self._norms, ("q_norm_weight", "k_norm_weight")):
+            if t is not None and t.shape[-1] != d:
+                raise ValueError(f"{what}: {t.shape[-1]} weights for heads of {d}")
+        q_out = self._new(q.shape, stream, q.dtype) if q_out is None else q_out
+        strides = [self._tokens(q, "q", total, d), self._tokens(q_out, "q_out", total, d)]
+        if q_out.shape != q.shape:
+            raise ValueError(f"q_out: shape {tuple(q_out.shape)}, expected {tuple(q.shape)}")
+        Hkv, k_ptrs, k_strides = 0, [None, None], [0, 0]
+        if k is not None:
+            k_out = self._new(k.shape, stream, k.dtype) if k_out is None else k_out
+            k_strides = [self._tokens(k, "k", total, d), self._tokens(k_out, "k_out", total, d)]
+            if k_out.shape != k.shape:
+                raise ValueError(f"k_out: shape {tuple(k_out.shape)}, expected {tuple(k.shape)}")
+            Hkv, k_ptrs = k.shape[1], [k.data_ptr(), k_out.data_ptr()]
+        if total == 0:
+            return q_out, k_out
+        self._enqueue("ac_rope_rows", [q.data_ptr(), q_out.data_ptr(), *strides, *k_ptrs, *k_strides, start_pos.data_ptr(),
+                                       row_offsets.data_ptr(), total, B, Hq, Hkv, d, self.cos.data_ptr(), self.sin.data_ptr(),
+                                       self.max_position, self._flag, None, self._options], stream, -2)
+        return q_out, k_out
+
+
 class CachePages(_OnDevice):
     """Pages of any number of pools under one block table: reserve, fork, release, trim, compact, copy.
 
     ``pools``: contiguous tensors [num_pages, ...], each alone or with the number of segments of its page ([page,
-    slot, ...]: 1; [page, head, slot, ...]: the heads).  ``block_table`` int32 [rows, max_pages_per_seq],
+    slot, ...]: 1; [page, head, slot, ...]: the heads) and, where its bytes do not follow the slots, True: a fork then copies
+    the whole of a partly filled page (``Q8Cache.pools``).  ``block_table`` int32 [rows, max_pages_per_seq],
     ``context_lens`` int32 [rows] (< 0: unused), ``ref_counts`` int32 [num_pages] (0: free); all are updated in place.
     ``status_flag`` collects what went wrong on the device (AC_FLAG_...).  The object owns its workspace: its calls must
     not overlap on the GPU."""
@@ -665,11 +843,11 @@ class CachePages(_OnDevice):
         self.block_table, self.context_lens, self.ref_counts = block_table, context_lens, ref_counts
         self.pools = [p if isinstance(p, tuple) else (p, 1) for p in pools]
         described = []
-        for t, segments in self.pools:
+        for t, segments, *whole in self.pools:
             if t.shape[0] != self.num_pages:
                 raise ValueError(f"a pool of {t.shape[0]} pages, ref_counts of {self.num_pages}")
             _want(t, "pool", t.shape, (t.dtype,), self.device)
-            described.append((t, t.numel() // self.num_pages * t.element_size(), segments))
+            described.append((t, t.numel() // self.num_pages * t.element_size(), segments, *(int(bool(w)) for w in whole)))
         self._pools = ac.page_pools(described)
         self.workspace = torch.empty(ac.ac_cache_workspace_bytes(self.rows, self.num_pages, self.rows),
                                      dtype=torch.uint8, device=self.device)
