@@ -145,6 +145,7 @@ int ac_init(int device) {
         if (e == cudaSuccess) e = proj_tc_set_attributes(st.smem_optin);
         if (e == cudaSuccess) e = q4_attn_set_attributes(st.smem_optin);
         if (e == cudaSuccess) e = q8_attn_set_attributes(st.smem_optin);
+        if (e == cudaSuccess) e = rope_rows_set_attributes(st.smem_optin);
         if (e != cudaSuccess) {
             status = fail_cuda(static_cast<int>(e));
             break;

@@ -169,6 +169,7 @@ cudaError_t launch_paged_decode_attn_q8(const CUtensorMap& k_map, const CUtensor
                                         void* out, int B, int Hq, int Hkv, int d, int page_size, int num_pages,
                                         int window, int sinks, const int32_t* row_order, int32_t* status_flag,
                                         cudaStream_t stream);
+cudaError_t rope_rows_set_attributes(int smem_optin);
 cudaError_t launch_rope_rows(const void* q_in, void* q_out, int64_t q_in_token, int64_t q_out_token, const void* k_in,
                              void* k_out, int64_t k_in_token, int64_t k_out_token, const int32_t* start_pos,
                              const int32_t* row_offsets, int total_tokens, int B, int Hq, int Hkv, int d,

@@ -24,13 +24,44 @@ struct RowsParams {
     const uint16_t* k_norm_w;
     float norm_eps;
     int max_position, total_tokens, B, Hq, Hkv, rotary_dim, interleaved;
-    int chunk, chunks;                                             // heads of one warp, and how many such pieces a token has
+    int chunk, q_chunks, chunks;                                   // heads of a piece of a token; pieces of its q, of q and k
     int32_t* status_flag;
 };
 
-// Position of a token, or -1 where it has none; the whole warp calls this.  The row is the last one whose offset is <= token:
-// each round the 32 lanes look at the ends of 32 equal pieces of what is left.
-__device__ __forceinline__ int token_position(const RowsParams& p, int token, int lane) {
+// A piece: `chunk` heads of q or of k of one token.
+struct Piece {
+    const uint16_t* src;
+    uint16_t* dst;
+    const uint16_t* norm_w;
+    int heads;
+};
+template <int D>
+__device__ __forceinline__ Piece find_piece(const RowsParams& p, int token, int piece) {
+    const bool is_q = piece < p.q_chunks;
+    const int from = (is_q ? piece : piece - p.q_chunks) * p.chunk;
+    Piece r;
+    r.src = (is_q ? p.q_in + token * p.q_in_token : p.k_in + token * p.k_in_token) + from * D;
+    r.dst = (is_q ? p.q_out + token * p.q_out_token : p.k_out + token * p.k_out_token) + from * D;
+    r.norm_w = is_q ? p.q_norm_w : p.k_norm_w;
+    r.heads = min(p.chunk, (is_q ? p.Hq : p.Hkv) - from);
+    return r;
+}
+
+// Position of a token of row `row`, or -1 where it has none.
+__device__ __forceinline__ int position_in(const RowsParams& p, int row, int token, bool tell) {
+    const int begin = p.row_offsets[row], end = p.row_offsets[row + 1], start = p.start_pos[row];
+    if (token < begin || token >= end || start < 0) return -1;
+    const long long pos = static_cast<long long>(start) + (token - begin);
+    if (pos >= p.max_position) {
+        if (p.status_flag != nullptr && tell) atomicOr(p.status_flag, AC_FLAG_POSITION_OOB);
+        return -1;
+    }
+    return static_cast<int>(pos);
+}
+
+// The row of a token is the last one whose offset is <= token.  Here for one token of the whole warp: each round the 32 lanes
+// look at the ends of 32 equal pieces of what is left.
+__device__ __forceinline__ int warp_token_position(const RowsParams& p, int token, int lane) {
     int lo = 0, n = p.B;                                   // the row is in [lo, lo + n)
     while (n > 1) {
         const int piece = (n + 31) / 32;
@@ -40,182 +71,324 @@ __device__ __forceinline__ int token_position(const RowsParams& p, int token, in
         lo += k * piece;
         n = min(piece, n - k * piece);
     }
-    const int begin = p.row_offsets[lo], end = p.row_offsets[lo + 1];
-    const int start = p.start_pos[lo];
-    if (token < begin || token >= end || start < 0) return -1;
-    const long long pos = static_cast<long long>(start) + (token - begin);
-    if (pos >= p.max_position) {
-        if (p.status_flag != nullptr && lane == 0) atomicOr(p.status_flag, AC_FLAG_POSITION_OOB);
-        return -1;
+    return position_in(p, lo, token, lane == 0);
+}
+// And for a token of each lane.
+__device__ __forceinline__ int lane_token_position(const RowsParams& p, int token) {
+    int lo = 0, hi = p.B;
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) / 2;
+        if (p.row_offsets[mid] <= token) lo = mid; else hi = mid;
     }
-    return static_cast<int>(pos);
+    return position_in(p, lo, token, true);
 }
 
-// A warp takes `chunk` heads of one token: D/8 lanes per vector, eight elements (16 bytes) each, so that 2 (D = 128) or 4
-// vectors are worked on side by side and the token's cosines and sines are loaded once.  A lane's partners in the other
-// half are one shuffle away; where pairs are interleaved they are its own elements.
-//
-// Bound: HBM, 2 bytes in and out per element.  70.3 thousand tokens of 40 heads of 128 (1.44 GB): see the launcher below.
-template <int D, bool INTERLEAVED, bool NORM>
-__global__ void __launch_bounds__(256) rope_rows_kernel(const RowsParams p) {
-    constexpr int LPV = D / 8, VECS = 32 / LPV, U = 4;     // U vectors of a lane in flight
-    const int lane = threadIdx.x & 31;
-    const long long item = static_cast<long long>(blockIdx.x) * 8 + (threadIdx.x >> 5);
-    if (item >= static_cast<long long>(p.total_tokens) * p.chunks) return;
-    const int token = static_cast<int>(item / p.chunks);
-    const int piece = static_cast<int>(item - static_cast<long long>(token) * p.chunks);
-    const int heads = p.Hq + p.Hkv;
-    const int h_end = min(heads, (piece + 1) * p.chunk);
-    const int at = lane % LPV, h0 = piece * p.chunk + lane / LPV;
-    const uint16_t* const q_src = p.q_in + token * p.q_in_token + at * 8;
-    const uint16_t* const k_src = p.k_in + token * p.k_in_token + at * 8;
+// Per-head RMSNorm of a lane's 16 elements (words x), D/16 lanes per vector: the fp64 arithmetic of rope_variant_vector.  The whole warp.
+template <int D>
+__device__ __forceinline__ void normalise16(uint32_t (&x)[8], const uint16_t* w0, const uint16_t* w1, float eps) {
+    double ss = 0.0;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+        const double d = static_cast<double>(__uint_as_float((e & 1) ? x[e >> 1] & 0xFFFF0000u : x[e >> 1] << 16));
+        ss = __dadd_rn(ss, __dmul_rn(d, d));
+    }
+#pragma unroll
+    for (int off = D / 32; off >= 1; off >>= 1) ss = __dadd_rn(ss, __shfl_xor_sync(0xffffffffu, ss, off));
+    const double rr = __ddiv_rn(1.0, __dsqrt_rn(__dadd_rn(__ddiv_rn(ss, static_cast<double>(D)), static_cast<double>(eps))));
+    const float rr_hi = static_cast<float>(rr), rr_lo = static_cast<float>(rr - static_cast<double>(rr_hi));
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+        const uint4 wv = __ldg(reinterpret_cast<const uint4*>(half ? w1 : w0));
+        const uint32_t wr[4] = {wv.x, wv.y, wv.z, wv.w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const uint32_t raw = x[4 * half + e];
+            x[4 * half + e] = rmsnorm_feature(static_cast<uint16_t>(raw), rr, rr_hi, rr_lo, __uint_as_float(wr[e] << 16)) |
+                              (static_cast<uint32_t>(rmsnorm_feature(static_cast<uint16_t>(raw >> 16), rr, rr_hi, rr_lo,
+                                                                     __uint_as_float(wr[e] & 0xFFFF0000u))) << 16);
+        }
+    }
+}
 
-    auto load = [&](uint4 (&x)[U], int h) {
+__device__ __forceinline__ void unpack(uint32_t (&x)[8], const uint4& a, const uint4& b) {
+    x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w, x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
+}
+
+// How the elements of a vector lie in D/16 lanes: a lane holds eight pairs, 16 bytes of either half, or 32 side by side where pairs are
+// interleaved (lanes past the rotary part hold 32 as well), so that partners never leave a lane and an angle serves two results.
+template <int D, bool INTERLEAVED>
+struct LaneElements {
+    int at, e0, apart;                                     // lane in the vector; its two runs of eight elements
+    bool turned;
+    __device__ __forceinline__ LaneElements(int lane, int rotary_dim) {
+        at = lane % (D / 16);
+        turned = at < rotary_dim / 16;
+        e0 = INTERLEAVED || !turned ? 16 * at : 8 * at;
+        apart = INTERLEAVED || !turned ? 8 : rotary_dim / 2;
+    }
+};
+
+// Few tokens: a warp takes a piece, four (D = 128) or eight vectors side by side, straight from and to memory.
+template <int D, bool INTERLEAVED, bool NORM>
+__global__ void __launch_bounds__(128) rope_rows_kernel(const RowsParams p) {
+    constexpr int LPV = D / 16, VECS = 32 / LPV, U = 2;    // U vectors of a lane at a time
+    const int lane = threadIdx.x & 31;
+    const unsigned item = blockIdx.x * 4 + (threadIdx.x >> 5);
+    const int token = static_cast<int>(item / static_cast<unsigned>(p.chunks));
+    if (token >= p.total_tokens) return;
+    const Piece at = find_piece<D>(p, token, static_cast<int>(item - static_cast<unsigned>(token) * p.chunks));
+    const LaneElements<D, INTERLEAVED> le(lane, p.rotary_dim);
+    const uint16_t* const src = at.src + le.e0;
+    uint16_t* const dst = at.dst + le.e0;
+
+    uint4 x[U][2];
+    auto load = [&](int h) {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int hh = h + u * VECS;
-            x[u] = make_uint4(0u, 0u, 0u, 0u);
-            if (hh < h_end)
-                x[u] = __ldcs(reinterpret_cast<const uint4*>(hh < p.Hq ? q_src + hh * D : k_src + (hh - p.Hq) * D));
+            x[u][0] = x[u][1] = make_uint4(0u, 0u, 0u, 0u);
+            if (h + u * VECS < at.heads) {
+                x[u][0] = __ldcs(reinterpret_cast<const uint4*>(src + (h + u * VECS) * D));
+                x[u][1] = __ldcs(reinterpret_cast<const uint4*>(src + (h + u * VECS) * D + le.apart));
+            }
         }
     };
-    uint4 x[U];
-    load(x, h0);                                           // does not wait for the position
-
-    const int pos = token_position(p, token, lane);
+    load(lane / LPV);                                      // does not wait for the position
+    const int pos = warp_token_position(p, token, lane);
     if (pos < 0) return;
-    const int half = p.rotary_dim / 2, hl = half / 8;      // lanes of a half
-    const bool turned = at * 8 < p.rotary_dim;
-    const bool second = !INTERLEAVED && at >= hl;
-    const int partner = (lane - at) + (second ? at - hl : at + hl) % LPV;        // of lanes that pass through: anyone
-    float c[8], s[8];
-    if (turned) {
-        const float* cr = p.rope_cos + static_cast<size_t>(pos) * half;
-        const float* sr = p.rope_sin + static_cast<size_t>(pos) * half;
-        if (INTERLEAVED) {
-            const float4 cv = __ldg(reinterpret_cast<const float4*>(cr) + at), sv = __ldg(reinterpret_cast<const float4*>(sr) + at);
-            const float cc[4] = {cv.x, cv.y, cv.z, cv.w}, ss[4] = {sv.x, sv.y, sv.z, sv.w};
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                c[2 * i] = c[2 * i + 1] = cc[i];
-                s[2 * i] = ss[i];
-                s[2 * i + 1] = -ss[i];
-            }
-        } else {
-            const int i0 = (second ? at - hl : at) * 2;
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const float4 cv = __ldg(reinterpret_cast<const float4*>(cr) + i0 + i), sv = __ldg(reinterpret_cast<const float4*>(sr) + i0 + i);
-                const float sign = second ? -1.0f : 1.0f;
-                c[4 * i] = cv.x, c[4 * i + 1] = cv.y, c[4 * i + 2] = cv.z, c[4 * i + 3] = cv.w;
-                s[4 * i] = sign * sv.x, s[4 * i + 1] = sign * sv.y, s[4 * i + 2] = sign * sv.z, s[4 * i + 3] = sign * sv.w;
-            }
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) c[i] = s[i] = 0.0f;    // not used
-    }
-
-    uint16_t* const q_dst = p.q_out + token * p.q_out_token + at * 8;
-    uint16_t* const k_dst = p.k_out + token * p.k_out_token + at * 8;
-    for (int h = h0; h < h_end + lane / LPV; h += U * VECS) {      // the same number of rounds for every lane
+    RopeAngles angles;
+    const size_t angle0 = static_cast<size_t>(pos) * (p.rotary_dim / 2) + (le.turned ? 8 * le.at : 0);
+    angles.set(p.rope_cos + angle0, p.rope_sin + angle0);
+    for (int h0 = 0; h0 < at.heads; h0 += U * VECS) {
+        if (h0 > 0) load(h0 + lane / LPV);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int hh = h + u * VECS;
-            uint4 v = x[u];
-            if (NORM) {
-                const bool is_q = hh < p.Hq;
-                const uint16_t* w = is_q ? p.q_norm_w : p.k_norm_w;
-                const uint32_t raw[4] = {v.x, v.y, v.z, v.w};
-                double ss = 0.0;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const double d = static_cast<double>(__uint_as_float((e & 1) ? raw[e >> 1] & 0xFFFF0000u : raw[e >> 1] << 16));
-                    ss = __dadd_rn(ss, __dmul_rn(d, d));
-                }
-#pragma unroll
-                for (int off = LPV / 2; off >= 1; off >>= 1) ss = __dadd_rn(ss, __shfl_xor_sync(0xffffffffu, ss, off));
-                if (w != nullptr) {
-                    const double rr = __ddiv_rn(1.0, __dsqrt_rn(__dadd_rn(__ddiv_rn(ss, static_cast<double>(D)), static_cast<double>(p.norm_eps))));
-                    const float rr_hi = static_cast<float>(rr), rr_lo = static_cast<float>(rr - static_cast<double>(rr_hi));
-                    const uint4 wv = __ldg(reinterpret_cast<const uint4*>(w) + at);
-                    const uint32_t wr[4] = {wv.x, wv.y, wv.z, wv.w};
-                    uint32_t y[4];
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        y[e] = rmsnorm_feature(static_cast<uint16_t>(raw[e]), rr, rr_hi, rr_lo, __uint_as_float(wr[e] << 16)) |
-                               (static_cast<uint32_t>(rmsnorm_feature(static_cast<uint16_t>(raw[e] >> 16), rr, rr_hi, rr_lo,
-                                                                      __uint_as_float(wr[e] & 0xFFFF0000u))) << 16);
-                    v = make_uint4(y[0], y[1], y[2], y[3]);
-                }
+            const int h = h0 + lane / LPV + u * VECS;
+            uint32_t v[8];
+            unpack(v, x[u][0], x[u][1]);
+            if (NORM && at.norm_w != nullptr) normalise16<D>(v, at.norm_w + le.e0, at.norm_w + le.e0 + le.apart, p.norm_eps);
+            if (h < at.heads) {
+                if (le.turned) rope_turn16<INTERLEAVED>(v, angles);
+                __stcs(reinterpret_cast<uint4*>(dst + h * D), make_uint4(v[0], v[1], v[2], v[3]));
+                __stcs(reinterpret_cast<uint4*>(dst + h * D + le.apart), make_uint4(v[4], v[5], v[6], v[7]));
             }
-            uint4 other;
-            if (INTERLEAVED) {
-                other = make_uint4(__byte_perm(v.x, 0u, 0x1032), __byte_perm(v.y, 0u, 0x1032), __byte_perm(v.z, 0u, 0x1032),
-                                   __byte_perm(v.w, 0u, 0x1032));
-            } else {
-                other.x = __shfl_sync(0xffffffffu, v.x, partner);
-                other.y = __shfl_sync(0xffffffffu, v.y, partner);
-                other.z = __shfl_sync(0xffffffffu, v.z, partner);
-                other.w = __shfl_sync(0xffffffffu, v.w, partner);
-            }
-            if (hh < h_end) {
-                if (turned) v = rope_turn8(v, other, c, s);
-                __stcs(reinterpret_cast<uint4*>(hh < p.Hq ? q_dst + hh * D : k_dst + (hh - p.Hq) * D), v);
-            }
-            __syncwarp();
         }
-        load(x, h + U * VECS);
     }
 }
 
-// The general form, for halves that are no whole number of lanes: a warp per vector, partners through shared memory.
+// Many tokens: the warps of persistent CTAs take pieces in turn.  Each has a ring of stages in shared memory; a stage receives
+// a piece and its row of angles by bulk copies, is rotated in place and leaves by a bulk copy, so that the bytes in flight cost no
+// registers and loads run ahead of the arithmetic by as many pieces as there are stages.  The positions of the next 32 pieces are
+// looked up at a time, one per lane.
+//
+// Bound: HBM, 2 bytes in and out per element.
+constexpr int kPieceBytes = 4096, kAngleBytes = 256;       // at most, of a piece and of its cosines or sines
+// 70.3 thousand tokens of 40 heads of 128, us, by (warps per SM, stages): (8, 4) 279, (12, 3) 243, (12, 4) 233, (10, 5) 256, (13, 3)
+// 278, (16, 3) 265; pieces of 2 or 8 KB are slower.
+constexpr int kStreamWarps = 12, kStreamStages = 4;
+constexpr int kStores = 1;                                 // stores that may still read their stages while the next piece is fetched
+constexpr int kStageBytes = kPieceBytes + 2 * kAngleBytes;
+constexpr int kStreamSmem = kStreamWarps * kStreamStages * (kStageBytes + 8) + 128;
+
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src),
+                 "r"(bytes), "r"(bar)
+                 : "memory");
+}
+__device__ __forceinline__ void bulk_store(void* dst, uint32_t src, uint32_t bytes) {
+    asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"(dst), "r"(src), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void bulk_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void bulk_wait_read() {         // all but the last N stores have read their stage
+    asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(N) : "memory");
+}
+
+template <int D, bool INTERLEAVED, bool NORM>
+__global__ void __launch_bounds__(kStreamWarps * 32, 1) rope_rows_stream_kernel(const RowsParams p) {
+    constexpr int LPV = D / 16, VECS = 32 / LPV, S = kStreamStages;
+    extern __shared__ uint8_t smem_raw[];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    uint8_t* const smem = smem_raw + (((smem_addr(smem_raw) + 127u) & ~127u) - smem_addr(smem_raw));
+    uint8_t* const ring = smem + warp * S * kStageBytes;
+    const uint32_t ring_at = smem_addr(ring);
+    const uint32_t bars = smem_addr(smem + kStreamWarps * S * kStageBytes) + warp * S * 8;
+    if (lane == 0) {
+#pragma unroll
+        for (int s = 0; s < S; ++s) mbar_init(bars + s * 8, 1);
+        mbar_init_fence();
+    }
+    __syncwarp();
+
+    const long long items = static_cast<long long>(p.total_tokens) * p.chunks;
+    const unsigned warps = gridDim.x * kStreamWarps;
+    const unsigned first = blockIdx.x * kStreamWarps + warp;       // this warp's pieces: first + n * warps
+    const long long n_my = first < items ? (items - first - 1) / warps + 1 : 0;
+    const uint32_t angle_bytes = p.rotary_dim * 2;
+    const LaneElements<D, INTERLEAVED> le(lane, p.rotary_dim);
+
+    int i_token = 0, i_piece = 0, i_pos = -1;              // lane l: piece 32 m + l, among those being fetched
+    int c_token = 0, c_piece = 0, c_pos = -1;              // and among those being rotated
+    auto look_up = [&](long long n0) {
+        const long long n = n0 + lane;
+        i_pos = -1;
+        if (n < n_my) {
+            const long long item = first + n * warps;
+            i_token = static_cast<int>(item / p.chunks);
+            i_piece = static_cast<int>(item - static_cast<long long>(i_token) * p.chunks);
+            i_pos = lane_token_position(p, i_token);
+        }
+    };
+    auto fetch = [&](long long n, int stage) {
+        const int src = static_cast<int>(n & 31);
+        const int token = __shfl_sync(0xffffffffu, i_token, src), piece = __shfl_sync(0xffffffffu, i_piece, src);
+        const int pos = __shfl_sync(0xffffffffu, i_pos, src);
+        if (lane == 0) {
+            const uint32_t bar = bars + stage * 8, at = ring_at + stage * kStageBytes;
+            if (pos >= 0) {
+                const Piece what = find_piece<D>(p, token, piece);
+                const uint32_t bytes = what.heads * D * 2;
+                mbar_arrive_expect_tx(bar, bytes + 2 * angle_bytes);
+                bulk_load(at, what.src, bytes, bar);
+                const size_t angle0 = static_cast<size_t>(pos) * (p.rotary_dim / 2);
+                bulk_load(at + kPieceBytes, p.rope_cos + angle0, angle_bytes, bar);
+                bulk_load(at + kPieceBytes + kAngleBytes, p.rope_sin + angle0, angle_bytes, bar);
+            } else {
+                mbar_arrive(bar);                          // nothing to fetch, nothing to write
+            }
+        }
+    };
+    look_up(0);
+#pragma unroll
+    for (int s = 0; s < S - 1 - kStores; ++s)
+        if (s < n_my) fetch(s, s);
+
+    int stage = 0;
+    uint32_t parity = 0;
+    for (long long n = 0; n < n_my; ++n) {
+        if ((n & 31) == 0) c_token = i_token, c_piece = i_piece, c_pos = i_pos;
+        const long long ahead = n + S - 1 - kStores;
+        if (ahead < n_my) {
+            if ((ahead & 31) == 0) look_up(ahead);
+            if (lane == 0) bulk_wait_read<kStores>();
+            fetch(ahead, (stage + S - 1 - kStores) % S);
+        }
+        const int src = static_cast<int>(n & 31);
+        const int token = __shfl_sync(0xffffffffu, c_token, src), piece = __shfl_sync(0xffffffffu, c_piece, src);
+        const int pos = __shfl_sync(0xffffffffu, c_pos, src);
+        if (!__all_sync(0xffffffffu, mbar_wait_bounded(bars + stage * 8, parity))) {
+            // Record the failure, and give the copies in flight a bounded chance to land before the shared memory is released.
+            if (lane == 0 && p.status_flag != nullptr) atomicOr(p.status_flag, AC_FLAG_WAIT_TIMEOUT);
+            for (int s = 0; s < S && n + s < n_my; ++s)
+                mbar_wait_bounded(bars + (stage + s) % S * 8, stage + s < S ? parity : parity ^ 1u);
+            break;
+        }
+        if (pos >= 0) {
+            uint8_t* const at = ring + stage * kStageBytes;
+            const Piece what = find_piece<D>(p, token, piece);
+            RopeAngles angles;
+            const float* cr = reinterpret_cast<const float*>(at + kPieceBytes) + (le.turned ? 8 * le.at : 0);
+            angles.set_shared(cr, cr + kAngleBytes / 4);
+            uint16_t* const x = reinterpret_cast<uint16_t*>(at) + le.e0;
+            for (int h0 = 0; h0 < what.heads; h0 += VECS) {
+                const int h = h0 + lane / LPV;
+                const bool on = h < what.heads;
+                uint32_t v[8];
+                if (NORM || (on && le.turned)) {
+                    uint4* const v0 = reinterpret_cast<uint4*>(x + (on ? h : 0) * D);
+                    uint4* const v1 = reinterpret_cast<uint4*>(x + (on ? h : 0) * D + le.apart);
+                    unpack(v, *v0, *v1);
+                    if (NORM) {
+                        if (what.norm_w != nullptr) normalise16<D>(v, what.norm_w + le.e0, what.norm_w + le.e0 + le.apart, p.norm_eps);
+                        __syncwarp();                      // lanes without a vector of their own have read another's
+                    }
+                    if (on) {
+                        if (le.turned) rope_turn16<INTERLEAVED>(v, angles);
+                        *v0 = make_uint4(v[0], v[1], v[2], v[3]);
+                        *v1 = make_uint4(v[4], v[5], v[6], v[7]);
+                    }
+                }
+            }
+            fence_proxy_async_shared();
+            __syncwarp();
+            if (lane == 0) bulk_store(what.dst, ring_at + stage * kStageBytes, what.heads * D * 2);
+        }
+        if (lane == 0) bulk_commit();                      // a group for every piece, empty where nothing is written
+        if (++stage == S) {
+            stage = 0;
+            parity ^= 1u;
+        }
+    }
+    if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+}
+
+// The general form, for rotary parts that are no whole number of lanes: a warp per vector, partners through shared memory.
 template <int D>
 __global__ void __launch_bounds__(256) rope_rows_any_kernel(const RowsParams p) {
     constexpr int EPL = D / 32;
     __shared__ uint16_t s_vec[8][D];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const long long item = static_cast<long long>(blockIdx.x) * 8 + warp;
-    if (item >= static_cast<long long>(p.total_tokens) * p.chunks) return;
-    const int token = static_cast<int>(item / p.chunks);
-    const int piece = static_cast<int>(item - static_cast<long long>(token) * p.chunks);
-    const int pos = token_position(p, token, lane);
+    const unsigned item = blockIdx.x * 8 + warp;
+    const int token = static_cast<int>(item / static_cast<unsigned>(p.chunks));
+    if (token >= p.total_tokens) return;
+    const int pos = warp_token_position(p, token, lane);
     if (pos < 0) return;
-    const int half = p.rotary_dim / 2;
-    const int h_end = min(p.Hq + p.Hkv, (piece + 1) * p.chunk);
-    for (int h = piece * p.chunk; h < h_end; ++h) {
-        const bool is_q = h < p.Hq;
-        const uint16_t* src = is_q ? p.q_in + token * p.q_in_token + h * D : p.k_in + token * p.k_in_token + (h - p.Hq) * D;
-        uint16_t* dst = is_q ? p.q_out + token * p.q_out_token + h * D : p.k_out + token * p.k_out_token + (h - p.Hq) * D;
+    const Piece at = find_piece<D>(p, token, static_cast<int>(item - static_cast<unsigned>(token) * p.chunks));
+    const float* cr = p.rope_cos + static_cast<size_t>(pos) * (p.rotary_dim / 2);
+    const float* sr = p.rope_sin + static_cast<size_t>(pos) * (p.rotary_dim / 2);
+    for (int h = 0; h < at.heads; ++h) {
         uint16_t x[EPL];
 #pragma unroll
-        for (int e = 0; e < EPL; ++e) x[e] = src[lane * EPL + e];
-        rope_variant_vector<D>(x, is_q ? p.q_norm_w : p.k_norm_w, p.norm_eps, p.rope_cos + static_cast<size_t>(pos) * half,
-                               p.rope_sin + static_cast<size_t>(pos) * half, p.rotary_dim, p.interleaved, s_vec[warp], lane);
+        for (int e = 0; e < EPL; ++e) x[e] = at.src[h * D + lane * EPL + e];
+        if (at.norm_w != nullptr) rope_variant_vector<D>(x, at.norm_w, p.norm_eps, cr, sr, p.rotary_dim, p.interleaved, s_vec[warp], lane);
+        else rope_vector<D>(x, cr, sr, p.rotary_dim, p.interleaved, s_vec[warp], lane);
 #pragma unroll
-        for (int e = 0; e < EPL; ++e) dst[lane * EPL + e] = x[e];
+        for (int e = 0; e < EPL; ++e) at.dst[h * D + lane * EPL + e] = x[e];
     }
 }
 
+#define AC_ROPE_EACH(DO, D_) DO(D_, false, false) DO(D_, false, true) DO(D_, true, false) DO(D_, true, true)
+
+// From how many bytes of input on the streaming kernel is used: 28 + 4 heads of 128, us, direct and streaming: 200 tokens 3.2 and
+// 5.2, 2000 tokens 9.6 and 11.4, 4000 (33 MB) 17.4 and 17.9, 8000 (66 MB) 31.6 and 30.8.
+constexpr long long kStreamFromBytes = 48 << 20;
+
 template <int D>
 cudaError_t launch_rows(RowsParams p, int sms, cudaStream_t stream) {
-    // Pieces of a token: as many as fill the GPU (32 warps per SM) where there are few tokens, of 8 (D = 128) or 16 vectors at least.
-    const int heads = p.Hq + p.Hkv;
-    constexpr int kLeast = 4 * 32 / (D / 8);
-    const long long want = (32ll * sms + p.total_tokens - 1) / p.total_tokens;
-    const int most = (heads + kLeast - 1) / kLeast;
-    const int chunks = static_cast<int>(want < most ? want : most);
-    p.chunk = (heads + chunks - 1) / chunks;
-    p.chunk = (p.chunk + kLeast - 1) / kLeast * kLeast;
-    p.chunks = (heads + p.chunk - 1) / p.chunk;
-    const long long items = static_cast<long long>(p.total_tokens) * p.chunks;
-    const long long grid = (items + 7) / 8;
-    if (grid > 0x7fffffffll) return cudaErrorInvalidConfiguration;
-    const unsigned g = static_cast<unsigned>(grid);
+    const bool any = p.rotary_dim % 16 != 0;
     const bool norm = p.q_norm_w != nullptr || p.k_norm_w != nullptr;
-    if (p.rotary_dim % (p.interleaved ? 8 : 16) != 0) rope_rows_any_kernel<D><<<g, 256, 0, stream>>>(p);
-    else if (p.interleaved) norm ? rope_rows_kernel<D, true, true><<<g, 256, 0, stream>>>(p) : rope_rows_kernel<D, true, false><<<g, 256, 0, stream>>>(p);
-    else norm ? rope_rows_kernel<D, false, true><<<g, 256, 0, stream>>>(p) : rope_rows_kernel<D, false, false><<<g, 256, 0, stream>>>(p);
+    const int heads = p.Hq + p.Hkv;
+    const bool many = !any && static_cast<long long>(p.total_tokens) * heads * D * 2 >= kStreamFromBytes;
+    // Pieces of 4 KB at most; where that leaves warps without one (32 per SM), half or a quarter of it.
+    p.chunk = kPieceBytes / (2 * D);
+    auto cut = [&]() {
+        p.q_chunks = (p.Hq + p.chunk - 1) / p.chunk;
+        p.chunks = p.q_chunks + (p.Hkv + p.chunk - 1) / p.chunk;
+    };
+    cut();
+    while (!many && p.chunk > 1024 / (2 * D) && static_cast<long long>(p.total_tokens) * p.chunks < 32ll * sms) {
+        p.chunk /= 2;
+        cut();
+    }
+    const long long items = static_cast<long long>(p.total_tokens) * p.chunks;
+    if (many) {
+        const long long most = (items + kStreamWarps - 1) / kStreamWarps;
+        const unsigned grid = static_cast<unsigned>(most < sms ? most : sms);
+#define AC_ROPE_STREAM(D_, I_, N_)                                                                                   \
+    if ((p.interleaved != 0) == I_ && norm == N_) rope_rows_stream_kernel<D_, I_, N_><<<grid, kStreamWarps * 32, kStreamSmem, stream>>>(p);
+        AC_ROPE_EACH(AC_ROPE_STREAM, D)
+#undef AC_ROPE_STREAM
+        return cudaGetLastError();
+    }
+    if (items > 0xffffffffll - 8) return cudaErrorInvalidConfiguration;
+    if (any) {
+        rope_rows_any_kernel<D><<<static_cast<unsigned>((items + 7) / 8), 256, 0, stream>>>(p);
+    } else {
+        const unsigned grid = static_cast<unsigned>((items + 3) / 4);
+#define AC_ROPE_DIRECT(D_, I_, N_)                                                                                   \
+    if ((p.interleaved != 0) == I_ && norm == N_) rope_rows_kernel<D_, I_, N_><<<grid, 128, 0, stream>>>(p);
+        AC_ROPE_EACH(AC_ROPE_DIRECT, D)
+#undef AC_ROPE_DIRECT
+    }
     return cudaGetLastError();
 }
 
@@ -260,6 +433,18 @@ __global__ void __launch_bounds__(256) rope_tables_kernel(float* __restrict__ co
 
 }  // namespace
 
+cudaError_t rope_rows_set_attributes(int smem_optin) {
+    if (kStreamSmem > smem_optin) return cudaErrorInvalidConfiguration;
+    cudaError_t e = cudaSuccess;
+#define AC_ROPE_SET(D_, I_, N_)                                                                                      \
+    if (e == cudaSuccess)                                                                                            \
+        e = cudaFuncSetAttribute(rope_rows_stream_kernel<D_, I_, N_>, cudaFuncAttributeMaxDynamicSharedMemorySize, kStreamSmem);
+    AC_ROPE_EACH(AC_ROPE_SET, 128)
+    AC_ROPE_EACH(AC_ROPE_SET, 64)
+#undef AC_ROPE_SET
+    return e;
+}
+
 cudaError_t launch_rope_rows(const void* q_in, void* q_out, int64_t q_in_token, int64_t q_out_token, const void* k_in,
                              void* k_out, int64_t k_in_token, int64_t k_out_token, const int32_t* start_pos,
                              const int32_t* row_offsets, int total_tokens, int B, int Hq, int Hkv, int d,
@@ -290,7 +475,7 @@ cudaError_t launch_rope_rows(const void* q_in, void* q_out, int64_t q_in_token, 
     p.Hkv = Hkv;
     p.rotary_dim = r.rotary_dim;
     p.interleaved = r.interleaved;
-    p.chunk = p.chunks = 0;
+    p.chunk = p.q_chunks = p.chunks = 0;
     p.status_flag = status_flag;
     return d == 128 ? launch_rows<128>(p, sms, stream) : launch_rows<64>(p, sms, stream);
 }

@@ -752,6 +752,8 @@ class Rope(_OnDevice):
         for t, what in zip(self._norms, ("q_norm_weight", "k_norm_weight")):
             if t is not None:
                 _want(t, what, (t.shape[-1],), _BF16, self.device)
+        self._head = next((t.shape[-1] for t in self._norms if t is not None), None)
+        self._tables = cos.data_ptr(), sin.data_ptr()
         self._options = ac._rope_options(self.rotary_dim, interleaved, q_norm_weight, k_norm_weight, norm_eps)
 
     @classmethod
@@ -781,14 +783,16 @@ class Rope(_OnDevice):
         self._enqueue("ac_rope_tables", [self.cos.data_ptr(), self.sin.data_ptr(), int(first_position), self.max_position,
                                          self.rotary_dim, how, None], stream, -1)
 
-    def _tokens(self, t, name, total, d):
-        """t is [total, heads, d] bf16 with dense heads; returns the elements from one token to the next."""
-        if t.dim() != 3 or t.shape[0] != total or t.shape[2] != d or t.dtype not in _BF16 or t.device != self.device:
-            raise ValueError(f"{name}: {t.dtype} {tuple(t.shape)} on {t.device}, expected bf16 [{total}, heads, {d}] on {self.device}")
-        heads = t.shape[1]
-        if t.stride(2) != 1 or (heads > 1 and t.stride(1) != d):
+    def _tokens(self, t, name, shape):
+        """t is bf16 of this shape [tokens, heads, d] with dense heads; returns the elements from one token to the next."""
+        if isinstance(t, torch.Tensor) and t.shape == shape and t.dtype in _BF16 and t.device == self.device:
+            apart, head, element = t.stride()
+            if element == 1 and (head == shape[2] or shape[1] == 1):
+                return apart if shape[0] > 1 else max(8, shape[1] * shape[2])
             raise ValueError(f"{name}: heads of a token are not contiguous")
-        return t.stride(0) if total > 1 else max(heads * d, 8)
+        if not isinstance(t, torch.Tensor):
+            raise TypeError(f"{name}: {type(t).__name__}, expected a tensor")
+        raise ValueError(f"{name}: {t.dtype} {tuple(t.shape)} on {t.device}, expected bf16 {tuple(shape)} on {self.device}")
 
     def rows(self, q, k, start_pos, row_offsets, q_out=None, k_out=None, stream=None):
         """Rotates q [tokens, Hq, d] and k [tokens, Hkv, d] (bf16, d 64 or 128; k may be None): row b's tokens row_offsets[b] ..
@@ -797,29 +801,30 @@ class Rope(_OnDevice):
         inputs; tokens of no row stay as they are.  Returns q_out, k_out."""
         if not isinstance(q, torch.Tensor) or q.dim() != 3:
             raise ValueError("q: expected a tensor [tokens, heads, d]")
-        total, Hq, d = q.shape
+        shape = q.shape
+        total, Hq, d = shape
+        if d != self._head and any(t is not None and t.shape[-1] != d for t in self._norms):
+            raise ValueError(f"norm weights for heads of another size than {d}")
         B = start_pos.shape[0]
         _want(start_pos, "start_pos", (B,), (torch.int32,), self.device)
         _want(row_offsets, "row_offsets", (B + 1,), (torch.int32,), self.device)
-        for t, what in zip(self._norms, ("q_norm_weight", "k_norm_weight")):
-            if t is not None and t.shape[-1] != d:
-                raise ValueError(f"{what}: {t.shape[-1]} weights for heads of {d}")
-        q_out = self._new(q.shape, stream, q.dtype) if q_out is None else q_out
-        strides = [self._tokens(q, "q", total, d), self._tokens(q_out, "q_out", total, d)]
-        if q_out.shape != q.shape:
-            raise ValueError(f"q_out: shape {tuple(q_out.shape)}, expected {tuple(q.shape)}")
-        Hkv, k_ptrs, k_strides = 0, [None, None], [0, 0]
-        if k is not None:
-            k_out = self._new(k.shape, stream, k.dtype) if k_out is None else k_out
-            k_strides = [self._tokens(k, "k", total, d), self._tokens(k_out, "k_out", total, d)]
-            if k_out.shape != k.shape:
-                raise ValueError(f"k_out: shape {tuple(k_out.shape)}, expected {tuple(k.shape)}")
-            Hkv, k_ptrs = k.shape[1], [k.data_ptr(), k_out.data_ptr()]
+        if q_out is None:
+            q_out = self._new(shape, stream, q.dtype)
+        args = [q.data_ptr(), q_out.data_ptr(), self._tokens(q, "q", shape), self._tokens(q_out, "q_out", shape)]
+        Hkv = 0
+        if k is None:
+            args += None, None, 0, 0
+        else:
+            Hkv = k.shape[1] if k.dim() == 3 else 0
+            shape = torch.Size((total, Hkv, d))
+            if k_out is None:
+                k_out = self._new(shape, stream, k.dtype)
+            args += k.data_ptr(), k_out.data_ptr(), self._tokens(k, "k", shape), self._tokens(k_out, "k_out", shape)
         if total == 0:
             return q_out, k_out
-        self._enqueue("ac_rope_rows", [q.data_ptr(), q_out.data_ptr(), *strides, *k_ptrs, *k_strides, start_pos.data_ptr(),
-                                       row_offsets.data_ptr(), total, B, Hq, Hkv, d, self.cos.data_ptr(), self.sin.data_ptr(),
-                                       self.max_position, self._flag, None, self._options], stream, -2)
+        args += (start_pos.data_ptr(), row_offsets.data_ptr(), total, B, Hq, Hkv, d, self._tables[0], self._tables[1],
+                 self.max_position, self._flag, None, self._options)
+        self._enqueue("ac_rope_rows", args, stream, -2)
         return q_out, k_out
 
 

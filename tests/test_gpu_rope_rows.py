@@ -218,3 +218,41 @@ def test_rotation_feeds_the_decode_step(rt):
     lens.zero_()
     caches[1].store(k_rot, k, table, lens, dev(np.array([0, n], np.int32)))
     assert torch.equal(caches[0].k_codes, caches[1].k_codes) and torch.equal(caches[0].params, caches[1].params)
+
+
+@pytest.mark.parametrize("d,Hq,Hkv,T,R,interleaved,norm", [(128, 17, 1, 12000, 128, False, False), (128, 17, 3, 12000, 64, True, False),
+                                                           (64, 33, 5, 13000, 32, False, True), (64, 40, 0, 12000, 64, True, True)])
+def test_a_call_of_many_tokens_is_its_pieces(rt, d, Hq, Hkv, T, R, interleaved, norm):
+    """Calls of 48 MB and more take another kernel: the same bits, also in place, with rows that are inactive, empty, past the table."""
+    import torch
+    from paper_2606_07665_b200 import binding as ac
+    assert T * (Hq + Hkv) * d * 2 >= 48 << 20
+    rng = np.random.default_rng(7)
+    cut = np.sort(rng.integers(5, T - 5, 40))
+    off = np.concatenate([[5], cut, cut[-1:], [T - 5]]).astype(np.int32)        # one row is empty; tokens of no row at both ends
+    start = rng.integers(0, 50, len(off) - 1).astype(np.int32)
+    start[7], start[20] = -1, 19_000
+    rope = rt.Rope.scaled(20_000, R, interleaved=interleaved, norm_eps=1e-5, q_norm_weight=dev(bits(rng, d)) if norm else None)
+    q, k = torch.randn(T, Hq, d, device="cuda").bfloat16(), torch.randn(T, Hkv, d, device="cuda").bfloat16()
+    q[100:200] = 0
+    q[300, 0, :4] = torch.tensor([float("inf"), float("nan"), 1e38, -0.0])
+    q_out, k_out = torch.full_like(q, 7.0), torch.full_like(k, 7.0)
+    want_q, want_k = q_out.clone(), k_out.clone()
+    k_, ko_ = (k, k_out) if Hkv else (None, None)
+    rope.rows(q, k_, dev(start), dev(off), q_out=q_out, k_out=ko_)
+    same = lambda a, b: torch.equal(a.view(torch.int16), b.view(torch.int16))      # noqa: E731
+    for b in range(len(start)):                                     # each row by itself, from a view that begins with it
+        lo, hi = int(off[b]), int(off[b + 1])
+        if hi > lo:
+            rope.rows(q[lo:hi], k[lo:hi] if Hkv else None, dev(start[b:b + 1]), dev(np.array([0, hi - lo], np.int32)), q_out=want_q[lo:hi],
+                      k_out=want_k[lo:hi] if Hkv else None)
+    assert same(q_out, want_q) and same(k_out, want_k)
+    assert int(rope.status_flag) in (0, ac.AC_FLAG_POSITION_OOB)
+    rope.rows(q, k_, dev(start), dev(off), q_out=q, k_out=k_)
+    untouched = torch.ones(T, dtype=torch.bool, device="cuda")
+    for b in range(len(start)):
+        if start[b] >= 0:
+            untouched[int(off[b]):int(off[b]) + max(0, min(int(off[b + 1] - off[b]), 20_000 - int(start[b])))] = False
+    assert same(q[~untouched], want_q[~untouched]) and same(k[~untouched], want_k[~untouched])
+    assert (want_q[untouched] == 7).all() and not (want_q[~untouched][:, 0] == 7).all(-1).any()
+    torch.cuda.synchronize()
