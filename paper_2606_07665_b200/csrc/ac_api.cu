@@ -979,24 +979,22 @@ int ac_kv_load_q4(void* k, void* v, const ac_q4_cache* cache, const int32_t* blo
                       page_size, num_pages, status_flag, stream, false);
 }
 
-// What the plan of a quantised cache goes by: bytes per token and head (K and V), rates in bytes per second, times in seconds.
-struct PlanRates {
-    double bytes_per_token;
-    double gpu;                // the whole GPU, of 148 SMs
-    double fat, alone, pair, ragged_pair;      // one CTA: of a one-per-SM launch, alone on its SM, sharing it, sharing it in a ragged batch
-    double wave, more_waves, merge;
-};
-
-static int plan_quantised(const PlanRates& rates, const int32_t* token_counts_host, int B, int Hq, int Hkv, int d, int page_size,
-                          int max_context_len, int sm_count, int* num_splits_out, int* split_tokens_out,
-                          size_t* workspace_bytes_out) {
+int ac_decode_plan_q4(const int32_t* token_counts_host, int B, int Hq, int Hkv, int d, int page_size,
+                      int max_context_len, int sm_count, int* num_splits_out, int* split_tokens_out,
+                      size_t* workspace_bytes_out) {
     if (!num_splits_out || !split_tokens_out || !workspace_bytes_out) return AC_ERR_NULL;
     Shape s{B, Hq, Hkv, d, page_size, 1};
     int st = check_shape(s);
     if (st != AC_OK) return st;
     if (max_context_len <= 0) return AC_ERR_SHAPE;
     if (sm_count <= 0) sm_count = g_last_sm_count > 0 ? g_last_sm_count : 148;
-    const double bytes_per_token = rates.bytes_per_token, gpu = rates.gpu * sm_count / 148.0;
+    // Every split count is priced by what launches with one and with two CTAs per SM (q4_attn.cu) were measured to do (short
+    // splits in more than two waves run three CTAs of four warps, which has no price of its own): the whole GPU moves
+    // 5.6 TB/s of this cache (its arithmetic keeps it below HBM's rate), one CTA alone on its SM 43 GB/s with twelve warps
+    // and 32 with six, two sharing an SM 20 each, in a ragged batch 25; a wave costs 4 us of start and end, a further one
+    // 3, the merge through the workspace 1.6 and the partial results' traffic.  (d/2 + 4 d/group bytes per token, side
+    // and head; the plan does not know the group and takes 64.)
+    const double bytes_per_token = 2.0 * (d / 2 + d / 16), gpu = 5.6e12 * sm_count / 148.0;
     auto tokens_of = [&](int b) {
         const int t = token_counts_host == nullptr ? max_context_len : token_counts_host[b];
         return t <= 0 ? 0 : t < max_context_len ? t : max_context_len;
@@ -1030,11 +1028,11 @@ static int plan_quantised(const PlanRates& rates, const int32_t* token_counts_ho
         }
         n *= Hkv;
         const bool fat = static_cast<long long>(B) * Hkv * cand <= sm_count;
-        const double rate = fat ? rates.fat : n <= sm_count ? rates.alone : n * longest * bytes_per_token > 1.25 * total ? rates.ragged_pair : rates.pair;
+        const double rate = fat ? 43e9 : n <= sm_count ? 32e9 : n * longest * bytes_per_token > 1.25 * total ? 25e9 : 20e9;
         const double alone = longest * bytes_per_token / rate, together = total / gpu;
-        double t = (alone > together ? alone : together) + rates.wave;
-        if (n > 2.0 * sm_count) t += (ceil(n / (2.0 * sm_count)) - 1.0) * rates.more_waves;
-        if (cand > 1) t += rates.merge + 2.0 * n * (Hq / Hkv) * (d + 1.0) * 4.0 / gpu;
+        double t = (alone > together ? alone : together) + 4e-6;
+        if (n > 2.0 * sm_count) t += (ceil(n / (2.0 * sm_count)) - 1.0) * 3e-6;
+        if (cand > 1) t += 1.6e-6 + 2.0 * n * (Hq / Hkv) * (d + 1.0) * 4.0 / gpu;
         if (best == 0.0 || t < best) {
             best = t;
             S = cand;
@@ -1046,20 +1044,6 @@ static int plan_quantised(const PlanRates& rates, const int32_t* token_counts_ho
     *split_tokens_out = split_tokens_for(max_context_len, static_cast<int>(S));
     *workspace_bytes_out = ac_fused_workspace_bytes(B, Hq, Hkv, d, static_cast<int>(S));
     return AC_OK;
-}
-
-int ac_decode_plan_q4(const int32_t* token_counts_host, int B, int Hq, int Hkv, int d, int page_size,
-                      int max_context_len, int sm_count, int* num_splits_out, int* split_tokens_out,
-                      size_t* workspace_bytes_out) {
-    // Every split count is priced by what launches with one and with two CTAs per SM (q4_attn.cu) were measured to do (short
-    // splits in more than two waves run three CTAs of four warps, which has no price of its own): the whole GPU moves
-    // 5.6 TB/s of this cache (its arithmetic keeps it below HBM's rate), one CTA alone on its SM 43 GB/s with twelve warps
-    // and 32 with six, two sharing an SM 20 each, in a ragged batch 25; a wave costs 4 us of start and end, a further one
-    // 3, the merge through the workspace 1.6 and the partial results' traffic.  (d/2 + 4 d/group bytes per token, side
-    // and head; the plan does not know the group and takes 64.)
-    const PlanRates rates = {2.0 * (d / 2 + d / 16), 5.6e12, 43e9, 32e9, 20e9, 25e9, 4e-6, 3e-6, 1.6e-6};
-    return plan_quantised(rates, token_counts_host, B, Hq, Hkv, d, page_size, max_context_len, sm_count, num_splits_out,
-                          split_tokens_out, workspace_bytes_out);
 }
 
 int ac_paged_decode_attn_q4(const void* q_rot, const ac_q4_cache* cache, const int32_t* block_table,
@@ -1233,9 +1217,72 @@ int ac_kv_load_q8(void* k, void* v, const ac_q8_cache* cache, const int32_t* blo
 int ac_decode_plan_q8(const int32_t* token_counts_host, int B, int Hq, int Hkv, int d, int page_size,
                       int max_context_len, int sm_count, int* num_splits_out, int* split_tokens_out,
                       size_t* workspace_bytes_out) {
-    const PlanRates rates = {2.0 * d + 0.5, 6.4e12, 50e9, 36e9, 24e9, 30e9, 4e-6, 3e-6, 1.6e-6};
-    return plan_quantised(rates, token_counts_host, B, Hq, Hkv, d, page_size, max_context_len, sm_count, num_splits_out,
-                          split_tokens_out, workspace_bytes_out);
+    if (!num_splits_out || !split_tokens_out || !workspace_bytes_out) return AC_ERR_NULL;
+    Shape s{B, Hq, Hkv, d, page_size, 1};
+    int st = check_shape(s);
+    if (st != AC_OK) return st;
+    if (max_context_len <= 0) return AC_ERR_SHAPE;
+    if (sm_count <= 0) sm_count = g_last_sm_count > 0 ? g_last_sm_count : 148;
+    // Every split count is priced by what its launch was measured to do: a warp consumes 8.15 GB/s of this cache (0.8 of it with heads of
+    // 64, 0.66 with more than eight heads per KV head), the whole GPU 6.35 TB/s; start and end cost 2.6 us, 1.7 more where SMs
+    // hold several CTAs, 5.3 per further wave, whose last CTAs end a quarter of one's time late; the merge 2 us and the partial
+    // results' traffic.  (Fitted to 130 launches of 16 batches; the choices are within 3 % of the best split count on average, 12 % at worst.)
+    const bool wide = Hq / Hkv > 8;
+    const double bytes_per_token = 2.0 * d + 0.5, gpu = 6.35e12 * sm_count / 148.0;
+    const double warp_rate = 8.15e9 * (d == 64 ? 0.8 : 1.0) * (wide ? 0.66 : 1.0);
+    auto tokens_of = [&](int b) {
+        const int t = token_counts_host == nullptr ? max_context_len : token_counts_host[b];
+        return t <= 0 ? 0 : t < max_context_len ? t : max_context_len;
+    };
+    double total = static_cast<double>(B) * max_context_len;
+    if (token_counts_host != nullptr) {
+        total = 0.0;
+        for (int b = 0; b < B; ++b) total += tokens_of(b);
+    }
+    total *= Hkv * bytes_per_token;
+    long long S = 1;
+    double best = 0.0;
+    long long most = (max_context_len - 1) / 256 + 1;                // splits of at least 256 tokens
+    if (most > 4096) most = 4096;
+    if (most > 1 + 8ll * sm_count / (static_cast<long long>(B) * Hkv)) most = 1 + 8ll * sm_count / (static_cast<long long>(B) * Hkv);
+    for (int cand = 1; cand <= most; ++cand) {
+        const int chunk = split_tokens_for(max_context_len, cand);
+        if (static_cast<long long>(chunk) * (cand - 1) >= max_context_len) continue;      // an empty split
+        double n = static_cast<double>(B) * cand;                                          // CTAs with tokens, per head
+        int longest = chunk < max_context_len ? chunk : max_context_len;
+        if (token_counts_host != nullptr) {
+            long long pieces = 0;
+            longest = 0;
+            for (int b = 0; b < B; ++b) {
+                const int t = tokens_of(b);
+                pieces += t > 0 ? (t - 1) / chunk + 1 : 0;
+                const int piece = t < chunk ? t : chunk;
+                longest = piece > longest ? piece : longest;
+            }
+            n = static_cast<double>(pieces);
+        }
+        n *= Hkv;
+        int warps, per_sm;
+        q8_attn_shape(static_cast<long long>(B) * Hkv * cand, chunk, wide, sm_count, &warps, &per_sm);
+        const double alone = longest * bytes_per_token / (warps * warp_rate), slots = static_cast<double>(per_sm) * sm_count;
+        double t = total / gpu > alone ? total / gpu : alone;
+        if (n > slots) {
+            const double all = total / (slots * warps * warp_rate) + 0.24 * alone;
+            t = (t > all ? t : all) + 5.3e-6 * (ceil(n / slots) - 1.0);
+        }
+        if (per_sm > 1) t += 1.7e-6;
+        if (cand > 1) t += 2e-6 + 2.0 * n * (Hq / Hkv) * (d + 1.0) * 4.0 / gpu;
+        if (best == 0.0 || t < best) {
+            best = t;
+            S = cand;
+        }
+    }
+    const int len = split_tokens_for(max_context_len, static_cast<int>(S));
+    S = (static_cast<long long>(max_context_len) + len - 1) / len;
+    *num_splits_out = static_cast<int>(S);
+    *split_tokens_out = split_tokens_for(max_context_len, static_cast<int>(S));
+    *workspace_bytes_out = ac_fused_workspace_bytes(B, Hq, Hkv, d, static_cast<int>(S));
+    return AC_OK;
 }
 
 int ac_paged_decode_attn_q8(const void* q_rot, const ac_q8_cache* cache, const int32_t* block_table,

@@ -161,6 +161,8 @@ cudaError_t launch_kv_bulk_q8(void* k, void* v, const Q8View& cache, const int32
                               int total_tokens, int B, int Hkv, int d, int page_size, int num_pages,
                               int32_t* status_flag, bool store, int sms, cudaStream_t stream);
 cudaError_t q8_attn_set_attributes(int smem_optin);
+// Warps of a CTA and CTAs per SM that a grid of this many CTAs gets.
+void q8_attn_shape(long long ctas, int split_tokens, bool wide, int sms, int* warps, int* per_sm);
 int q8_attn_box(int page_size);         // tokens of the boxes that the attention kernel's tensor maps must have
 cudaError_t launch_paged_decode_attn_q8(const CUtensorMap& k_map, const CUtensorMap& v_map, const void* q_rot,
                                         const Q8View& cache, const int32_t* block_table, int max_pages_per_seq,

@@ -38,12 +38,14 @@ constexpr float LN2 = 0.6931471805599453f;
 constexpr float kLag = 8.0f;                  // how far (in powers of two) the softmax reference may lag
 constexpr float kLowest = -3.0e38f;           // reference of a warp that has seen no token
 
-template <int D, int NW, int STAGES>
+template <int D, int NT, int NW, int STAGES>
 struct Q8Smem {
     static constexpr int K_BYTES = TILE * D;
     static constexpr int STAGE_BYTES = 2 * K_BYTES;           // K codes, V codes
     static constexpr int RING_BYTES = STAGES * STAGE_BYTES;
-    static constexpr int BAR_OFFSET = NW * RING_BYTES;
+    static constexpr int Q_OFFSET = NW * RING_BYTES;          // query fragments, where they do not stay in registers
+    static constexpr int Q_BYTES = NT == 2 ? D / 16 * 32 * 16 : 0;
+    static constexpr int BAR_OFFSET = Q_OFFSET + Q_BYTES;
     static constexpr int TOTAL = BAR_OFFSET + NW * STAGES * 8 + 1024;      // the swizzle wants rings aligned to 1024
 };
 
@@ -87,7 +89,7 @@ __device__ __forceinline__ uint32_t q8_tile_offset(int row, int chunk) {
 template <int D, int FMT, int NT, int NW, int STAGES, int CTAS>
 __global__ void __launch_bounds__(NW * 32, CTAS) paged_decode_attn_q8_kernel(
     const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map, const Q8AttnParams p) {
-    using L = Q8Smem<D, NW, STAGES>;
+    using L = Q8Smem<D, NT, NW, STAGES>;
     constexpr int WARPS = NW, THREADS = NW * 32;
     constexpr int NC = D / 16;                     // 16-byte chunks (16 elements) per row
 
@@ -103,6 +105,14 @@ __global__ void __launch_bounds__(NW * 32, CTAS) paged_decode_attn_q8_kernel(
     const int S = p.num_splits;
 
     // ---- the row's range: attended tokens laid end to end, in boxes (see the bf16 kernel) ---------------------
+    // Without a window the pages of the first tiles do not depend on the row's length: they are asked for beside it.
+    const int32_t* bt_row = p.block_table + static_cast<size_t>(b) * p.max_pages_per_seq;
+    int page_early = -1;
+    if (p.window == 0) {
+        const uint32_t gr = (static_cast<uint32_t>(split) * p.split_tokens + (warp + (lane >> 1) * WARPS) * TILE) / GRAN + (lane & 1);
+        const uint32_t idx = p.gpp == 1 ? gr : __umulhi(gr, p.gpp_magic);
+        if (idx < static_cast<uint32_t>(p.max_pages_per_seq)) page_early = bt_row[idx];
+    }
     const int ctx = p.context_lens[b];
     int n_tokens = ctx < 0 ? 0 : ctx + p.new_tokens;
     const long long table_tokens = static_cast<long long>(p.max_pages_per_seq) * p.page_size;
@@ -146,7 +156,6 @@ __global__ void __launch_bounds__(NW * 32, CTAS) paged_decode_attn_q8_kernel(
     }
     __syncwarp();
 
-    const int32_t* bt_row = p.block_table + static_cast<size_t>(b) * p.max_pages_per_seq;
     const int n_tiles = (tok_end - tok_begin + TILE - 1) / TILE;
     const int n_my = n_tiles > warp ? (n_tiles - warp + WARPS - 1) / WARPS : 0;
     const uint64_t policy = l2_policy_evict_first();
@@ -214,7 +223,8 @@ __global__ void __launch_bounds__(NW * 32, CTAS) paged_decode_attn_q8_kernel(
     // which may have rounded that block's codes again; no scale is read before ------------------------------------------
     const int dependent_from = (ctx > 0 ? (ctx - 1) / p.block * p.block : 0) - window_base;     // range position, maybe negative
     bool dependency_met = false;
-    settle_pages(0, load_pages(0));
+    int sub_first;
+    settle_pages(0, p.window != 0 ? load_pages(0) : locate(0, sub_first) >= 0 ? page_early : -1);
     int pages_ahead = load_pages(16);
 #pragma unroll
     for (int s = 0; s < STAGES; ++s) {
@@ -264,6 +274,18 @@ __global__ void __launch_bounds__(NW * 32, CTAS) paged_decode_attn_q8_kernel(
         }
         cs[nt][0] = __shfl_sync(0xffffffffu, factor, 8 * t);
         cs[nt][1] = __shfl_sync(0xffffffffu, factor, 8 * t + 4);
+    }
+
+    // With two column blocks the fragments would crowd out the accumulators: they go to shared memory, 16 bytes per chunk and lane
+    // (the same for every warp).
+    uint8_t* const q_frag = smem + L::Q_OFFSET + lane * 16;
+    if constexpr (NT == 2) {
+        if (warp == 0) {
+#pragma unroll
+            for (int c = 0; c < NC; ++c)
+                *reinterpret_cast<uint4*>(q_frag + c * 512) = make_uint4(qb[0][c][0], qb[0][c][1], qb[1][c][0], qb[1][c][1]);
+        }
+        __syncthreads();
     }
 
     // O^T, heads 2t and 2t + 1 as pairs: [chunk][element 2g + i of it]
@@ -345,10 +367,17 @@ __global__ void __launch_bounds__(NW * 32, CTAS) paged_decode_attn_q8_kernel(
                     uint32_t a0, a1, a2, a3;
                     q8_pairs<FMT>(w[2 * i], a0, a2);
                     q8_pairs<FMT>(w[2 * i + 1], a1, a3);
+                    uint32_t b[NT][2];
+                    if constexpr (NT == 2) {
+                        const uint4 f = *reinterpret_cast<const uint4*>(q_frag + (c + i) * 512);
+                        b[0][0] = f.x, b[0][1] = f.y, b[NT - 1][0] = f.z, b[NT - 1][1] = f.w;
+                    } else {
+                        b[0][0] = qb[0][c + i][0], b[0][1] = qb[0][c + i][1];
+                    }
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt) {
-                        if (c + i == 0) mma_f16_16816_zero(acc[nt], a0, a1, a2, a3, qb[nt][0][0], qb[nt][0][1]);
-                        else mma_f16_16816(acc[nt], a0, a1, a2, a3, qb[nt][c + i][0], qb[nt][c + i][1]);
+                        if (c + i == 0) mma_f16_16816_zero(acc[nt], a0, a1, a2, a3, b[nt][0], b[nt][1]);
+                        else mma_f16_16816(acc[nt], a0, a1, a2, a3, b[nt][0], b[nt][1]);
                     }
                 }
             }
@@ -581,17 +610,33 @@ __global__ void __launch_bounds__(NW * 32, CTAS) paged_decode_attn_q8_kernel(
     else merge_splits_from_workspace<D, THREADS, 4, 4>(p, hq0, items, S, n_active);
 }
 
-// Shapes of the CTA:
-//   FAT    one CTA per SM, for grids of at most that many;
-//   BASE   two CTAs per SM: the second one's stream covers the first one's start and end.
-enum class Fit { FAT, BASE };
+// Shapes of the CTA, by the CTAs of the grid and (measured below) with 128 KB of loads in flight on an SM, where HBM delivers most
+// (4 rows of 131072 tokens, 64:8 heads of 128: 161 us with 8 warps of 2 stages against 173 with 12):
+//   FAT    eight warps, one CTA per SM, for grids of at most that many;
+//   BASE   four warps, two CTAs per SM: the second one's stream covers the first one's start and end;
+//   THREE  three CTAs per SM and
+//   SHORT  three warps, four CTAs per SM, for grids of more than two, and more than four, CTAs per SM of short splits, where
+//          starts and ends are much of a CTA's life (256 rows of 512 to 2048 tokens, 32:8 heads: BASE 118 us, THREE 111, SHORT
+//          109; 128 such rows of 28:4: 30.1, 28.3, 33.8; 64 rows of up to 8192, which are not short: 81, 97 in THREE).
+// Groups of 9-16 heads need the arithmetic of more warps: six in BASE (128 rows under a window of 4096, 32:2 heads: 53.6 -> 51.9
+// us; heads of 64: 31 -> 23.5), and at most THREE (256 rows, 36:4 heads: 71 -> 68).
+enum class Fit { FAT, BASE, THREE, SHORT };
+constexpr int kShortSplitTokens = 2560;
+
+constexpr int shape_warps(Fit f, bool wide) { return f == Fit::FAT ? 8 : f == Fit::SHORT ? 3 : f == Fit::BASE && wide ? 6 : 4; }
+constexpr int shape_ctas(Fit f) { return f == Fit::FAT ? 1 : f == Fit::BASE ? 2 : f == Fit::THREE ? 3 : 4; }
+Fit fit_for(long long ctas, int split_tokens, bool wide, int sms) {
+    if (ctas <= sms) return Fit::FAT;
+    if (ctas <= 2ll * sms || split_tokens > kShortSplitTokens) return Fit::BASE;
+    return ctas > 4ll * sms && !wide ? Fit::SHORT : Fit::THREE;
+}
 
 template <int D, int NT, Fit F>
 struct Q8Shape {
-    static constexpr int NW = NT == 2 ? (F == Fit::FAT ? 8 : 4) : F == Fit::FAT ? 12 : 6;
-    static constexpr int STAGES = (D == 64 ? 2 : 1) * (NT == 2 ? 3 : 2);
-    static constexpr int CTAS = F == Fit::FAT ? 1 : 2;
-    using Smem = Q8Smem<D, NW, STAGES>;
+    static constexpr int NW = shape_warps(F, NT == 2);
+    static constexpr int STAGES = D == 64 ? 4 : 2;
+    static constexpr int CTAS = shape_ctas(F);
+    using Smem = Q8Smem<D, NT, NW, STAGES>;
 };
 #define AC_Q8_KERNEL(D_, FMT_, NT_, F_)                                                                              \
     paged_decode_attn_q8_kernel<D_, FMT_, NT_, Q8Shape<D_, NT_, F_>::NW, Q8Shape<D_, NT_, F_>::STAGES,                \
@@ -615,9 +660,13 @@ cudaError_t launch_q8_shape(const CUtensorMap& k_map, const CUtensorMap& v_map, 
 
 template <int D, int FMT, int NT>
 cudaError_t launch_q8(const CUtensorMap& k_map, const CUtensorMap& v_map, const Q8AttnParams& p, int B, int sms, cudaStream_t stream) {
-    const long long ctas = static_cast<long long>(B) * p.Hkv * p.num_splits;
-    if (ctas <= sms) return launch_q8_shape<D, FMT, NT, Fit::FAT>(k_map, v_map, p, B, stream);
-    return launch_q8_shape<D, FMT, NT, Fit::BASE>(k_map, v_map, p, B, stream);
+    switch (fit_for(static_cast<long long>(B) * p.Hkv * p.num_splits, p.split_tokens, NT == 2, sms)) {
+        case Fit::FAT: return launch_q8_shape<D, FMT, NT, Fit::FAT>(k_map, v_map, p, B, stream);
+        case Fit::BASE: return launch_q8_shape<D, FMT, NT, Fit::BASE>(k_map, v_map, p, B, stream);
+        case Fit::SHORT:
+            if constexpr (NT == 1) return launch_q8_shape<D, FMT, NT, Fit::SHORT>(k_map, v_map, p, B, stream);
+        default: return launch_q8_shape<D, FMT, NT, Fit::THREE>(k_map, v_map, p, B, stream);
+    }
 }
 
 template <int D, int FMT, int NT, Fit F>
@@ -631,6 +680,10 @@ template <int D, int FMT, int NT>
 cudaError_t set_q8(int smem_optin) {
     cudaError_t e = set_q8_shape<D, FMT, NT, Fit::FAT>(smem_optin);
     if (e == cudaSuccess) e = set_q8_shape<D, FMT, NT, Fit::BASE>(smem_optin);
+    if (e == cudaSuccess) e = set_q8_shape<D, FMT, NT, Fit::THREE>(smem_optin);
+    if constexpr (NT == 1) {
+        if (e == cudaSuccess) e = set_q8_shape<D, FMT, NT, Fit::SHORT>(smem_optin);
+    }
     return e;
 }
 
@@ -646,6 +699,12 @@ cudaError_t q8_attn_set_attributes(int smem_optin) {
     if (e == cudaSuccess) e = set_q8<64, Q8_E4M3, 1>(smem_optin);
     if (e == cudaSuccess) e = set_q8<64, Q8_E4M3, 2>(smem_optin);
     return e;
+}
+
+void q8_attn_shape(long long ctas, int split_tokens, bool wide, int sms, int* warps, int* per_sm) {
+    const Fit f = fit_for(ctas, split_tokens, wide, sms);
+    *warps = shape_warps(f, wide);
+    *per_sm = shape_ctas(f);
 }
 
 int q8_attn_box(int page_size) { return page_size % TILE == 0 ? TILE : GRAN; }
