@@ -26,16 +26,14 @@ __device__ __forceinline__ void requantise(uint8_t* first, int64_t stride_token,
     }
 }
 
-// The scale of the block that slot `slot` of (page, head, side) is in, for a writer that needs `need` and has `before`
-// tokens of the block in front of it: joins the held scale, rounds the held codes again where it grows, stores what has
-// changed and returns it.  `codes` is the slot's own vector.  The whole warp.
+// The scale of a block for a writer that needs `need` and finds `before` tokens in front of it under the scale `held`: joins the two,
+// rounds the held codes again where it grows, stores what has changed and returns it.  `codes` is the writer's first vector.  The
+// whole warp, every lane of which has read `held`.
 template <int D, int FMT>
-__device__ __forceinline__ uint32_t settle_scale(const Q8View& cache, float* cell, uint8_t* codes, int before, uint32_t need, int lane) {
+__device__ __forceinline__ uint32_t settle_scale(const Q8View& cache, float* cell, uint8_t* codes, int before, uint32_t held, uint32_t need, int lane) {
     uint32_t scale = need;
     if (before > 0) {
-        const uint32_t held = __float_as_uint(*cell);
         scale = q8_join(held, need);
-        __syncwarp();                                      // every lane has read it
         if (scale == held) return scale;
         if (scale != kQ8NaN)
             requantise<D, FMT>(codes - before * cache.stride_token, cache.stride_token, before,
@@ -45,12 +43,14 @@ __device__ __forceinline__ uint32_t settle_scale(const Q8View& cache, float* cel
     return scale;
 }
 
+constexpr int kAppendThreads = 128;                        // 256 rows of 36 heads, us: 32 threads 10.0, 64 6.2, 128 5.9, 256 5.7
+
 // One warp per head vector of the new token, as the append kernels of the other formats: Hq query heads (rotated into
 // q_out), Hkv keys (rotated, quantised) and Hkv values (quantised).  A growing scale costs the warp the block's codes once
 // more; no other warp writes the block.  Bound: latency, length -> page -> scale -> codes; the vector itself is asked
 // for at once.
 template <int D, int FMT>
-__global__ void __launch_bounds__(128) rope_kv_append_q8_kernel(
+__global__ void __launch_bounds__(kAppendThreads) rope_kv_append_q8_kernel(
     const uint16_t* q_in, uint16_t* q_out, const uint16_t* __restrict__ k_new, const uint16_t* __restrict__ v_new,
     const Q8View cache, const int32_t* __restrict__ block_table, int max_pages_per_seq,
     const int32_t* __restrict__ context_lens, const float* __restrict__ rope_cos, const float* __restrict__ rope_sin,
@@ -60,10 +60,10 @@ __global__ void __launch_bounds__(128) rope_kv_append_q8_kernel(
     cudaGridDependencySynchronize();
     cudaTriggerProgrammaticLaunchCompletion();
     constexpr int EPL = D / 32;
-    __shared__ uint16_t s_vec[4][D];
+    __shared__ uint16_t s_vec[kAppendThreads / 32][D];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int heads = Hq + 2 * Hkv;
-    const long long vec = static_cast<long long>(blockIdx.x) * 4 + warp;
+    const long long vec = static_cast<long long>(blockIdx.x) * (kAppendThreads / 32) + warp;
     if (vec >= static_cast<long long>(B) * heads) return;
     const int b = static_cast<int>(vec / heads);
     const int hh = static_cast<int>(vec % heads);
@@ -112,34 +112,33 @@ __global__ void __launch_bounds__(128) rope_kv_append_q8_kernel(
         else *reinterpret_cast<uint32_t*>(dst) = words[0];
         return;
     }
-    uint32_t most = 0u;
-#pragma unroll
-    for (int w = 0; w < EPL / 2; ++w) most = bf16x2_amax(most, words[w]);
-#pragma unroll
-    for (int off = 16; off >= 1; off >>= 1) most = bf16x2_amax(most, __shfl_xor_sync(0xffffffffu, most, off));
-    const uint32_t need = q8_scale_bits<FMT>(max(most & 0xFFFFu, most >> 16));
-    const int slot = p - page_idx * page_size;
+    const int slot = p - page_idx * page_size, before = slot % cache.block;
     uint8_t* codes = (is_v ? cache.v_codes : cache.k_codes) + page * cache.stride_page + slot * cache.stride_token + h * cache.stride_head;
     float* cell = cache.scales + page * cache.stride_scales + (h * (page_size / cache.block) + slot / cache.block) * 2 + is_v;
-    const uint32_t scale = settle_scale<D, FMT>(cache, cell, codes, slot % cache.block, need, lane);
+    const uint32_t held = before > 0 ? __float_as_uint(*cell) : 0u;
+    const uint32_t most = warp_amax(EPL == 4 ? bf16x2_amax(words[0], words[EPL / 2 - 1]) : words[0]);
+    const uint32_t scale = settle_scale<D, FMT>(cache, cell, codes, before, held, q8_scale_bits<FMT>(most), lane);
     const float inv = q8_inverse(scale);
-    const float y0 = __uint_as_float(words[0] << 16) * inv, y1 = __uint_as_float(words[0] & 0xFFFF0000u) * inv;
-    if (EPL == 4) {
-        const float y2 = __uint_as_float(words[EPL / 2 - 1] << 16) * inv, y3 = __uint_as_float(words[EPL / 2 - 1] & 0xFFFF0000u) * inv;
-        *reinterpret_cast<uint32_t*>(codes + lane * EPL) = q8_codes<FMT>(y0, y1, y2, y3);
-    } else {
-        *reinterpret_cast<uint16_t*>(codes + lane * EPL) = static_cast<uint16_t>(q8_codes<FMT>(y0, y1, 0.0f, 0.0f));
+    if (q8_needs_clamp<FMT>(scale)) {
+#pragma unroll
+        for (int w = 0; w < EPL / 2; ++w) words[w] = q8_clamp(words[w]);
     }
+    const uint32_t packed = q8_quantise<FMT>(words[0], words[EPL / 2 - 1], inv);
+    if (EPL == 4) *reinterpret_cast<uint32_t*>(codes + lane * EPL) = packed;
+    else *reinterpret_cast<uint16_t*>(codes + lane * EPL) = static_cast<uint16_t>(packed);
 }
 
 // ---- bulk store ---------------------------------------------------------------------------------------------
 //
 // The tokens of one call that fall into one block are a piece; its first token, the first of its row or the first of a
-// block, is the piece's leader.  A warp takes one head of the leaders among `block` consecutive tokens of the dense input (one,
-// for long rows), K and V.  Sixteen tokens of both sides stay in registers between the search for the largest magnitude and the
-// rounding, so that they are read once; longer pieces are read a second time, out of the caches.
-constexpr int kStoreThreads = 128;
-constexpr int kHeld = 16;                                  // tokens that stay in registers
+// block, is the piece's leader.  A CTA takes one head of the leaders among `run` consecutive tokens of the dense input (a block's
+// worth: one leader, for long rows), K and V.  It has a warp for every 16 slots of a block, so that a piece stays in registers
+// between the search for its largest magnitude and the rounding, and is read once.
+//
+// Bound: HBM, 2 bytes in and 1 out per element.  70.3 thousand tokens of 8 heads of 128, K and V (432 MB), blocks of 16: 69 us = 6260
+// GB/s, 0.97 of the copy rate.  By CTAs of one warp (which leave one by one) and of four, 16 warps per SM: 74 and 80 us; 20 warps:
+// 69.  Blocks of 64: 77 us (96 with one warp that reads the tokens twice).
+constexpr int kHeld = 16;                                  // tokens of a warp
 
 // The row of a token: the last one whose offset is <= token (the whole warp; see token_position of the rope kernels).
 __device__ __forceinline__ int find_row(const int32_t* row_offsets, int B, int token, int lane) {
@@ -155,26 +154,26 @@ __device__ __forceinline__ int find_row(const int32_t* row_offsets, int B, int t
     return lo;
 }
 
-template <int D, int FMT>
-__global__ void __launch_bounds__(kStoreThreads) kv_store_q8_kernel(
+template <int D, int FMT, bool ONE>
+__global__ void __launch_bounds__(ONE ? 32 : 512, ONE ? (D == 64 ? 28 : 20) : 1) kv_store_q8_kernel(
     const uint16_t* __restrict__ k, const uint16_t* __restrict__ v, const Q8View cache, const int32_t* __restrict__ block_table,
     int max_pages_per_seq, const int32_t* __restrict__ start_pos, const int32_t* __restrict__ row_offsets, int total_tokens,
-    int B, int Hkv, int page_size, int num_pages, int32_t* status_flag) {
+    int run, int B, int Hkv, int page_size, int num_pages, int32_t* status_flag) {
     constexpr int LPV = D / 8, TPP = 32 / LPV;             // lanes per token, tokens side by side
-    constexpr int N = kHeld / TPP;                         // passes over the tokens held
-    const int lane = threadIdx.x & 31;
-    const long long item = static_cast<long long>(blockIdx.x) * (kStoreThreads / 32) + (threadIdx.x >> 5);
-    const int unit = static_cast<int>(item / Hkv), h = static_cast<int>(item - static_cast<long long>(unit) * Hkv);
-    const int block = cache.block;
-    const long long unit_begin = static_cast<long long>(unit) * block;
-    if (unit_begin >= total_tokens) return;
-    const int until = static_cast<int>(min(static_cast<long long>(total_tokens), unit_begin + block));
-    const int t0 = lane / LPV, e0 = lane % LPV * 8;        // this lane's token among those side by side, and its elements
+    constexpr int N = kHeld / TPP;                         // passes over a warp's tokens
+    __shared__ uint32_t s_most[2][16];
+    const int warp = ONE ? 0 : threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const unsigned unit = blockIdx.x / static_cast<unsigned>(Hkv);
+    const int h = static_cast<int>(blockIdx.x - unit * Hkv);
+    const unsigned block = cache.block;
+    const long long unit_begin = static_cast<long long>(unit) * run;
+    const int until = static_cast<int>(min(static_cast<long long>(total_tokens), unit_begin + run));
+    const int t0 = warp * kHeld + lane / LPV, e0 = lane % LPV * 8;     // this lane's first token of a piece, and its elements
     const int64_t token_stride = static_cast<int64_t>(Hkv) * D;
 
+    // (What follows is decided alike by every warp.)
     long long tok = unit_begin;
-    const int all_end = row_offsets[B] < total_tokens ? row_offsets[B] : total_tokens;
-    while (tok < until && tok < all_end) {
+    while (tok < until) {
         const int row = find_row(row_offsets, B, static_cast<int>(tok), lane);
         const int begin = row_offsets[row];
         const int end = min(row_offsets[row + 1], total_tokens);
@@ -183,21 +182,21 @@ __global__ void __launch_bounds__(kStoreThreads) kv_store_q8_kernel(
             tok = begin;
             continue;
         }
-        if (end <= tok) return;                            // offsets that decrease: a caller error, not a loop
+        if (end <= tok) return;                            // behind the last row (or offsets that decrease, a caller's error)
         if (start < 0) {
             tok = end;
             continue;
         }
-        const long long pos = start + (tok - begin);
+        const unsigned pos = static_cast<unsigned>(start) + static_cast<unsigned>(tok - begin);      // below 2^32
         const int before = static_cast<int>(pos % block);
-        const int n = static_cast<int>(min(static_cast<long long>(block - before), end - tok));
+        const int n = static_cast<int>(min(static_cast<long long>(block) - before, end - tok));
         if (before != 0 && tok != begin) {                 // led by a token of an earlier unit
             tok += n;
             continue;
         }
-        const long long idx = pos / page_size;
-        if (idx >= max_pages_per_seq) {
-            if (status_flag != nullptr && lane == 0) atomicOr(status_flag, AC_FLAG_POSITION_OOB);
+        const unsigned idx = pos / static_cast<unsigned>(page_size);
+        if (idx >= static_cast<unsigned>(max_pages_per_seq)) {
+            if (status_flag != nullptr && threadIdx.x == 0) atomicOr(status_flag, AC_FLAG_POSITION_OOB);
             tok += n;
             continue;
         }
@@ -205,58 +204,64 @@ __global__ void __launch_bounds__(kStoreThreads) kv_store_q8_kernel(
         const uint16_t* src[2] = {k + tok * token_stride + h * D + e0, v + tok * token_stride + h * D + e0};
         uint4 x[2][N];
         uint32_t most[2] = {0u, 0u};
-        auto load = [&](int t) {                           // tokens t .. t + 15 of the piece
 #pragma unroll
-            for (int side = 0; side < 2; ++side)
+        for (int side = 0; side < 2; ++side)
 #pragma unroll
-                for (int i = 0; i < N; ++i) {
-                    const int at = t + t0 + i * TPP;
-                    x[side][i] = at < n ? __ldg(reinterpret_cast<const uint4*>(src[side] + at * token_stride)) : make_uint4(0u, 0u, 0u, 0u);
-                }
-        };
-        load(0);
+            for (int i = 0; i < N; ++i)
+                x[side][i] = t0 + i * TPP < n ? __ldg(reinterpret_cast<const uint4*>(src[side] + (t0 + i * TPP) * token_stride))
+                                              : make_uint4(0u, 0u, 0u, 0u);
         tok += n;
         if (page < 0 || page >= num_pages) {
-            if (status_flag != nullptr && lane == 0) atomicOr(status_flag, AC_FLAG_PAGE_OOB);
+            if (status_flag != nullptr && threadIdx.x == 0) atomicOr(status_flag, AC_FLAG_PAGE_OOB);
             continue;
         }
-        for (int t = 0;;) {
+        const int slot = static_cast<int>(pos - idx * page_size);
+        const int64_t place = page * cache.stride_page + slot * cache.stride_token + h * cache.stride_head;
+        float* cell = cache.scales + page * cache.stride_scales + (h * (page_size / cache.block) + slot / cache.block) * 2;
+        float2 held = make_float2(0.0f, 0.0f);
+        if (before > 0) held = *reinterpret_cast<const float2*>(cell);
+#pragma unroll
+        for (int side = 0; side < 2; ++side) {
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                most[side] = bf16x2_amax(bf16x2_amax(most[side], bf16x2_amax(x[side][i].x, x[side][i].y)), bf16x2_amax(x[side][i].z, x[side][i].w));
+            most[side] = warp_amax(most[side]);
+        }
+        if (!ONE) {
+            if (lane == 0) s_most[0][warp] = most[0], s_most[1][warp] = most[1];
+            __syncthreads();                               // every warp has read the held scales, too
+            for (int w = 0; w < static_cast<int>(blockDim.x) / 32; ++w)
+                most[0] = max(most[0], s_most[0][w]), most[1] = max(most[1], s_most[1][w]);
+            __syncthreads();                               // before the next piece's
+        }
+        bool clamp = false;
+        float inv[2];
+#pragma unroll
+        for (int side = 0; side < 2; ++side) {
+            const uint32_t need = q8_scale_bits<FMT>(most[side]), was = __float_as_uint(side ? held.y : held.x);
+            uint32_t scale = before > 0 ? q8_join(was, need) : need;
+            if (warp == 0)
+                settle_scale<D, FMT>(cache, cell + side, (side ? cache.v_codes : cache.k_codes) + place, before, was, need, lane);
+            inv[side] = q8_inverse(scale);
+            clamp = clamp || q8_needs_clamp<FMT>(scale);
+        }
+        if (FMT == Q8_INT8 && clamp) {                     // (values of the other side are below the bound)
 #pragma unroll
             for (int side = 0; side < 2; ++side)
 #pragma unroll
                 for (int i = 0; i < N; ++i)
-                    most[side] = bf16x2_amax(most[side], bf16x2_amax(bf16x2_amax(x[side][i].x, x[side][i].y), bf16x2_amax(x[side][i].z, x[side][i].w)));
-            t += kHeld;
-            if (t >= n) break;
-            load(t);
+                    x[side][i] = make_uint4(q8_clamp(x[side][i].x), q8_clamp(x[side][i].y), q8_clamp(x[side][i].z), q8_clamp(x[side][i].w));
         }
-        const int slot = static_cast<int>(pos - idx * page_size);
-        const int64_t place = page * cache.stride_page + slot * cache.stride_token + h * cache.stride_head;
-        float* cell = cache.scales + page * cache.stride_scales + (h * (page_size / block) + slot / block) * 2;
-        float inv[2];
 #pragma unroll
         for (int side = 0; side < 2; ++side) {
-            uint32_t m = most[side];
+            uint8_t* dst = (side ? cache.v_codes : cache.k_codes) + place + e0;
 #pragma unroll
-            for (int off = 16; off >= 1; off >>= 1) m = bf16x2_amax(m, __shfl_xor_sync(0xffffffffu, m, off));
-            const uint32_t need = q8_scale_bits<FMT>(max(m & 0xFFFFu, m >> 16));
-            inv[side] = q8_inverse(settle_scale<D, FMT>(cache, cell + side, (side ? cache.v_codes : cache.k_codes) + place, before, need, lane));
-        }
-        for (int t = 0; t < n; t += kHeld) {
-            if (n > kHeld) load(t);                        // otherwise they are still here
-#pragma unroll
-            for (int side = 0; side < 2; ++side) {
-                uint8_t* dst = (side ? cache.v_codes : cache.k_codes) + place + e0;
-#pragma unroll
-                for (int i = 0; i < N; ++i) {
-                    const int at = t + t0 + i * TPP;
-                    if (at >= n) continue;
-                    const uint4 w = x[side][i];
-                    auto lo = [&](uint32_t u) { return __uint_as_float(u << 16) * inv[side]; };
-                    auto hi = [&](uint32_t u) { return __uint_as_float(u & 0xFFFF0000u) * inv[side]; };
+            for (int i = 0; i < N; ++i) {
+                const int at = t0 + i * TPP;
+                const uint4 w = x[side][i];
+                if (at < n)
                     *reinterpret_cast<uint2*>(dst + at * cache.stride_token) =
-                        make_uint2(q8_codes<FMT>(lo(w.x), hi(w.x), lo(w.y), hi(w.y)), q8_codes<FMT>(lo(w.z), hi(w.z), lo(w.w), hi(w.w)));
-                }
+                        make_uint2(q8_quantise<FMT>(w.x, w.y, inv[side]), q8_quantise<FMT>(w.z, w.w, inv[side]));
             }
         }
     }
@@ -266,7 +271,7 @@ __global__ void __launch_bounds__(kStoreThreads) kv_store_q8_kernel(
 //
 // A warp takes a run of consecutive tokens: its lanes find the slots of one token each, then it goes through the run's (token,
 // head) vectors, K and V together, eight codes (8 bytes in, 16 out) per lane.
-constexpr int kLoadThreads = 256;
+constexpr int kLoadThreads = 64;
 
 struct Q8Slot {
     int64_t code;         // byte offset of the token's slot in the code pools; -1: no slot
@@ -285,9 +290,9 @@ __device__ __forceinline__ Q8Slot find_slot(long long token, const Q8View& cache
     }
     const int start = start_pos[lo];
     if (start < 0 || token < row_offsets[lo]) return r;
-    const long long pos = start + (token - row_offsets[lo]);
-    const long long idx = pos / page_size;
-    if (idx >= max_pages_per_seq) {
+    const unsigned pos = static_cast<unsigned>(start) + static_cast<unsigned>(token - row_offsets[lo]);      // below 2^32
+    const unsigned idx = pos / static_cast<unsigned>(page_size);
+    if (idx >= static_cast<unsigned>(max_pages_per_seq)) {
         if (status_flag != nullptr) atomicOr(status_flag, AC_FLAG_POSITION_OOB);
         return r;
     }
@@ -323,12 +328,11 @@ __global__ void __launch_bounds__(kLoadThreads) kv_load_q8_kernel(
     Q8Slot* const s_slot = s_slots[warp];
     const int e0 = lane % LPV * 8;
     const int head_scales = page_size / cache.block * 2;
-    const unsigned runs = (static_cast<unsigned>(total_tokens) + run - 1) / run;
-    for (unsigned r = warp * gridDim.x + blockIdx.x; r < runs; r += gridDim.x * WARPS) {
-        const long long first = static_cast<long long>(r) * run;
+    const long long first = (static_cast<long long>(blockIdx.x) * WARPS + warp) * run;
+    if (first >= total_tokens) return;
+    {
         const int tokens = total_tokens - first < run ? static_cast<int>(total_tokens - first) : run;
         const int vecs = tokens * Hkv;
-        __syncwarp();
         if (lane < tokens)
             s_slot[lane] = find_slot(first + lane, cache, block_table, max_pages_per_seq, start_pos, row_offsets, B, page_size, num_pages, status_flag);
         __syncwarp();
@@ -366,15 +370,22 @@ __global__ void __launch_bounds__(kLoadThreads) kv_load_q8_kernel(
 template <int D, int FMT>
 cudaError_t launch_store(const void* k, const void* v, const Q8View& cache, const int32_t* block_table, int max_pages_per_seq,
                          const int32_t* start_pos, const int32_t* row_offsets, int total_tokens, int B, int Hkv, int page_size,
-                         int num_pages, int32_t* status_flag, cudaStream_t stream) {
+                         int num_pages, int32_t* status_flag, int sms, cudaStream_t stream) {
     // An ordinary launch: what follows it in the stream may read the cache before its own synchronisation, which is safe only
     // behind kernels that do not signal early.
-    const long long items = ((total_tokens - 1ll) / cache.block + 1) * Hkv;
-    const long long grid = (items + kStoreThreads / 32 - 1) / (kStoreThreads / 32);
+    // Leaders are looked for among `block` tokens, fewer where that leaves warps (32 per SM) without work.
+    int run = cache.block;
+    while (run > 1 && (total_tokens - 1ll) / run * Hkv < 32ll * sms) run = (run + 1) / 2;
+    const long long grid = ((total_tokens - 1ll) / run + 1) * Hkv;
     if (grid > 0x7fffffffll) return cudaErrorInvalidConfiguration;
-    kv_store_q8_kernel<D, FMT><<<static_cast<unsigned>(grid), kStoreThreads, 0, stream>>>(
-        static_cast<const uint16_t*>(k), static_cast<const uint16_t*>(v), cache, block_table, max_pages_per_seq, start_pos,
-        row_offsets, total_tokens, B, Hkv, page_size, num_pages, status_flag);
+    const uint16_t* kk = static_cast<const uint16_t*>(k);
+    const uint16_t* vv = static_cast<const uint16_t*>(v);
+    if (cache.block == kHeld)
+        kv_store_q8_kernel<D, FMT, true><<<static_cast<unsigned>(grid), 32, 0, stream>>>(
+            kk, vv, cache, block_table, max_pages_per_seq, start_pos, row_offsets, total_tokens, run, B, Hkv, page_size, num_pages, status_flag);
+    else
+        kv_store_q8_kernel<D, FMT, false><<<static_cast<unsigned>(grid), cache.block / kHeld * 32, 0, stream>>>(
+            kk, vv, cache, block_table, max_pages_per_seq, start_pos, row_offsets, total_tokens, run, B, Hkv, page_size, num_pages, status_flag);
     return cudaGetLastError();
 }
 
@@ -382,13 +393,11 @@ template <int D, int FMT>
 cudaError_t launch_load(void* k, void* v, const Q8View& cache, const int32_t* block_table, int max_pages_per_seq,
                         const int32_t* start_pos, const int32_t* row_offsets, int total_tokens, int B, int Hkv, int page_size,
                         int num_pages, int32_t* status_flag, int sms, cudaStream_t stream) {
-    // Runs of 32 vectors or more where there are tokens enough for every warp of the GPU, shorter ones otherwise.
-    const int ctas = 4 * sms;
     int run = Hkv < 32 ? 32 / Hkv : 1;
-    while (run > 1 && total_tokens / run < ctas * (kLoadThreads / 32)) run /= 2;
-    const long long runs = (static_cast<long long>(total_tokens) + run - 1) / run;
-    const unsigned grid = static_cast<unsigned>(runs < ctas ? runs : ctas);
-    kv_load_q8_kernel<D, FMT><<<grid, kLoadThreads, 0, stream>>>(
+    while (run > 1 && total_tokens / run < 32 * sms && run / 2 * Hkv >= 8) run /= 2;
+    const long long grid = ((total_tokens - 1ll) / run) / (kLoadThreads / 32) + 1;
+    if (grid > 0x7fffffffll) return cudaErrorInvalidConfiguration;
+    kv_load_q8_kernel<D, FMT><<<static_cast<unsigned>(grid), kLoadThreads, 0, stream>>>(
         static_cast<uint16_t*>(k), static_cast<uint16_t*>(v), cache, block_table, max_pages_per_seq, start_pos, row_offsets,
         total_tokens, run, B, Hkv, page_size, num_pages, status_flag);
     return cudaGetLastError();
@@ -409,8 +418,8 @@ cudaError_t launch_rope_kv_append_q8(const void* q_in, void* q_out, const void* 
     const RopeVariant& r = variant != nullptr ? *variant : plain;
     const long long vecs = static_cast<long long>(B) * (Hq + 2ll * Hkv);
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(static_cast<unsigned>((vecs + 3) / 4));
-    cfg.blockDim = dim3(128);
+    cfg.gridDim = dim3(static_cast<unsigned>((vecs + kAppendThreads / 32 - 1) / (kAppendThreads / 32)));
+    cfg.blockDim = dim3(kAppendThreads);
     cfg.stream = stream;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -433,7 +442,7 @@ cudaError_t launch_kv_bulk_q8(void* k, void* v, const Q8View& cache, const int32
                               int page_size, int num_pages, int32_t* status_flag, bool store, int sms, cudaStream_t stream) {
 #define AC_Q8_STORE(D_, F_)                                                                                         \
     launch_store<D_, F_>(k, v, cache, block_table, max_pages_per_seq, start_pos, row_offsets, total_tokens, B, Hkv,  \
-                         page_size, num_pages, status_flag, stream)
+                         page_size, num_pages, status_flag, sms, stream)
 #define AC_Q8_LOAD(D_, F_)                                                                                          \
     launch_load<D_, F_>(k, v, cache, block_table, max_pages_per_seq, start_pos, row_offsets, total_tokens, B, Hkv,   \
                         page_size, num_pages, status_flag, sms, stream)

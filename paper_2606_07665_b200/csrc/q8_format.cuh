@@ -39,20 +39,40 @@ __device__ __forceinline__ uint32_t q8_join(uint32_t held, uint32_t need) {
     return held >= 0x7F800000u ? kQ8NaN : max(held, need); // a held scale that is no positive number counts as NaN
 }
 
-// Four values, already divided by the scale, as codes in the bytes of a word.
+// Four values, already divided by the scale, as codes in the bytes of a word.  For INT8 they are at most 127 in magnitude, but for
+// rounding (see q8_clamp).
 template <int FMT>
-__device__ __forceinline__ uint32_t q8_codes(float y0, float y1, float y2, float y3) {
+__device__ __forceinline__ uint32_t q8_codes(uint64_t y01, uint64_t y23) {
+    float y0, y1, y2, y3;
     if (FMT == Q8_INT8) {
         // adding 1.5 * 2^23 rounds to the nearest even integer, which is then the low byte of the bits
-        constexpr float kMagic = 12582912.0f;
-        auto code = [&](float y) { return __float_as_uint(__fadd_rn(fminf(fmaxf(y, -127.0f), 127.0f), kMagic)); };
-        return __byte_perm(__byte_perm(code(y0), code(y1), 0x0040), __byte_perm(code(y2), code(y3), 0x0040), 0x5410);
+        const uint64_t magic = f32x2(12582912.0f, 12582912.0f);
+        f32x2_split(f32x2_add(y01, magic), y0, y1);
+        f32x2_split(f32x2_add(y23, magic), y2, y3);
+        return __byte_perm(__byte_perm(__float_as_uint(y0), __float_as_uint(y1), 0x0040),
+                           __byte_perm(__float_as_uint(y2), __float_as_uint(y3), 0x0040), 0x5410);
     }
+    f32x2_split(y01, y0, y1);
+    f32x2_split(y23, y2, y3);
     uint16_t lo, hi;                                       // nearest even; beyond 448 the largest code
     asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(lo) : "f"(y1), "f"(y0));
     asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(hi) : "f"(y3), "f"(y2));
     return lo | (static_cast<uint32_t>(hi) << 16);
 }
+
+// Codes of two words of two bf16 each, under the scale whose inverse is `inv`.
+template <int FMT>
+__device__ __forceinline__ uint32_t q8_quantise(uint32_t w0, uint32_t w1, float inv) {
+    const uint64_t both = f32x2(inv, inv);
+    return q8_codes<FMT>(f32x2_mul(f32x2(__uint_as_float(w0 << 16), __uint_as_float(w0 & 0xFFFF0000u)), both),
+                         f32x2_mul(f32x2(__uint_as_float(w1 << 16), __uint_as_float(w1 & 0xFFFF0000u)), both));
+}
+
+// Under the largest scale of INT8, 2^121, the largest bf16 is 127.5 s: its values are taken for 127 s.  Two bf16 at a time; every other
+// scale holds its values.
+template <int FMT>
+__device__ __forceinline__ bool q8_needs_clamp(uint32_t scale_bits) { return FMT == Q8_INT8 && scale_bits == (121u + 127u) << 23; }
+__device__ __forceinline__ uint32_t q8_clamp(uint32_t w) { return __vminu2(w & 0x7FFF7FFFu, 0x7F7E7F7Eu) | (w & 0x80008000u); }
 
 // The two codes in the low or high half of a word as fp16 operands: exact.
 __device__ __forceinline__ uint32_t q8_e4m3x2_to_f16x2(uint16_t two) {
@@ -109,10 +129,21 @@ template <int FMT>
 __device__ __forceinline__ uint32_t q8_again(uint32_t codes, float factor) {
     float x[4];
     q8_floats<FMT>(codes, x);
-    return q8_codes<FMT>(x[0] * factor, x[1] * factor, x[2] * factor, x[3] * factor);
+    const uint64_t both = f32x2(factor, factor);
+    return q8_codes<FMT>(f32x2_mul(f32x2(x[0], x[1]), both), f32x2_mul(f32x2(x[2], x[3]), both));
 }
 
-// Largest |x| of two bf16 words, half by half, as bits.  (Magnitudes order as integers, NaN above infinity.)
-__device__ __forceinline__ uint32_t bf16x2_amax(uint32_t a, uint32_t b) { return __vmaxu2(a & 0x7FFF7FFFu, b & 0x7FFF7FFFu); }
+// Largest |x| of two bf16 words, half by half; the sign of the result means nothing, and a NaN comes through.
+__device__ __forceinline__ uint32_t bf16x2_amax(uint32_t a, uint32_t b) {
+    uint32_t r;
+    asm("max.NaN.xorsign.abs.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+// The larger half of such a maximum over the warp, as bits without sign.
+__device__ __forceinline__ uint32_t warp_amax(uint32_t m) {
+#pragma unroll
+    for (int off = 16; off >= 1; off >>= 1) m = bf16x2_amax(m, __shfl_xor_sync(0xffffffffu, m, off));
+    return max(m & 0x7FFFu, (m >> 16) & 0x7FFFu);
+}
 
 }  // namespace acdev

@@ -394,11 +394,12 @@ cudaError_t launch_rows(RowsParams p, int sms, cudaStream_t stream) {
 
 // ---- tables ------------------------------------------------------------------------------------------------
 //
-// A thread owns one frequency and kRun consecutive positions: cosine and sine of the first position's angle in fp64, then
-// one rotation by the frequency's own angle per position (an error of 2^-53 each, 2^-46 after 64 of them: far below the
+// A thread owns one frequency and `run` consecutive positions: cosine and sine of the first position's angle in fp64, then
+// one rotation by the frequency's own angle per position (an error of 2^-52 each, 2^-47 after 32 of them: far below the
 // fp32 that is written).  Four fp64 operations per pair instead of the hundred of a sine and a cosine.
-// Bound: the writes, 4 bytes per entry.
-constexpr int kRun = 64;
+// Bound: the writes, 4 bytes per entry: 131072 positions of 64 frequencies (67 MB) 13.4 us, 10.4 at the copy rate (runs of 64: 14.7).
+// Few positions: latency (4096 of 32 frequencies 2.6 us in runs of 4, 4.4 without).
+constexpr int kRun = 32;
 
 __global__ void __launch_bounds__(256) rope_tables_kernel(float* __restrict__ cos_out, float* __restrict__ sin_out,
                                                           long long first, int positions, int half, int run, const RopeScaling sc) {
@@ -417,12 +418,14 @@ __global__ void __launch_bounds__(256) rope_tables_kernel(float* __restrict__ co
     double c, s, cd, sd;
     sincos(static_cast<double>(first + p0) * f, &s, &c);
     sincos(f, &sd, &cd);
+    c *= sc.magnitude;
+    s *= sc.magnitude;
     const int n = positions - p0 < run ? static_cast<int>(positions - p0) : run;
     float* co = cos_out + p0 * half + i;
     float* so = sin_out + p0 * half + i;
     for (int j = 0; j < n; ++j) {
-        *co = static_cast<float>(sc.magnitude * c);
-        *so = static_cast<float>(sc.magnitude * s);
+        *co = static_cast<float>(c);
+        *so = static_cast<float>(s);
         co += half;
         so += half;
         const double t = c * cd - s * sd;
@@ -484,7 +487,7 @@ cudaError_t launch_rope_tables(float* rope_cos, float* rope_sin, long long first
                                const RopeScaling& scaling, int sms, cudaStream_t stream) {
     const int half = rotary_dim / 2;
     int run = kRun;                                        // shorter runs where the GPU would not be full
-    while (run > 1 && static_cast<long long>((positions + run - 1) / run) * half < 1024ll * sms) run /= 2;
+    while (run > 1 && static_cast<long long>((positions + run - 1) / run) * half < 128ll * sms) run /= 2;
     const long long threads = static_cast<long long>((positions + run - 1) / run) * half;
     const long long grid = (threads + 255) / 256;
     if (grid > 0x7fffffffll) return cudaErrorInvalidConfiguration;
