@@ -180,7 +180,8 @@ __global__ void __launch_bounds__(128) rope_rows_kernel(const RowsParams p) {
 // registers and loads run ahead of the arithmetic by as many pieces as there are stages.  The positions of the next 32 pieces are
 // looked up at a time, one per lane.
 //
-// Bound: HBM, 2 bytes in and out per element.
+// Bound: HBM, 2 bytes in and out per element: 70.3 thousand tokens of 40 heads of 128 (1.44 GB) 232 us = 6210 GB/s, 0.96 of the
+// copy rate.  (Through registers, as above: 262 at best, 24 warps per SM.)
 constexpr int kPieceBytes = 4096, kAngleBytes = 256;       // at most, of a piece and of its cosines or sines
 // 70.3 thousand tokens of 40 heads of 128, us, by (warps per SM, stages): (8, 4) 279, (12, 3) 243, (12, 4) 233, (10, 5) 256, (13, 3)
 // 278, (16, 3) 265; pieces of 2 or 8 KB are slower.
