@@ -265,6 +265,14 @@ class AttentionBlockStep:
 # outlive them.
 
 _BF16 = (torch.bfloat16, torch.int16)          # bf16 values, or their bits
+_I32 = (torch.int32,)
+
+
+def _prepared(name, args):
+    """args of a call with the numbers among them as ctypes objects of the call's types, which the call then need not make (a
+    third of what marshalling costs); what changes from call to call is None here and filled in by the caller."""
+    types = getattr(ac.lib(), name).argtypes
+    return [t(a) if type(a) in (int, float) else a for t, a in zip(types, args)]
 
 
 def _want(t, name, shape, dtypes, device):
@@ -505,19 +513,27 @@ class _QuantisedCache(_OnDevice):
         self.k_codes, self.v_codes = k_codes, v_codes
         return k_codes.stride(0), k_codes.stride(token), k_codes.stride(head)
 
+    def _describe(self, struct):
+        self.struct = struct
+        self._bulk_args = _prepared("ac_kv_store_" + self._format, [None, None, struct, None, None, None, None, None, None, self.Hkv, self.d,
+                                                                    self.page_size, self.num_pages, self._flag, None])
+
     def _bulk(self, name, k, v, block_table, start_pos, row_offsets, stream):
         B = start_pos.shape[0]
         total = k.shape[0]
-        for t, what in ((k, "k"), (v, "v")):
-            _want(t, what, (total, self.Hkv, self.d), _BF16, self.device)
-        _want(start_pos, "start_pos", (B,), (torch.int32,), self.device)
-        _want(row_offsets, "row_offsets", (B + 1,), (torch.int32,), self.device)
-        _want(block_table, "block_table", (B, block_table.shape[-1]), (torch.int32,), self.device)
+        shape = (total, self.Hkv, self.d)
+        _want(k, "k", shape, _BF16, self.device)
+        _want(v, "v", shape, _BF16, self.device)
+        _want(start_pos, "start_pos", (B,), _I32, self.device)
+        _want(row_offsets, "row_offsets", (B + 1,), _I32, self.device)
+        width = block_table.shape[-1]
+        _want(block_table, "block_table", (B, width), _I32, self.device)
         if total == 0:
             return
-        self._enqueue(name, [k.data_ptr(), v.data_ptr(), self.struct, block_table.data_ptr(), block_table.shape[1],
-                             start_pos.data_ptr(), row_offsets.data_ptr(), total, B, self.Hkv, self.d, self.page_size,
-                             self.num_pages, self._flag, None], stream, -1)
+        args = self._bulk_args.copy()
+        args[:2] = k.data_ptr(), v.data_ptr()
+        args[3:9] = block_table.data_ptr(), width, start_pos.data_ptr(), row_offsets.data_ptr(), total, B
+        self._enqueue(name, args, stream, -1)
 
     def store(self, k, v, block_table, start_pos, row_offsets, stream=None):
         """Quantises k, v (bf16 [tokens, Hkv, d], keys rotated): row b's tokens row_offsets[b] .. row_offsets[b+1] - 1
@@ -556,7 +572,7 @@ class Q4Cache(_QuantisedCache):
         self.group = self.d // groups
         _want(params, "params", (self.num_pages, self.Hkv, self.page_size, 2, groups, 2), _BF16, self.device)
         self.params = params
-        self.struct = ac.q4_cache(k_codes, v_codes, params, *strides, self.group)
+        self._describe(ac.q4_cache(k_codes, v_codes, params, *strides, self.group))
 
     @classmethod
     def empty(cls, num_pages, page_size, Hkv, d, group=64, layout="token_major", device="cuda:0"):
@@ -589,8 +605,8 @@ class Q8Cache(_QuantisedCache):
 
     def __init__(self, k_codes, v_codes, scales, page_size=None, layout="token_major"):
         self._bind(k_codes.device)
-        if k_codes.dim() != 4 or scales.dim() != 4:
-            raise ValueError("codes and scales have 4 dimensions")
+        if k_codes.dim() != 4 or scales.dim() != 4 or not k_codes.shape[0] or not scales.shape[0]:
+            raise ValueError("codes and scales have 4 dimensions, and a page at least")
         strides = self._codes(k_codes, v_codes, page_size, layout, (torch.int8, torch.float8_e4m3fn))
         self.d, blocks = k_codes.shape[3], scales.shape[2]
         if blocks <= 0 or self.page_size % blocks:
@@ -605,7 +621,7 @@ class Q8Cache(_QuantisedCache):
             raise ValueError("scales: pages overlap")
         self.scales, self._apart = scales, apart
         fmt = ac.AC_Q8_INT8 if k_codes.dtype == torch.int8 else ac.AC_Q8_E4M3
-        self.struct = ac.q8_cache(k_codes, v_codes, scales, *strides, apart, self.block, fmt)
+        self._describe(ac.q8_cache(k_codes, v_codes, scales, *strides, apart, self.block, fmt))
 
     @classmethod
     def empty(cls, num_pages, page_size, Hkv, d, block=16, dtype=torch.float8_e4m3fn, layout="token_major", device="cuda:0"):
@@ -675,12 +691,14 @@ class _QuantisedStep(_Rows):
     def _marshal(self):
         shape = [self.B, self.Hq, self.Hkv, self.d, self.page_size, self.num_pages]
         table = [self.cache.struct, self.block_table.data_ptr(), self.max_pages_per_seq, self.context_lens.data_ptr()]
-        self._attn_args = [None, *table, self.new_tokens, self.softmax_scale, self.num_splits,
-                           self.workspace.data_ptr(), self.workspace_bytes, None, *shape, self.max_context_len,
-                           self._flag, None, self._options]
+        self._attn_call, self._append_call = ("ac_" + f + self.cache._format for f in ("paged_decode_attn_", "rope_kv_append_"))
+        self._attn_args = _prepared(self._attn_call, [None, *table, self.new_tokens, self.softmax_scale, self.num_splits,
+                                                      self.workspace.data_ptr(), self.workspace_bytes, None, *shape,
+                                                      self.max_context_len, self._flag, None, self._options])
         if self.rope_cos is not None:
-            self._append_args = [None, None, None, None, *table, self.rope_cos.data_ptr(), self.rope_sin.data_ptr(),
-                                 self.rope_cos.shape[0], *shape, self._flag, None, self._rope]
+            self._append_args = _prepared(self._append_call, [None, None, None, None, *table, self.rope_cos.data_ptr(),
+                                                              self.rope_sin.data_ptr(), self.rope_cos.shape[0], *shape,
+                                                              self._flag, None, self._rope])
 
     def append(self, q_in, k_new, v_new, q_out=None, stream=None):
         """Rotates q_in [B, Hq, d] into q_out (allocated unless given, may be q_in) and writes k_new, v_new
@@ -696,7 +714,7 @@ class _QuantisedStep(_Rows):
             _want(q_out, "q_out", self._q_shape, _BF16, self.device)
         args = self._append_args.copy()
         args[:4] = q_in.data_ptr(), q_out.data_ptr(), k_new.data_ptr(), v_new.data_ptr()
-        self._enqueue("ac_rope_kv_append_" + self.cache._format, args, stream, -2)
+        self._enqueue(self._append_call, args, stream, -2)
         return q_out
 
     def attention(self, q, out=None, stream=None):
@@ -708,7 +726,7 @@ class _QuantisedStep(_Rows):
             _want(out, "out", self._q_shape, _BF16, self.device)
         args = self._attn_args.copy()
         args[0], args[10] = q.data_ptr(), out.data_ptr()
-        self._enqueue("ac_paged_decode_attn_" + self.cache._format, args, stream, -2)
+        self._enqueue(self._attn_call, args, stream, -2)
         return out
 
     def step(self, q_in, k_new, v_new, q_rot=None, out=None, stream=None):
@@ -753,8 +771,9 @@ class Rope(_OnDevice):
             if t is not None:
                 _want(t, what, (t.shape[-1],), _BF16, self.device)
         self._head = next((t.shape[-1] for t in self._norms if t is not None), None)
-        self._tables = cos.data_ptr(), sin.data_ptr()
         self._options = ac._rope_options(self.rotary_dim, interleaved, q_norm_weight, k_norm_weight, norm_eps)
+        self._rows_args = _prepared("ac_rope_rows", [None] * 15 + [cos.data_ptr(), sin.data_ptr(), self.max_position, self._flag,
+                                                                   None, self._options])
 
     @classmethod
     def scaled(cls, max_position, rotary_dim, base=10000.0, scaling="none", factor=1.0, original=0.0, low=0.0, high=0.0,
@@ -766,6 +785,7 @@ class Rope(_OnDevice):
         rope = cls(cos, sin, **variants)
         rope._allocated = (cos, sin)
         rope.fill(0, base, scaling, factor, original, low, high, magnitude)
+        torch.cuda.current_stream(rope.device).synchronize()      # filled whatever stream the tables are read on
         return rope
 
     def _buffers(self):
@@ -778,52 +798,57 @@ class Rope(_OnDevice):
         turn less than ``low`` times in ``original`` positions / factor, more than ``high`` times as they are, blended between)."""
         if scaling not in self._KINDS:
             raise ValueError(f"scaling {scaling!r}, expected one of {', '.join(self._KINDS)}")
+        if magnitude == 0:
+            raise ValueError("magnitude 0")                # which the library takes for 1
         how = ac.rope_scaling(float(base), self._KINDS[scaling], float(factor), float(original), float(low), float(high),
                               float(magnitude))
         self._enqueue("ac_rope_tables", [self.cos.data_ptr(), self.sin.data_ptr(), int(first_position), self.max_position,
                                          self.rotary_dim, how, None], stream, -1)
 
-    def _tokens(self, t, name, shape):
+    def _tokens(self, t, name, shape, heads, d):
         """t is bf16 of this shape [tokens, heads, d] with dense heads; returns the elements from one token to the next."""
-        if isinstance(t, torch.Tensor) and t.shape == shape and t.dtype in _BF16 and t.device == self.device:
-            apart, head, element = t.stride()
-            if element == 1 and (head == shape[2] or shape[1] == 1):
-                return apart if shape[0] > 1 else max(8, shape[1] * shape[2])
-            raise ValueError(f"{name}: heads of a token are not contiguous")
-        if not isinstance(t, torch.Tensor):
-            raise TypeError(f"{name}: {type(t).__name__}, expected a tensor")
+        try:
+            if t.shape == shape and t.dtype in _BF16 and t.device == self.device:
+                apart, head, element = t.stride()
+                if element == 1 and (head == d or heads == 1):
+                    return apart if shape[0] > 1 else max(8, heads * d)
+                raise ValueError(f"{name}: heads of a token are not contiguous")
+        except AttributeError:
+            raise TypeError(f"{name}: {type(t).__name__}, expected a tensor") from None
         raise ValueError(f"{name}: {t.dtype} {tuple(t.shape)} on {t.device}, expected bf16 {tuple(shape)} on {self.device}")
 
     def rows(self, q, k, start_pos, row_offsets, q_out=None, k_out=None, stream=None):
         """Rotates q [tokens, Hq, d] and k [tokens, Hkv, d] (bf16, d 64 or 128; k may be None): row b's tokens row_offsets[b] ..
         row_offsets[b+1] - 1 stand at positions start_pos[b], start_pos[b] + 1, ...  The heads of a token are contiguous, tokens
         may be any multiple of 8 elements apart (parts of a joint projection).  Outputs are allocated unless given and may be the
-        inputs; tokens of no row stay as they are.  Returns q_out, k_out."""
+        inputs; tokens of no row stay as they are (in an output that is allocated here: whatever its memory held).  Returns q_out, k_out."""
         if not isinstance(q, torch.Tensor) or q.dim() != 3:
             raise ValueError("q: expected a tensor [tokens, heads, d]")
         shape = q.shape
         total, Hq, d = shape
-        if d != self._head and any(t is not None and t.shape[-1] != d for t in self._norms):
+        if self._head is not None and any(t is not None and t.shape[-1] != d for t in self._norms):
             raise ValueError(f"norm weights for heads of another size than {d}")
         B = start_pos.shape[0]
-        _want(start_pos, "start_pos", (B,), (torch.int32,), self.device)
-        _want(row_offsets, "row_offsets", (B + 1,), (torch.int32,), self.device)
+        _want(start_pos, "start_pos", (B,), _I32, self.device)
+        _want(row_offsets, "row_offsets", (B + 1,), _I32, self.device)
         if q_out is None:
             q_out = self._new(shape, stream, q.dtype)
-        args = [q.data_ptr(), q_out.data_ptr(), self._tokens(q, "q", shape), self._tokens(q_out, "q_out", shape)]
+        args = self._rows_args.copy()
+        args[2:4] = self._tokens(q, "q", shape, Hq, d), self._tokens(q_out, "q_out", shape, Hq, d)
+        args[:2] = q.data_ptr(), q_out.data_ptr()
         Hkv = 0
         if k is None:
-            args += None, None, 0, 0
+            args[6:8] = 0, 0
         else:
             Hkv = k.shape[1] if k.dim() == 3 else 0
             shape = torch.Size((total, Hkv, d))
             if k_out is None:
                 k_out = self._new(shape, stream, k.dtype)
-            args += k.data_ptr(), k_out.data_ptr(), self._tokens(k, "k", shape), self._tokens(k_out, "k_out", shape)
+            args[6:8] = self._tokens(k, "k", shape, Hkv, d), self._tokens(k_out, "k_out", shape, Hkv, d)
+            args[4:6] = k.data_ptr(), k_out.data_ptr()
         if total == 0:
             return q_out, k_out
-        args += (start_pos.data_ptr(), row_offsets.data_ptr(), total, B, Hq, Hkv, d, self._tables[0], self._tables[1],
-                 self.max_position, self._flag, None, self._options)
+        args[8:15] = start_pos.data_ptr(), row_offsets.data_ptr(), total, B, Hq, Hkv, d
         self._enqueue("ac_rope_rows", args, stream, -2)
         return q_out, k_out
 
