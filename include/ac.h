@@ -28,8 +28,9 @@
  *   - The kernels are launched with programmatic stream serialization and signal launch completion
  *     early, so that in a chain of calls each kernel's set-up overlaps the tail of the one before.
  *     Before synchronising on the preceding kernel the attention kernels read only context_lens,
- *     block_table and cache tiles below the one holding slot context_lens[b] - 1, and the projection
- *     kernels only their weights.  The attention and RoPE kernels signal only after their own
+ *     block_table and cache tiles below the one holding slot context_lens[b] - 1 (over an 8-bit cache, whose
+ *     append also rewrites the slots in front of its own in a block: below the block holding that slot, and
+ *     no scales), and the projection kernels only their weights.  The attention and RoPE kernels signal only after their own
  *     synchronisation, so no kernel that writes the cache can still be running two launches back:
  *     consecutive steps on one cache need nothing between them.  The early reads are invisible
  *     unless the kernel enqueued directly before one of these calls BOTH writes context_lens,
@@ -547,7 +548,8 @@ int ac_paged_decode_attn_q4(const void* q_rot, const ac_q4_cache* cache, const i
  * become c * (old s / new s), rounded as above.  A scale at least doubles when it grows, so a code that was rounded more than once
  * is off by less than one of its final steps (INT8).  A write at the first slot of a block begins it anew, whatever it held.  What
  * appending one by one and storing at once leave may differ by that.  No other block is touched: a page that rows share is
- * written by none of them (ac_cache_fork copies the partly filled page).  Attention and load take any finite positive scale. */
+ * written by none of them (ac_cache_fork copies the partly filled page).  Two rows of a call that write into one block are a
+ * caller error.  Attention and load take any finite positive scale. */
 #define AC_Q8_INT8 0
 #define AC_Q8_E4M3 1
 typedef struct ac_q8_cache {
@@ -636,7 +638,8 @@ int ac_rope_tables(float* rope_cos, float* rope_sin, int64_t first_position, int
  * tokens stride_*_token elements apart (multiples of 8, at least Hq*d or Hkv*d), so that they may be parts of a joint projection's
  * output; q_out and k_out likewise, each either its input with the same stride or apart from both inputs.  Hkv may be 0 (then k_in
  * and k_out are ignored).  row_offsets, start_pos and their rows as ac_kv_store_q4: tokens of inactive rows and of no row are not
- * touched; a token at or past max_position is not written and sets AC_FLAG_POSITION_OOB.  Any Hq and Hkv whose sum is at most
+ * touched; a token at or past max_position is not written and sets AC_FLAG_POSITION_OOB (AC_FLAG_WAIT_TIMEOUT: a copy of the call did
+ * not arrive).  Any Hq and Hkv whose sum is at most
  * 65535; d is 64 or 128. */
 int ac_rope_rows(const void* q_in, void* q_out, int64_t stride_q_in_token, int64_t stride_q_out_token,
                  const void* k_in, void* k_out, int64_t stride_k_in_token, int64_t stride_k_out_token,
