@@ -265,7 +265,8 @@ class AttentionBlockStep:
 # outlive them.
 
 _BF16 = (torch.bfloat16, torch.int16)          # bf16 values, or their bits
-_I32 = (torch.int32,)
+_INT = torch.int32
+_I32 = (_INT,)
 
 
 def _prepared(name, args):
@@ -519,21 +520,40 @@ class _QuantisedCache(_OnDevice):
                                                                     self.page_size, self.num_pages, self._flag, None])
 
     def _bulk(self, name, k, v, block_table, start_pos, row_offsets, stream):
-        B = start_pos.shape[0]
-        total = k.shape[0]
-        shape = (total, self.Hkv, self.d)
-        _want(k, "k", shape, _BF16, self.device)
-        _want(v, "v", shape, _BF16, self.device)
-        _want(start_pos, "start_pos", (B,), _I32, self.device)
-        _want(row_offsets, "row_offsets", (B + 1,), _I32, self.device)
-        width = block_table.shape[-1]
-        _want(block_table, "block_table", (B, width), _I32, self.device)
+        # All in one expression where all is well (a microsecond less than tensor by tensor, a sixth of the call); what is wrong is
+        # then looked for one by one.
+        device = self.device
+        try:
+            shape, (B,), (rows, width) = k.shape, start_pos.shape, block_table.shape
+            total, heads, d = shape
+            well = (heads == self.Hkv and d == self.d and v.shape == shape and rows == B and row_offsets.shape == (B + 1,)
+                    and k.dtype in _BF16 and v.dtype in _BF16 and start_pos.dtype is _INT and row_offsets.dtype is _INT
+                    and block_table.dtype is _INT and k.is_contiguous() and v.is_contiguous() and start_pos.is_contiguous()
+                    and row_offsets.is_contiguous() and block_table.is_contiguous() and k.device == device and v.device == device
+                    and start_pos.device == device and row_offsets.device == device and block_table.device == device)
+        except (AttributeError, ValueError):
+            well = False
+        if not well:
+            self._refuse_bulk(k, v, block_table, start_pos, row_offsets)
         if total == 0:
             return
         args = self._bulk_args.copy()
         args[:2] = k.data_ptr(), v.data_ptr()
         args[3:9] = block_table.data_ptr(), width, start_pos.data_ptr(), row_offsets.data_ptr(), total, B
         self._enqueue(name, args, stream, -1)
+
+    def _refuse_bulk(self, k, v, block_table, start_pos, row_offsets):
+        for t, what in ((k, "k"), (v, "v"), (start_pos, "start_pos"), (row_offsets, "row_offsets"), (block_table, "block_table")):
+            if not isinstance(t, torch.Tensor):
+                raise TypeError(f"{what}: {type(t).__name__}, expected a tensor")
+        B = start_pos.shape[0] if start_pos.dim() else 0
+        shape = (k.shape[0] if k.dim() else 0, self.Hkv, self.d)
+        _want(k, "k", shape, _BF16, self.device)
+        _want(v, "v", shape, _BF16, self.device)
+        _want(start_pos, "start_pos", (B,), _I32, self.device)
+        _want(row_offsets, "row_offsets", (B + 1,), _I32, self.device)
+        _want(block_table, "block_table", (B, block_table.shape[-1] if block_table.dim() else 0), _I32, self.device)
+        raise ValueError("tensors that do not go together")
 
     def store(self, k, v, block_table, start_pos, row_offsets, stream=None):
         """Quantises k, v (bf16 [tokens, Hkv, d], keys rotated): row b's tokens row_offsets[b] .. row_offsets[b+1] - 1
@@ -828,9 +848,13 @@ class Rope(_OnDevice):
         total, Hq, d = shape
         if self._head is not None and any(t is not None and t.shape[-1] != d for t in self._norms):
             raise ValueError(f"norm weights for heads of another size than {d}")
+        device = self.device
         B = start_pos.shape[0]
-        _want(start_pos, "start_pos", (B,), _I32, self.device)
-        _want(row_offsets, "row_offsets", (B + 1,), _I32, self.device)
+        if not (start_pos.shape == (B,) and row_offsets.shape == (B + 1,) and start_pos.dtype is _INT and row_offsets.dtype is _INT
+                and start_pos.is_contiguous() and row_offsets.is_contiguous() and start_pos.device == device
+                and row_offsets.device == device):
+            _want(start_pos, "start_pos", (B,), _I32, device)
+            _want(row_offsets, "row_offsets", (B + 1,), _I32, device)
         if q_out is None:
             q_out = self._new(shape, stream, q.dtype)
         args = self._rows_args.copy()
