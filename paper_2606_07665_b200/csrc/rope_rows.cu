@@ -175,18 +175,19 @@ __global__ void __launch_bounds__(128) rope_rows_kernel(const RowsParams p) {
     }
 }
 
-// Many tokens: the warps of persistent CTAs take pieces in turn.  Each has a ring of stages in shared memory; a stage receives
+// Many tokens: the warps of persistent CTAs share the pieces out evenly.  Each has a ring of stages in shared memory; a stage receives
 // a piece and its row of angles by bulk copies, is rotated in place and leaves by a bulk copy, so that the bytes in flight cost no
-// registers and loads run ahead of the arithmetic by as many pieces as there are stages.  The positions of the next 32 pieces are
-// looked up at a time, one per lane.
+// registers: while a piece is rotated the next one arrives and the two before it leave.  Where the next 32 pieces lie is looked up at
+// a time, one per lane.
 //
-// Bound: HBM, 2 bytes in and out per element: 70.3 thousand tokens of 40 heads of 128 (1.44 GB) 232 us = 6210 GB/s, 0.96 of the
+// Bound: HBM, 2 bytes in and out per element: 70.3 thousand tokens of 40 heads of 128 (1.44 GB) 240 us = 6000 GB/s, 0.93 of the
 // copy rate.  (Through registers, as above: 262 at best, 24 warps per SM.)
 constexpr int kPieceBytes = 4096, kAngleBytes = 256;       // at most, of a piece and of its cosines or sines
-// 70.3 thousand tokens of 40 heads of 128, us, by (warps per SM, stages): (8, 4) 279, (12, 3) 243, (12, 4) 233, (10, 5) 256, (13, 3)
-// 278, (16, 3) 265; pieces of 2 or 8 KB are slower.
+// 70.3 thousand tokens of 40 heads of 128, us, in a burst and in a second of such calls, which the power limit holds back, by (stages,
+// stores in flight) of 12 warps: (2, 0) 236 and 238, (3, 1) 238 and 239, (4, 2) 238 and 237, (4, 1) 256 and 235.  Warps that take the
+// pieces in turn instead of neighbouring ones, (4, 2): 238 and 242, and 152 instead of 125 with heads of 64.
 constexpr int kStreamWarps = 12, kStreamStages = 4;
-constexpr int kStores = 1;                                 // stores that may still read their stages while the next piece is fetched
+constexpr int kStores = 2;                                 // stores that may still read their stages while the next piece is fetched
 constexpr int kStageBytes = kPieceBytes + 2 * kAngleBytes;
 constexpr int kStreamSmem = kStreamWarps * kStreamStages * (kStageBytes + 8) + 128;
 
@@ -195,8 +196,14 @@ __device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_
                  "r"(bytes), "r"(bar)
                  : "memory");
 }
-__device__ __forceinline__ void bulk_store(void* dst, uint32_t src, uint32_t bytes) {
-    asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"(dst), "r"(src), "r"(bytes) : "memory");
+__device__ __forceinline__ void bulk_load_once(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar, uint64_t policy) {
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1], %2, [%3], %4;" ::"r"(dst),
+                 "l"(src), "r"(bytes), "r"(bar), "l"(policy)
+                 : "memory");
+}
+__device__ __forceinline__ void bulk_store(void* dst, uint32_t src, uint32_t bytes, uint64_t policy) {
+    asm volatile("cp.async.bulk.global.shared::cta.bulk_group.L2::cache_hint [%0], [%1], %2, %3;" ::"l"(dst), "r"(src), "r"(bytes), "l"(policy)
+                 : "memory");
 }
 __device__ __forceinline__ void bulk_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
 template <int N>
@@ -222,34 +229,44 @@ __global__ void __launch_bounds__(kStreamWarps * 32, 1) rope_rows_stream_kernel(
 
     const long long items = static_cast<long long>(p.total_tokens) * p.chunks;
     const unsigned warps = gridDim.x * kStreamWarps;
-    const unsigned first = blockIdx.x * kStreamWarps + warp;       // this warp's pieces: first + n * warps
-    const long long n_my = first < items ? (items - first - 1) / warps + 1 : 0;
+    const long long w = static_cast<long long>(blockIdx.x) * kStreamWarps + warp;
+    const long long first = items * w / warps, n_my = items * (w + 1) / warps - first;     // this warp's pieces lie side by side
     const uint32_t angle_bytes = p.rotary_dim * 2;
+    const uint64_t policy = l2_policy_evict_first();       // for what is read and written once; the angles serve many pieces
     const LaneElements<D, INTERLEAVED> le(lane, p.rotary_dim);
 
-    int i_token = 0, i_piece = 0, i_pos = -1;              // lane l: piece 32 m + l, among those being fetched
-    int c_token = 0, c_piece = 0, c_pos = -1;              // and among those being rotated
+    // Lane l: piece 32 m + l, where it lies and how many heads it has (0: no position; negative: heads of k), among those being
+    // fetched (i_) and among those being rotated (c_).
+    const uint16_t* i_src = nullptr;
+    uint16_t* i_dst = nullptr;
+    uint16_t* c_dst = nullptr;
+    int i_heads = 0, i_pos = 0, c_heads = 0;
     auto look_up = [&](long long n0) {
         const long long n = n0 + lane;
-        i_pos = -1;
+        i_heads = 0;
         if (n < n_my) {
-            const long long item = first + n * warps;
-            i_token = static_cast<int>(item / p.chunks);
-            i_piece = static_cast<int>(item - static_cast<long long>(i_token) * p.chunks);
-            i_pos = lane_token_position(p, i_token);
+            const long long item = first + n;
+            const int token = static_cast<int>(item / p.chunks);
+            const int piece = static_cast<int>(item - static_cast<long long>(token) * p.chunks);
+            i_pos = lane_token_position(p, token);
+            if (i_pos >= 0) {
+                const Piece what = find_piece<D>(p, token, piece);
+                i_src = what.src;
+                i_dst = what.dst;
+                i_heads = piece < p.q_chunks ? what.heads : -what.heads;
+            }
         }
     };
     auto fetch = [&](long long n, int stage) {
-        const int src = static_cast<int>(n & 31);
-        const int token = __shfl_sync(0xffffffffu, i_token, src), piece = __shfl_sync(0xffffffffu, i_piece, src);
-        const int pos = __shfl_sync(0xffffffffu, i_pos, src);
+        const int from = static_cast<int>(n & 31);
+        const unsigned long long src = __shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(i_src), from);
+        const int heads = abs(__shfl_sync(0xffffffffu, i_heads, from)), pos = __shfl_sync(0xffffffffu, i_pos, from);
         if (lane == 0) {
             const uint32_t bar = bars + stage * 8, at = ring_at + stage * kStageBytes;
-            if (pos >= 0) {
-                const Piece what = find_piece<D>(p, token, piece);
-                const uint32_t bytes = what.heads * D * 2;
+            if (heads > 0) {
+                const uint32_t bytes = heads * D * 2;
                 mbar_arrive_expect_tx(bar, bytes + 2 * angle_bytes);
-                bulk_load(at, what.src, bytes, bar);
+                bulk_load_once(at, reinterpret_cast<const void*>(src), bytes, bar, policy);
                 const size_t angle0 = static_cast<size_t>(pos) * (p.rotary_dim / 2);
                 bulk_load(at + kPieceBytes, p.rope_cos + angle0, angle_bytes, bar);
                 bulk_load(at + kPieceBytes + kAngleBytes, p.rope_sin + angle0, angle_bytes, bar);
@@ -266,40 +283,40 @@ __global__ void __launch_bounds__(kStreamWarps * 32, 1) rope_rows_stream_kernel(
     int stage = 0;
     uint32_t parity = 0;
     for (long long n = 0; n < n_my; ++n) {
-        if ((n & 31) == 0) c_token = i_token, c_piece = i_piece, c_pos = i_pos;
+        if ((n & 31) == 0) c_dst = i_dst, c_heads = i_heads;
         const long long ahead = n + S - 1 - kStores;
         if (ahead < n_my) {
             if ((ahead & 31) == 0) look_up(ahead);
             if (lane == 0) bulk_wait_read<kStores>();
             fetch(ahead, (stage + S - 1 - kStores) % S);
         }
-        const int src = static_cast<int>(n & 31);
-        const int token = __shfl_sync(0xffffffffu, c_token, src), piece = __shfl_sync(0xffffffffu, c_piece, src);
-        const int pos = __shfl_sync(0xffffffffu, c_pos, src);
+        const int from = static_cast<int>(n & 31);
+        const unsigned long long dst = __shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(c_dst), from);
+        const int signed_heads = __shfl_sync(0xffffffffu, c_heads, from), heads = abs(signed_heads);
         if (!__all_sync(0xffffffffu, mbar_wait_bounded(bars + stage * 8, parity))) {
             // Record the failure, and give the copies in flight a bounded chance to land before the shared memory is released.
             if (lane == 0 && p.status_flag != nullptr) atomicOr(p.status_flag, AC_FLAG_WAIT_TIMEOUT);
-            for (int s = 0; s < S && n + s < n_my; ++s)
+            for (int s = 0; s < S - kStores && n + s < n_my; ++s)
                 mbar_wait_bounded(bars + (stage + s) % S * 8, stage + s < S ? parity : parity ^ 1u);
             break;
         }
-        if (pos >= 0) {
+        if (heads > 0) {
             uint8_t* const at = ring + stage * kStageBytes;
-            const Piece what = find_piece<D>(p, token, piece);
+            const uint16_t* const norm_w = signed_heads > 0 ? p.q_norm_w : p.k_norm_w;
             RopeAngles angles;
             const float* cr = reinterpret_cast<const float*>(at + kPieceBytes) + (le.turned ? 8 * le.at : 0);
             angles.set_shared(cr, cr + kAngleBytes / 4);
             uint16_t* const x = reinterpret_cast<uint16_t*>(at) + le.e0;
-            for (int h0 = 0; h0 < what.heads; h0 += VECS) {
+            for (int h0 = 0; h0 < heads; h0 += VECS) {
                 const int h = h0 + lane / LPV;
-                const bool on = h < what.heads;
+                const bool on = h < heads;
                 uint32_t v[8];
                 if (NORM || (on && le.turned)) {
                     uint4* const v0 = reinterpret_cast<uint4*>(x + (on ? h : 0) * D);
                     uint4* const v1 = reinterpret_cast<uint4*>(x + (on ? h : 0) * D + le.apart);
                     unpack(v, *v0, *v1);
                     if (NORM) {
-                        if (what.norm_w != nullptr) normalise16<D>(v, what.norm_w + le.e0, what.norm_w + le.e0 + le.apart, p.norm_eps);
+                        if (norm_w != nullptr) normalise16<D>(v, norm_w + le.e0, norm_w + le.e0 + le.apart, p.norm_eps);
                         __syncwarp();                      // lanes without a vector of their own have read another's
                     }
                     if (on) {
@@ -311,7 +328,7 @@ __global__ void __launch_bounds__(kStreamWarps * 32, 1) rope_rows_stream_kernel(
             }
             fence_proxy_async_shared();
             __syncwarp();
-            if (lane == 0) bulk_store(what.dst, ring_at + stage * kStageBytes, what.heads * D * 2);
+            if (lane == 0) bulk_store(reinterpret_cast<void*>(dst), ring_at + stage * kStageBytes, heads * D * 2, policy);
         }
         if (lane == 0) bulk_commit();                      // a group for every piece, empty where nothing is written
         if (++stage == S) {
@@ -349,9 +366,9 @@ __global__ void __launch_bounds__(256) rope_rows_any_kernel(const RowsParams p) 
 
 #define AC_ROPE_EACH(DO, D_) DO(D_, false, false) DO(D_, false, true) DO(D_, true, false) DO(D_, true, true)
 
-// From how many bytes of input on the streaming kernel is used: 28 + 4 heads of 128, us, direct and streaming: 200 tokens 3.2 and
-// 5.2, 2000 tokens 9.6 and 11.4, 4000 (33 MB) 17.4 and 17.9, 8000 (66 MB) 31.6 and 30.8.
-constexpr long long kStreamFromBytes = 48 << 20;
+// From how many bytes of input on the streaming kernel is used: 28 + 4 heads of 128, us, direct and streaming: 200 tokens 3.1 and
+// 4.8, 2000 (16 MB) 10.0 and 10.1, 4000 (33 MB) 17.2 and 14.8, 8000 31.2 and 26.0, 16000 59 and 47.
+constexpr long long kStreamFromBytes = 24 << 20;
 
 template <int D>
 cudaError_t launch_rows(RowsParams p, int sms, cudaStream_t stream) {
