@@ -619,7 +619,7 @@ class Q8Cache(_QuantisedCache):
     ``k_codes``, ``v_codes``: int8 or float8_e4m3fn [num_pages, page_size, Hkv, d] ("token_major") or [num_pages, Hkv,
     page_size, d] ("head_major"); ``scales``: fp32 [num_pages, Hkv, page_size/block, 2] (K and V), powers of two, one for every
     ``block`` consecutive slots.  Pages of the scales may lie further apart than they are long; for ``pools`` they have
-    to be a multiple of 16 bytes apart, as ``empty`` makes them."""
+    to be a multiple of 16 bytes apart, as ``empty`` makes them, and what lies between two of them goes with the first."""
 
     _format = "q8"
 
