@@ -849,10 +849,15 @@ class Rope(_OnDevice):
         if self._head is not None and any(t is not None and t.shape[-1] != d for t in self._norms):
             raise ValueError(f"norm weights for heads of another size than {d}")
         device = self.device
-        B = start_pos.shape[0]
-        if not (start_pos.shape == (B,) and row_offsets.shape == (B + 1,) and start_pos.dtype is _INT and row_offsets.dtype is _INT
-                and start_pos.is_contiguous() and row_offsets.is_contiguous() and start_pos.device == device
-                and row_offsets.device == device):
+        try:
+            B = start_pos.shape[0] if start_pos.dim() else 0
+            well = (start_pos.shape == (B,) and row_offsets.shape == (B + 1,) and start_pos.dtype is _INT and row_offsets.dtype is _INT
+                    and start_pos.is_contiguous() and row_offsets.is_contiguous() and start_pos.device == device
+                    and row_offsets.device == device)
+            Hkv = 0 if k is None or k.dim() != 3 else k.shape[1]
+        except AttributeError:
+            raise TypeError("start_pos, row_offsets and k: expected tensors") from None
+        if not well:
             _want(start_pos, "start_pos", (B,), _I32, device)
             _want(row_offsets, "row_offsets", (B + 1,), _I32, device)
         if q_out is None:
@@ -860,11 +865,9 @@ class Rope(_OnDevice):
         args = self._rows_args.copy()
         args[2:4] = self._tokens(q, "q", shape, Hq, d), self._tokens(q_out, "q_out", shape, Hq, d)
         args[:2] = q.data_ptr(), q_out.data_ptr()
-        Hkv = 0
         if k is None:
             args[6:8] = 0, 0
         else:
-            Hkv = k.shape[1] if k.dim() == 3 else 0
             shape = torch.Size((total, Hkv, d))
             if k_out is None:
                 k_out = self._new(shape, stream, k.dtype)

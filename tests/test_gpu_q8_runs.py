@@ -329,3 +329,17 @@ def test_rope_refusals(rt):
         rt.Rope(f(8, 32), f(8, 32), q_norm_weight=b(128)).rows(q, k, start, off)
     q0, k0 = r.rows(b(0, 4, 64), b(0, 2, 64), start, off)
     assert q0.shape == (0, 4, 64) and k0.shape == (0, 2, 64)
+
+
+def test_rope_refuses_what_is_no_tensor(rt):
+    import torch
+    r = rt.Rope(torch.zeros(8, 32, device="cuda"), torch.zeros(8, 32, device="cuda"))
+    q = torch.zeros(5, 4, 64, device="cuda", dtype=torch.bfloat16)
+    start, off = torch.zeros(1, device="cuda", dtype=torch.int32), torch.zeros(2, device="cuda", dtype=torch.int32)
+    for bad in ((q, None, None, off), (q, None, start, [0, 5]), (q, [q], start, off), (q, None, 0, off)):
+        with pytest.raises(TypeError):
+            r.rows(*bad)
+    with pytest.raises(ValueError):
+        r.rows(q, None, start[0], off)
+    with pytest.raises(ValueError):
+        r.rows(q, None, start, off[0])
