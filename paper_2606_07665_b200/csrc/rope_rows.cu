@@ -83,17 +83,71 @@ __device__ __forceinline__ int lane_token_position(const RowsParams& p, int toke
     return position_in(p, lo, token, true);
 }
 
-// Per-head RMSNorm of a lane's 16 elements (words x), D/16 lanes per vector: the fp64 arithmetic of rope_variant_vector.  The whole warp.
-template <int D>
-__device__ __forceinline__ void normalise16(uint32_t (&x)[8], const uint16_t* w0, const uint16_t* w1, float eps) {
+// The sum of squares as rope_variant_vector forms it: D/32 neighbours at a time, these partial sums joined at distances 16, 8, 4, 2, 1.
+// a and b are the lane's two runs of eight elements; the runs are brought into order among the D/16 lanes first.
+template <int D, bool INTERLEAVED>
+__device__ __noinline__ double squares_in_order(uint4 a, uint4 b, int rotary_dim, int lane) {
+    constexpr int EPL = D / 32, NP = 8 / EPL, LPV = D / 16;        // elements of a partial sum, partial sums of a run, lanes
+    const uint32_t words[2][4] = {{a.x, a.y, a.z, a.w}, {b.x, b.y, b.z, b.w}};
+    double part[2][NP], sum[2 * NP];
+#pragma unroll
+    for (int r = 0; r < 2; ++r)
+#pragma unroll
+        for (int i = 0; i < NP; ++i) {
+            part[r][i] = 0.0;
+#pragma unroll
+            for (int e = i * EPL; e < (i + 1) * EPL; ++e) {
+                const uint32_t w = words[r][e >> 1];
+                const double d = static_cast<double>(__uint_as_float((e & 1) ? w & 0xFFFF0000u : w << 16));
+                part[r][i] = __fma_rn(d, d, part[r][i]);
+            }
+        }
+    const int at = lane % LPV, turned = rotary_dim / 16;
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+        const int run = 2 * at + r;                        // which lane holds it, as its first or second (see LaneElements)
+        const bool halves = !INTERLEAVED && run < 2 * turned;
+        const int holder = lane - at + (!halves ? at : run < turned ? run : run - turned);
+        const bool second = halves ? run >= turned : r == 1;
+#pragma unroll
+        for (int i = 0; i < NP; ++i) {
+            const double s0 = __shfl_sync(0xffffffffu, part[0][i], holder), s1 = __shfl_sync(0xffffffffu, part[1][i], holder);
+            sum[r * NP + i] = second ? s1 : s0;
+        }
+    }
+#pragma unroll
+    for (int off = LPV / 2; off >= 1; off >>= 1)
+#pragma unroll
+        for (int i = 0; i < 2 * NP; ++i) sum[i] = __dadd_rn(sum[i], __shfl_xor_sync(0xffffffffu, sum[i], off));
+#pragma unroll
+    for (int off = NP; off >= 1; off >>= 1)
+#pragma unroll
+        for (int i = 0; i < off; ++i) sum[i] = __dadd_rn(sum[i], sum[i + off]);
+    return sum[0];
+}
+
+// Per-head RMSNorm of a lane's 16 elements (words x), D/16 lanes per vector, with the bits of rope_variant_vector.  The whole warp.
+//
+// Nearly always the squares add up exactly, in whatever order: elements whose least exponent field is f are multiples of
+// q = 2^(f - 134), their squares and sums of them of q^2, and those below 2^53 q^2 are fp64 numbers.  (Zeros do not count; f is taken over
+// the warp; the sum is looked at with a bit to spare, since it is rounded where it is not exact.)
+template <int D, bool INTERLEAVED>
+__device__ __forceinline__ void normalise16(uint32_t (&x)[8], const uint16_t* w0, const uint16_t* w1, float eps, int rotary_dim, int lane) {
     double ss = 0.0;
+    uint32_t least = 0xFFFFFFFFu;                          // of the magnitudes minus 1, where zero is the largest
+#pragma unroll
+    for (int i = 0; i < 8; ++i) least = __viaddmin_u16x2(x[i] & 0x7FFF7FFFu, 0xFFFFFFFFu, least);
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
         const double d = static_cast<double>(__uint_as_float((e & 1) ? x[e >> 1] & 0xFFFF0000u : x[e >> 1] << 16));
-        ss = __dadd_rn(ss, __dmul_rn(d, d));
+        ss = __fma_rn(d, d, ss);                           // d * d is exact
     }
 #pragma unroll
     for (int off = D / 32; off >= 1; off >>= 1) ss = __dadd_rn(ss, __shfl_xor_sync(0xffffffffu, ss, off));
+    const int f = static_cast<int>((__reduce_min_sync(0xffffffffu, min(least & 0xFFFFu, least >> 16)) + 1u) >> 7);
+    const bool exact = (__double2hiint(ss) >> 20) - 1023 + 2 <= 53 + 2 * (f - 134);
+    if (!__all_sync(0xffffffffu, exact))
+        ss = squares_in_order<D, INTERLEAVED>(make_uint4(x[0], x[1], x[2], x[3]), make_uint4(x[4], x[5], x[6], x[7]), rotary_dim, lane);
     const double rr = __ddiv_rn(1.0, __dsqrt_rn(__dadd_rn(__ddiv_rn(ss, static_cast<double>(D)), static_cast<double>(eps))));
     const float rr_hi = static_cast<float>(rr), rr_lo = static_cast<float>(rr - static_cast<double>(rr_hi));
 #pragma unroll
@@ -165,7 +219,7 @@ __global__ void __launch_bounds__(128) rope_rows_kernel(const RowsParams p) {
             const int h = h0 + lane / LPV + u * VECS;
             uint32_t v[8];
             unpack(v, x[u][0], x[u][1]);
-            if (NORM && at.norm_w != nullptr) normalise16<D>(v, at.norm_w + le.e0, at.norm_w + le.e0 + le.apart, p.norm_eps);
+            if (NORM && at.norm_w != nullptr) normalise16<D, INTERLEAVED>(v, at.norm_w + le.e0, at.norm_w + le.e0 + le.apart, p.norm_eps, p.rotary_dim, lane);
             if (h < at.heads) {
                 if (le.turned) rope_turn16<INTERLEAVED>(v, angles);
                 __stcs(reinterpret_cast<uint4*>(dst + h * D), make_uint4(v[0], v[1], v[2], v[3]));
@@ -316,7 +370,7 @@ __global__ void __launch_bounds__(kStreamWarps * 32, 1) rope_rows_stream_kernel(
                     uint4* const v1 = reinterpret_cast<uint4*>(x + (on ? h : 0) * D + le.apart);
                     unpack(v, *v0, *v1);
                     if (NORM) {
-                        if (norm_w != nullptr) normalise16<D>(v, norm_w + le.e0, norm_w + le.e0 + le.apart, p.norm_eps);
+                        if (norm_w != nullptr) normalise16<D, INTERLEAVED>(v, norm_w + le.e0, norm_w + le.e0 + le.apart, p.norm_eps, p.rotary_dim, lane);
                         __syncwarp();                      // lanes without a vector of their own have read another's
                     }
                     if (on) {
