@@ -679,8 +679,10 @@ class _QuantisedStep(_Rows):
     def __init__(self, cache, block_table, context_lens, Hq, lens_host=None, window=0, sinks=0, rope_cos=None,
                  rope_sin=None, max_context_len=None, num_splits=None, row_order="auto", rope_variants=None,
                  softmax_scale=0.0, new_tokens=1):
-        if not isinstance(cache, self._cache_type):
-            raise TypeError(f"cache: {type(cache).__name__}, expected a {self._cache_type.__name__}")
+        try:                                               # any object that has the format's descriptor
+            getattr(ac.lib(), "ac_paged_decode_attn_" + self._format).argtypes[1].from_param(cache.struct)
+        except (AttributeError, TypeError, ctypes.ArgumentError):
+            raise TypeError(f"cache: {type(cache).__name__} without the descriptor of a cache of format {self._format}") from None
         self._bind(cache.device)
         self.cache, self.window, self.sinks = cache, int(window), int(sinks)
         self.softmax_scale, self.new_tokens = float(softmax_scale), _new_tokens(new_tokens)
@@ -705,13 +707,13 @@ class _QuantisedStep(_Rows):
         return super()._buffers() + self.cache._buffers()
 
     def _choose(self, counts, span):
-        plan = getattr(ac, "ac_decode_plan_" + self.cache._format)
+        plan = getattr(ac, "ac_decode_plan_" + self._format)
         return plan(counts, self.B, self.Hq, self.Hkv, self.d, self.page_size, span)[0]
 
     def _marshal(self):
         shape = [self.B, self.Hq, self.Hkv, self.d, self.page_size, self.num_pages]
         table = [self.cache.struct, self.block_table.data_ptr(), self.max_pages_per_seq, self.context_lens.data_ptr()]
-        self._attn_call, self._append_call = ("ac_" + f + self.cache._format for f in ("paged_decode_attn_", "rope_kv_append_"))
+        self._attn_call, self._append_call = ("ac_" + f + self._format for f in ("paged_decode_attn_", "rope_kv_append_"))
         self._attn_args = _prepared(self._attn_call, [None, *table, self.new_tokens, self.softmax_scale, self.num_splits,
                                                       self.workspace.data_ptr(), self.workspace_bytes, None, *shape,
                                                       self.max_context_len, self._flag, None, self._options])
@@ -759,13 +761,13 @@ class _QuantisedStep(_Rows):
 class Q4DecodeStep(_QuantisedStep):
     """One decode step over a 4-bit cache: RoPE + quantised append, then attention (two launches).  See _QuantisedStep."""
 
-    _cache_type = Q4Cache
+    _format = "q4"
 
 
 class Q8DecodeStep(_QuantisedStep):
     """One decode step over an 8-bit cache: RoPE + quantised append, then attention (two launches).  See _QuantisedStep."""
 
-    _cache_type = Q8Cache
+    _format = "q8"
 
 
 class Rope(_OnDevice):
