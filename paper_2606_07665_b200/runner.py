@@ -868,6 +868,8 @@ class Rope(_OnDevice):
         args[2:4] = self._tokens(q, "q", shape, Hq, d), self._tokens(q_out, "q_out", shape, Hq, d)
         args[:2] = q.data_ptr(), q_out.data_ptr()
         if k is None:
+            if k_out is not None:
+                raise ValueError("k_out without k")
             args[6:8] = 0, 0
         else:
             shape = torch.Size((total, Hkv, d))
