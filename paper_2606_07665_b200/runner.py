@@ -791,7 +791,7 @@ class Rope(_OnDevice):
         self._norms = (q_norm_weight, k_norm_weight)       # kept alive
         for t, what in zip(self._norms, ("q_norm_weight", "k_norm_weight")):
             if t is not None:
-                _want(t, what, (t.shape[-1],), _BF16, self.device)
+                _want(t, what, t.shape[-1:] if isinstance(t, torch.Tensor) and t.dim() else (0,), _BF16, self.device)
         self._head = next((t.shape[-1] for t in self._norms if t is not None), None)
         self._options = ac._rope_options(self.rotary_dim, interleaved, q_norm_weight, k_norm_weight, norm_eps)
         self._rows_args = _prepared("ac_rope_rows", [None] * 15 + [cos.data_ptr(), sin.data_ptr(), self.max_position, self._flag,
