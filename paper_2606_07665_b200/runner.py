@@ -655,7 +655,8 @@ class Q8Cache(_QuantisedCache):
         blocks = page_size // block
         width = Hkv * blocks * 2
         held = torch.zeros((num_pages, -(-width // 4) * 4), dtype=torch.float32, device=device)
-        cache = cls(k, v, held[:, :width].view(num_pages, Hkv, blocks, 2), layout=layout)
+        # (a view() of a single page would forget how far apart pages are)
+        cache = cls(k, v, held.as_strided((num_pages, Hkv, blocks, 2), (held.shape[1], 2 * blocks, 2, 1)), layout=layout)
         cache._allocated = (k, v, held)
         return cache
 
