@@ -619,7 +619,8 @@ class Q8Cache(_QuantisedCache):
     ``k_codes``, ``v_codes``: int8 or float8_e4m3fn [num_pages, page_size, Hkv, d] ("token_major") or [num_pages, Hkv,
     page_size, d] ("head_major"); ``scales``: fp32 [num_pages, Hkv, page_size/block, 2] (K and V), powers of two, one for every
     ``block`` consecutive slots.  Pages of the scales may lie further apart than they are long; for ``pools`` they have
-    to be a multiple of 16 bytes apart, as ``empty`` makes them, and what lies between two of them goes with the first."""
+    to be a multiple of 16 bytes apart, as ``empty`` makes them, with less than 16 bytes between two of them, which go with the
+    first."""
 
     _format = "q8"
 
@@ -665,6 +666,8 @@ class Q8Cache(_QuantisedCache):
         """(tensor, segments of a page, whether a fork copies the whole page) of the three pools, for CachePages."""
         if self._apart % 4:
             raise ValueError("scales: pages have to be a multiple of 16 bytes apart (empty makes them so)")
+        if self._apart - self.scales[0].numel() >= 4:      # more than padding: another cache's scales, which would be moved too
+            raise ValueError("scales: 16 bytes or more between two pages")
         codes = 1 if self.layout == "token_major" else self.Hkv
         held = self.scales.as_strided((self.num_pages, self._apart), (self._apart, 1))
         return [(self.k_codes, codes), (self.v_codes, codes), (held, 1, True)]

@@ -37,3 +37,18 @@ def test_pools_of_empty_caches(rt, pages, H, ps, block):
     book.compact()
     torch.cuda.synchronize()
     assert int(book.status_flag) == 0 and refs.tolist() == [1] + [0] * (pages - 1)
+
+
+@pytest.mark.parametrize("layers", [2, 3])
+@pytest.mark.parametrize("H,ps,block", [(2, 32, 16), (4, 16, 16), (1, 64, 16)])
+def test_scales_of_layers_side_by_side(rt, layers, H, ps, block):
+    """Pages of one layer's scales with other layers' between them: calls take them, the page operations would move the others' too."""
+    import torch
+    every = torch.zeros(6, layers, H, ps // block, 2, device="cuda")
+    for layer in range(layers):
+        cache = rt.Q8Cache(*codes(6, ps, H, 64), every[:, layer])
+        with pytest.raises(ValueError, match="scales"):
+            cache.pools
+    apart = torch.zeros(layers, 6, H, ps // block, 2, device="cuda")
+    for layer in range(layers):
+        assert len(rt.Q8Cache(*codes(6, ps, H, 64), apart[layer]).pools) == 3
