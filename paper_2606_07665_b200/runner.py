@@ -668,6 +668,8 @@ class Q8Cache(_QuantisedCache):
             raise ValueError("scales: pages have to be a multiple of 16 bytes apart (empty makes them so)")
         if self._apart - self.scales[0].numel() >= 4:      # more than padding: another cache's scales, which would be moved too
             raise ValueError("scales: 16 bytes or more between two pages")
+        if self.scales.storage_offset() + self.num_pages * self._apart > self.scales.untyped_storage().nbytes() // 4:
+            raise ValueError("scales: no room behind the last page for what lies between two pages")
         codes = 1 if self.layout == "token_major" else self.Hkv
         held = self.scales.as_strided((self.num_pages, self._apart), (self._apart, 1))
         return [(self.k_codes, codes), (self.v_codes, codes), (held, 1, True)]

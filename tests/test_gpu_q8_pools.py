@@ -52,3 +52,13 @@ def test_scales_of_layers_side_by_side(rt, layers, H, ps, block):
     apart = torch.zeros(layers, 6, H, ps // block, 2, device="cuda")
     for layer in range(layers):
         assert len(rt.Q8Cache(*codes(6, ps, H, 64), apart[layer]).pools) == 3
+
+
+def test_scales_without_room_behind_the_last_page(rt):
+    import torch
+    flat = torch.zeros(3 * 4 - 2, device="cuda")
+    short = flat.as_strided((3, 1, 1, 2), (4, 2, 2, 1))
+    with pytest.raises(ValueError, match="scales"):
+        rt.Q8Cache(*codes(3, 16, 1, 64), short).pools
+    room = torch.zeros(3 * 4, device="cuda").as_strided((3, 1, 1, 2), (4, 2, 2, 1))
+    assert len(rt.Q8Cache(*codes(3, 16, 1, 64), room).pools) == 3
