@@ -660,13 +660,15 @@ int ac_rope_rows(const void* q_in, void* q_out, int64_t stride_q_in_token, int64
  * Free pages are handed out lowest index first, in the order of the call's list, so every call's
  * result is determined by its inputs.  The pools themselves are opaque bytes: any number of them (K and V
  * of every layer, codes, parameters) can share one block table. */
+#define AC_PAGE_WHOLE (-1)
 typedef struct ac_page_pool {
     void* base;              /* page p occupies bytes [p*page_bytes, (p+1)*page_bytes); 16-byte aligned */
     int64_t page_bytes;      /* a multiple of 16 * segments */
     int segments;            /* a page is this many equal pieces, each holding the page's slots in order: 1 for
-                                [page, slot, head, d], Hkv for [page, head, slot, ...] */
-    int whole;               /* non-zero: a page's bytes do not follow its slots (the scales of an 8-bit cache), so that
-                                ac_cache_fork copies all of a partly filled page; page_bytes is then any multiple of 16 */
+                                [page, slot, head, d], Hkv for [page, head, slot, ...]; or AC_PAGE_WHOLE where its bytes do not
+                                follow its slots (the scales of an 8-bit cache): ac_cache_fork then copies all of a partly filled
+                                page, and page_bytes is any multiple of 16 */
+    int reserved;
 } ac_page_pool;
 
 /* Most pools of one call. */

@@ -24,6 +24,7 @@ AC_FLAG_POOL_EXHAUSTED = 8
 AC_FLAG_REF_COUNT = 16
 AC_FLAG_ROW_OOB = 32
 AC_MAX_PAGE_POOLS = 128
+AC_PAGE_WHOLE = -1
 AC_Q8_INT8, AC_Q8_E4M3 = 0, 1
 AC_ROPE_NONE, AC_ROPE_LINEAR, AC_ROPE_BASE, AC_ROPE_RAMP = range(4)
 
@@ -76,7 +77,7 @@ class AcRopeScaling(ctypes.Structure):
 
 class AcPagePool(ctypes.Structure):
     """Mirror of ac_page_pool."""
-    _fields_ = [("base", c_void_p), ("page_bytes", c_int64), ("segments", c_int), ("whole", c_int)]
+    _fields_ = [("base", c_void_p), ("page_bytes", c_int64), ("segments", c_int), ("reserved", c_int)]
 
 
 class AcError(RuntimeError):
@@ -603,8 +604,9 @@ def ac_rope_rows(q_in, q_out, stride_q_in_token, stride_q_out_token, k_in, k_out
 
 
 def page_pools(pools):
-    """``pools``: sequence of (tensor or address, page_bytes, segments[, whole]) -> a ctypes array of ac_page_pool."""
-    return (AcPagePool * max(1, len(pools)))(*[AcPagePool(_ptr(base), page_bytes, segments, *whole)
+    """``pools``: sequence of (tensor or address, page_bytes, segments[, whole]) -> a ctypes array of ac_page_pool; whole stands for
+    AC_PAGE_WHOLE segments."""
+    return (AcPagePool * max(1, len(pools)))(*[AcPagePool(_ptr(base), page_bytes, AC_PAGE_WHOLE if any(whole) else segments, 0)
                                                for base, page_bytes, segments, *whole in pools])
 
 

@@ -1408,9 +1408,11 @@ static int check_pools(const ac_page_pool* pools, int n_pools, int page_size) {
     if (n_pools > 0 && pools == nullptr) return AC_ERR_NULL;
     for (int i = 0; i < n_pools; ++i) {
         if (pools[i].base == nullptr) return AC_ERR_NULL;
-        if (pools[i].page_bytes <= 0 || pools[i].segments <= 0) return AC_ERR_SHAPE;
-        if (!aligned16(pools[i].base) || pools[i].page_bytes % (16ll * pools[i].segments) != 0) return AC_ERR_ALIGN;
-        if (page_size > 0 && pools[i].whole == 0 && pools[i].page_bytes / pools[i].segments % page_size != 0) return AC_ERR_SHAPE;
+        const bool whole = pools[i].segments == AC_PAGE_WHOLE;
+        const int segments = whole ? 1 : pools[i].segments;
+        if (pools[i].page_bytes <= 0 || segments <= 0) return AC_ERR_SHAPE;
+        if (!aligned16(pools[i].base) || pools[i].page_bytes % (16ll * segments) != 0) return AC_ERR_ALIGN;
+        if (page_size > 0 && !whole && pools[i].page_bytes / segments % page_size != 0) return AC_ERR_SHAPE;
     }
     return AC_OK;
 }

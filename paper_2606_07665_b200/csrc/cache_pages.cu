@@ -172,7 +172,7 @@ __device__ __forceinline__ void copy_piece(char* dst, const char* src, int64_t l
 __device__ __forceinline__ void run_copies(const ac_page_pool& pool, const int2* jobs, const int32_t* lens, int n,
                                            int page_size, int num_pages, int32_t* status_flag) {
     const int lane = threadIdx.x & 31;
-    const bool slots = lens != nullptr && pool.whole == 0;
+    const bool slots = lens != nullptr && pool.segments != AC_PAGE_WHOLE;
     const int segments = slots ? pool.segments : 1;
     const int64_t seg_bytes = pool.page_bytes / segments;
     const int pieces = static_cast<int>((seg_bytes + kPiece - 1) / kPiece);
@@ -480,8 +480,9 @@ PoolArgs<N> pool_args(const ac_page_pool* pools, int n_pools) {
 unsigned copy_grid(const ac_page_pool* pools, int n_pools, long long jobs, int sms) {
     long long most = 1;
     for (int i = 0; i < n_pools; ++i) {
-        const long long seg = pools[i].page_bytes / pools[i].segments;
-        const long long units = jobs * pools[i].segments * ((seg + kPiece - 1) / kPiece);
+        const int segments = pools[i].segments == AC_PAGE_WHOLE ? 1 : pools[i].segments;
+        const long long seg = pools[i].page_bytes / segments;
+        const long long units = jobs * segments * ((seg + kPiece - 1) / kPiece);
         const long long ctas = (units + kCopyThreads / 32 - 1) / (kCopyThreads / 32);
         most = ctas > most ? ctas : most;
     }

@@ -1,4 +1,7 @@
-"""The pools of an 8-bit cache for the page operations."""
+"""The pools of an 8-bit cache for the page operations, and the descriptors of pools in C callers' memory."""
+import ctypes
+
+import numpy as np
 import pytest
 
 pytestmark = pytest.mark.gpu
@@ -62,3 +65,27 @@ def test_scales_without_room_behind_the_last_page(rt):
         rt.Q8Cache(*codes(3, 16, 1, 64), short).pools
     room = torch.zeros(3 * 4, device="cuda").as_strided((3, 1, 1, 2), (4, 2, 2, 1))
     assert len(rt.Q8Cache(*codes(3, 16, 1, 64), room).pools) == 3
+
+
+def test_pools_that_were_described_without_the_last_member(rt):
+    """The int behind `segments` has never had a meaning for callers that copy by slots: whatever it holds, a fork copies the filled slots."""
+    import torch
+    from paper_2606_07665_b200 import binding as ac
+    rng = np.random.default_rng(1)
+    ps, pages = 16, 4
+    for junk in (1, -1, 0x7FFFFFFF, 77):
+        pool = torch.from_numpy(rng.integers(1, 100, (pages, ps, 64)).astype(np.uint8)).cuda()
+        before = pool.clone()
+        described = ac.page_pools([(pool, ps * 64, 1)])
+        ctypes.memmove(ctypes.addressof(described) + 20, ctypes.byref(ctypes.c_int(junk)), 4)
+        table = torch.tensor([[2, -1], [-1, -1]], dtype=torch.int32, device="cuda")
+        lens = torch.tensor([5, -1], dtype=torch.int32, device="cuda")
+        refs = torch.tensor([0, 0, 1, 0], dtype=torch.int32, device="cuda")
+        pairs = torch.tensor([[0, 1]], dtype=torch.int32, device="cuda")
+        room = torch.zeros(ac.ac_cache_workspace_bytes(2, pages, 1), dtype=torch.uint8, device="cuda")
+        ac.ac_init(0)
+        ac.ac_cache_fork(described, 1, table, 2, lens, refs, pairs, 1, 2, ps, pages, room, room.numel())
+        torch.cuda.synchronize()
+        want = before.clone()
+        want[0, :5] = before[2, :5]
+        assert table[1, 0] == 0 and torch.equal(pool, want), junk
