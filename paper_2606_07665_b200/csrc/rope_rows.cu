@@ -559,8 +559,9 @@ cudaError_t launch_rope_tables(float* rope_cos, float* rope_sin, long long first
                                const RopeScaling& scaling, int sms, cudaStream_t stream) {
     const int half = rotary_dim / 2;
     int run = kRun;                                        // shorter runs where the GPU would not be full
-    while (run > 1 && static_cast<long long>((positions + run - 1) / run) * half < 128ll * sms) run /= 2;
-    const long long threads = static_cast<long long>((positions + run - 1) / run) * half;
+    auto runs = [&]() { return (positions - 1ll) / run + 1; };
+    while (run > 1 && runs() * half < 128ll * sms) run /= 2;
+    const long long threads = runs() * half;
     const long long grid = (threads + 255) / 256;
     if (grid > 0x7fffffffll) return cudaErrorInvalidConfiguration;
     rope_tables_kernel<<<static_cast<unsigned>(grid), 256, 0, stream>>>(rope_cos, rope_sin, first_position, positions, half, run, scaling);
