@@ -619,7 +619,7 @@ int ac_paged_decode_attn_q8(const void* q_rot, const ac_q8_cache* cache, const i
 typedef struct ac_rope_scaling {
     int kind;                /* AC_ROPE_... */
     int reserved;
-    double base;             /* > 0 */
+    double base;             /* > 0; no number of the struct, nor the larger base, above 1e300 in magnitude */
     double factor;           /* > 0 (not used for AC_ROPE_NONE) */
     double original;         /* AC_ROPE_RAMP: positions of the original context, > 0 */
     double low, high;        /* AC_ROPE_RAMP: low < high */

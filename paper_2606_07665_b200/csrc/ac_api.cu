@@ -1341,12 +1341,21 @@ int ac_rope_tables(float* rope_cos, float* rope_sin, int64_t first_position, int
     if (!rope_cos || !rope_sin || !scaling) return AC_ERR_NULL;
     if (positions < 0 || first_position < 0 || rotary_dim <= 0 || rotary_dim % 2 != 0) return AC_ERR_SHAPE;
     if (scaling->kind < AC_ROPE_NONE || scaling->kind > AC_ROPE_RAMP) return AC_ERR_UNSUPPORTED;
-    auto positive = [](double x) { return x > 0.0 && x <= 1e300; };        // false for NaN
+    if (first_position > INT64_MAX - positions) return AC_ERR_SHAPE;
+    auto finite = [](double x) { return x >= -1e300 && x <= 1e300; };      // false for NaN
+    auto positive = [&](double x) { return x > 0.0 && finite(x); };
     if (!positive(scaling->base)) return AC_ERR_SHAPE;
     if (scaling->kind != AC_ROPE_NONE && !positive(scaling->factor)) return AC_ERR_SHAPE;
-    if (scaling->kind == AC_ROPE_BASE && rotary_dim < 4) return AC_ERR_SHAPE;
-    if (scaling->kind == AC_ROPE_RAMP && (!positive(scaling->original) || !(scaling->low < scaling->high))) return AC_ERR_SHAPE;
-    if (!(scaling->magnitude >= 0.0)) return AC_ERR_SHAPE;
+    double base = scaling->base;
+    if (scaling->kind == AC_ROPE_BASE) {
+        if (rotary_dim < 4) return AC_ERR_SHAPE;
+        base *= pow(scaling->factor, rotary_dim / (rotary_dim - 2.0));
+        if (!positive(base)) return AC_ERR_SHAPE;
+    }
+    if (scaling->kind == AC_ROPE_RAMP && (!positive(scaling->original) || !finite(scaling->low) || !finite(scaling->high) ||
+                                          !(scaling->low < scaling->high)))
+        return AC_ERR_SHAPE;
+    if (!(scaling->magnitude >= 0.0) || !finite(scaling->magnitude)) return AC_ERR_SHAPE;
     if (!aligned16(rope_cos) || !aligned16(rope_sin)) return AC_ERR_ALIGN;
     int dev;
     int st = current_ready_device(&dev);
@@ -1354,8 +1363,7 @@ int ac_rope_tables(float* rope_cos, float* rope_sin, int64_t first_position, int
     if (positions == 0) return AC_OK;
     RopeScaling sc;
     sc.kind = scaling->kind;
-    sc.base = scaling->base;
-    if (sc.kind == AC_ROPE_BASE) sc.base *= pow(scaling->factor, rotary_dim / (rotary_dim - 2.0));
+    sc.base = base;
     sc.factor = scaling->factor;
     sc.original = scaling->original;
     sc.low = scaling->low;
