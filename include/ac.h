@@ -627,8 +627,11 @@ typedef struct ac_rope_scaling {
 } ac_rope_scaling;
 
 /* Tables for ac_rope_kv_append and its relatives and for ac_rope_rows: rope_cos[j, i] = magnitude * cos((first_position + j) f_i),
- * rope_sin likewise, j < positions, fp32 [positions, rotary_dim/2] dense, rounded from an fp64 evaluation (error of the angle:
- * 2^-52 of it).  rotary_dim is even; for AC_ROPE_BASE it is at least 4.  positions may be 0. */
+ * rope_sin likewise, j < positions, fp32 [positions, rotary_dim/2] dense, evaluated in fp64 and rounded: each entry is within
+ * magnitude * 2^-45 of the one of an angle that is off by at most (|ln b| + 2 |ln factor| + 12) 2^-53 of itself (2^-48 for bases
+ * below 10^8 that stay; b is the larger base for AC_ROPE_BASE), and then rounded once.  AC_ROPE_RAMP with low >= 0: max(factor,
+ * 1/factor) * high / (high - low) times that where frequencies are blended.  rotary_dim is even; for AC_ROPE_BASE it is at least 4.
+ * positions may be 0. */
 int ac_rope_tables(float* rope_cos, float* rope_sin, int64_t first_position, int positions, int rotary_dim,
                    const ac_rope_scaling* scaling, void* stream);
 
