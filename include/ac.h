@@ -594,7 +594,7 @@ int ac_decode_plan_q8(const int32_t* token_counts_host, int B, int Hq, int Hkv, 
 /* Paged decode attention over the 8-bit cache, merge included: ac_paged_decode_attn_ex with fused_merge set (splits, workspace,
  * inactive rows, window, sinks, row_order and max_context_len as there; options->rope must be NULL).  K and V enter as the
  * exact values c * s; q is bf16, products and sums are fp32, and the softmax weights times V's scale are rounded to fp16
- * (2^-11 relative, or 2^-31 of the largest V scale seen, whichever is more) for the second product.  Slots at or past n_b, the
+ * (2^-11 relative, or 2^-31 of the largest V scale seen, which counts as 2^-120 at least, whichever is more) for the second product.  Slots at or past n_b, the
  * scales of blocks in which the row attends over no token, unreferenced pages and unused block-table entries never influence
  * the result; a page id outside [0, num_pages) reads as zeros.  Outside the supported range: as ac_paged_decode_attn_q4
  * says of q and V.  AC_FLAG_WAIT_TIMEOUT is the only status bit.  The workspace belongs to one call at a time: calls that may

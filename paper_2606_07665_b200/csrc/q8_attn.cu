@@ -304,8 +304,8 @@ __global__ void __launch_bounds__(NW * 32, CTAS) paged_decode_attn_q8_kernel(
 #pragma unroll
         for (int c = 0; c < NC; ++c) o[c][0][nt] = o[c][1][nt] = 0ull;
     }
-    // power of two on V's scales: the largest one seen * vf is in [32, 64); before any, so high that one moves it
-    float vf = 1.329227995784916e36f;              // 2^120
+    // power of two on V's scales: the largest one seen * vf is in [64, 128); before any, so high that one of 2^-119 moves it
+    float vf = 8.507059173023462e37f;              // 2^126, whose inverse is a normal number
     float v_top = 0.0f;
 
     // ldmatrix addresses, the same for K (bytes 4t .. 4t + 3 of a row's chunk land in lane (row, t)) and, transposed, for V:
@@ -426,7 +426,7 @@ __global__ void __launch_bounds__(NW * 32, CTAS) paged_decode_attn_q8_kernel(
             if (v_max > v_top) {
                 v_top = v_max;
                 int k = 6 - (static_cast<int>(__float_as_uint(v_top) >> 23) - 127);
-                k = max(-126, min(k, 120));
+                k = max(-126, min(k, 126));
                 const float next = __uint_as_float(static_cast<uint32_t>(k + 127) << 23);
                 vr = next / vf;
                 vf = next;
