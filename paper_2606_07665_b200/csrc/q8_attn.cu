@@ -91,6 +91,9 @@ __device__ __forceinline__ uint32_t q8_tile_offset(int row, int chunk) {
     return D == 128 ? row * 128 + ((chunk ^ (row & 7)) << 4) : row * 64 + ((chunk ^ ((row >> 1) & 3)) << 4);
 }
 
+// 2^-e of 2^e, |e| <= 126.  (A division takes its slow way beside such numbers.)
+__device__ __forceinline__ float power_of_two_inverse(float x) { return __uint_as_float((254u << 23) - __float_as_uint(x)); }
+
 template <int D, int FMT, int NT, int NW, int STAGES, int CTAS>
 __global__ void __launch_bounds__(NW * 32, CTAS) paged_decode_attn_q8_kernel(
     const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map, const Q8AttnParams p) {
@@ -428,7 +431,7 @@ __global__ void __launch_bounds__(NW * 32, CTAS) paged_decode_attn_q8_kernel(
                 int k = 6 - (static_cast<int>(__float_as_uint(v_top) >> 23) - 127);
                 k = max(-126, min(k, 126));
                 const float next = __uint_as_float(static_cast<uint32_t>(k + 127) << 23);
-                vr = next / vf;
+                vr = next * power_of_two_inverse(vf);
                 vf = next;
             }
 #pragma unroll
@@ -533,7 +536,7 @@ __global__ void __launch_bounds__(NW * 32, CTAS) paged_decode_attn_q8_kernel(
     float* wo = reinterpret_cast<float*>(smem + warp * L::RING_BYTES);
     float* wm = wo + WROWS * WSTRIDE;
     float* wl = wm + WROWS;
-    const float unscale = 1.0f / vf;
+    const float unscale = power_of_two_inverse(vf);
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
         float l[2];
