@@ -21,9 +21,11 @@
 // where pages are no multiple of 32 tokens), no CTA-wide synchronisation in the main loop.
 //
 // Bound: HBM up to eight heads per KV head: 4 rows of 131072 tokens, 64:8 heads of 128 (1.08 GB): 160 us = 6720 GB/s, 1.04 of the measured
-// copy rate; 64 rows of 128 to 8192, 32:8 heads (506 MB): 81 us = 6260 GB/s.  With more heads the arithmetic: 128 rows under a
-// window of 4096, 32:2 heads, int8 (260 MB): 52 us = 5000 GB/s (issue slots 40-47 %, ALU 35, tensor pipe 31, 3 warps a scheduler).
-// Short: 512 tokens of 2 heads 3.9 us, a merge of splits 2 more.
+// copy rate; 64 rows of 128 to 8192, 32:8 heads (506 MB): 81 us = 6260 GB/s, int8 84.  Elsewhere the latency of a tile's chain (wait,
+// ldmatrix, conversion, dependent products, maximum, exponentials, transpose, products), of which a warp has one open: no unit is near
+// its limit.  More heads: 128 rows under a window of 4096, 32:2 heads, int8 (260 MB): 52 us = 5000 GB/s (issue slots 40-47 %, ALU 35,
+// tensor pipe 31, 3 warps a scheduler).  Heads of 64: 64 rows of 128 to 8192, 16:4 (127 MB): 27 us = 4640 GB/s (issue slots 32 %, ALU 30,
+// tensor pipe 10, 2 warps a scheduler).  Short: 512 tokens of 2 heads 3.9 us, a merge of splits 2 more.
 #include <limits.h>
 #include <math.h>
 

@@ -131,6 +131,9 @@ __device__ __noinline__ double squares_in_order(uint4 a, uint4 b, int rotary_dim
 // Nearly always the squares add up exactly, in whatever order: elements whose least exponent field is f are multiples of
 // q = 2^(f - 134), their squares and sums of them of q^2, and those below 2^53 q^2 are fp64 numbers.  (Zeros do not count; f is taken over
 // the warp; the sum is looked at with a bit to spare, since it is rounded where it is not exact.)
+//
+// Bound: instructions, 50 per element and lane with it, 12 without (issue slots 57 %, ALU 51, 3 warps a scheduler): 70.3 thousand tokens
+// of 40 heads of 128 864 us (850 without the look at the exponents), 240 without norms.
 template <int D, bool INTERLEAVED>
 __device__ __forceinline__ void normalise16(uint32_t (&x)[8], const uint16_t* w0, const uint16_t* w1, float eps, int rotary_dim, int lane) {
     double ss = 0.0;
@@ -393,7 +396,8 @@ __global__ void __launch_bounds__(kStreamWarps * 32, 1) rope_rows_stream_kernel(
     if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
 }
 
-// The general form, for rotary parts that are no whole number of lanes: a warp per vector, partners through shared memory.
+// The general form, for rotary parts that are no whole number of lanes: a warp per vector, partners through shared memory.  Bound: latency,
+// a warp has one vector in hand: 70.3 thousand tokens of 40 heads of 128 in 1167 us with a rotary part of 18, 1195 with 34.
 template <int D>
 __global__ void __launch_bounds__(256) rope_rows_any_kernel(const RowsParams p) {
     constexpr int EPL = D / 32;
