@@ -664,14 +664,16 @@ class Q8Cache(_QuantisedCache):
     @property
     def pools(self):
         """(tensor, segments of a page, whether a fork copies the whole page) of the three pools, for CachePages."""
-        if self._apart % 4:
+        page = self.scales[0].numel()
+        apart = page if self.num_pages == 1 and page % 4 == 0 else self._apart        # nothing follows a single page
+        if apart % 4:
             raise ValueError("scales: pages have to be a multiple of 16 bytes apart (empty makes them so)")
-        if self._apart - self.scales[0].numel() >= 4:      # more than padding: another cache's scales, which would be moved too
+        if apart - page >= 4:                              # more than padding: another cache's scales, which would be moved too
             raise ValueError("scales: 16 bytes or more between two pages")
-        if self.scales.storage_offset() + self.num_pages * self._apart > self.scales.untyped_storage().nbytes() // 4:
+        if self.scales.storage_offset() + self.num_pages * apart > self.scales.untyped_storage().nbytes() // 4:
             raise ValueError("scales: no room behind the last page for what lies between two pages")
         codes = 1 if self.layout == "token_major" else self.Hkv
-        held = self.scales.as_strided((self.num_pages, self._apart), (self._apart, 1))
+        held = self.scales.as_strided((self.num_pages, apart), (apart, 1))
         return [(self.k_codes, codes), (self.v_codes, codes), (held, 1, True)]
 
 

@@ -52,6 +52,8 @@ def test_scales_of_layers_side_by_side(rt, layers, H, ps, block):
         cache = rt.Q8Cache(*codes(6, ps, H, 64), every[:, layer])
         with pytest.raises(ValueError, match="scales"):
             cache.pools
+        one = rt.Q8Cache(*codes(1, ps, H, 64), every[2:3, layer]).pools[2][0]      # of a single page nothing lies between
+        assert one.shape == (1, H * (ps // block) * 2) and one.data_ptr() == every[2, layer].data_ptr()
     apart = torch.zeros(layers, 6, H, ps // block, 2, device="cuda")
     for layer in range(layers):
         assert len(rt.Q8Cache(*codes(6, ps, H, 64), apart[layer]).pools) == 3
