@@ -519,7 +519,7 @@ int ac_decode_plan_q4(const int32_t* token_counts_host, int B, int Hq, int Hkv, 
  * set (splits, workspace, inactive rows, window, sinks, row_order and max_context_len as there; options->rope must
  * be NULL; no status bit is set).  K and V enter as the exact values c * s + m; q is bf16, products and sums are
  * fp32, and the softmax weights times a V group's scale are rounded to fp16 (2^-11 relative, or 2^-31 of the
- * largest V scale seen, whichever is more) for the second product.  Slots at or past n_b, unreferenced pages and
+ * largest V scale seen, which counts as 2^-114 at least, whichever is more) for the second product.  Slots at or past n_b, unreferenced pages and
  * unused block-table entries never influence the result; a page id outside [0, num_pages) reads as zeros.
  * Outside the supported range: queries of magnitude 2^116 and more; rows whose tokens times the largest magnitude of V
  * reach 2^118 (the running sums are fp32, and a weight may be up to 2^8 before the final division); and
